@@ -1,0 +1,365 @@
+"""Operators to time that stand beside the MoE layer calls of a decoder: the rotation and the
+appending of new keys and values to a paged cache, the attention of new tokens over that cache,
+and the choice of the next tokens from logits.
+
+`run` computes an operator in its plain form from elementary torch operations, or, where `own`
+is true, through the package.  `exact` computes the same from the definitions in 64 bits.
+
+The cache's layout (one layer; D = head size, P = tokens per page, eight elements to 16 bytes):
+    keys   [page][kv head][D / 8][P][8]      element d of token t at [d / 8][t][d % 8]
+    values [page][kv head][P / 8][D][8]      element d of token t at [t / 8][d][t % 8]
+A sequence's token t lies in page pages[sequence][t / P], at t % P.  The new tokens' rows of
+sequence s are starts[s] .. starts[s + 1], its length (the new ones counted) lengths[s].
+"""
+import math
+import random
+
+import numpy as np
+import torch
+
+own = False
+
+TYPES = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+
+ATTENTION = {"dtype": "bf16", "heads": 32, "kv_heads": 4, "dim": 128, "page": 64, "window": 0,
+             "input": "bf16", "rope_dim": 128, "theta": 1e6, "adjacent": False}
+
+
+def _case(name, kind, **kw):
+    base = {} if kind == "sample" else dict(ATTENTION)
+    return dict(base, name=name, kind=kind, **kw)
+
+
+def listed():
+    return [
+        # one decode step of a full batch: latency, 64 scattered tokens
+        _case("append_decode64", "append", seqs=64, new_lo=1, new_hi=1, past_lo=100, past_hi=4000),
+        # a long prompt's chunk, straight from 32-bit projections
+        _case("append_prompt4096", "append", seqs=1, new_lo=4096, new_hi=4096, past_lo=0, past_hi=0,
+              input="f32"),
+        # ragged chunks of several prompts; half of each head rotated, adjacent pairs
+        _case("append_ragged9", "append", seqs=9, new_lo=1, new_hi=601, past_lo=0, past_hi=1999,
+              dtype="f16", input="f16", heads=16, kv_heads=16, dim=64, page=16, rope_dim=32,
+              theta=1e4, adjacent=True),
+        # one user, one token, a short context: latency
+        _case("attend_decode1", "attend", seqs=1, new_lo=1, new_hi=1, past_lo=776, past_hi=776),
+        # a full batch, every context of its own length
+        _case("attend_decode64", "attend", seqs=64, new_lo=1, new_hi=1, past_lo=200, past_hi=16000),
+        # one user with a very long context
+        _case("attend_long1", "attend", seqs=1, new_lo=1, new_hi=1, past_lo=131070, past_hi=131070,
+              dtype="f16", input="f16", heads=16, kv_heads=2, page=128),
+        # verification windows of five tokens (a target's token and four drafts)
+        _case("attend_window24", "attend", seqs=24, new_lo=5, new_hi=5, past_lo=1000, past_hi=9000),
+        # a chunk of a long prompt behind its earlier chunks: the largest product here
+        _case("attend_chunk4096", "attend", seqs=1, new_lo=4096, new_hi=4096, past_lo=12288,
+              past_hi=12288),
+        # a mixed batch of chunks, no shared heads, a sliding window
+        _case("attend_mixed12", "attend", seqs=12, new_lo=1, new_hi=513, past_lo=0, past_hi=3000,
+              dtype="f16", input="f16", heads=12, kv_heads=12, dim=64, page=16, window=1024,
+              rope_dim=64),
+        # one user's next token
+        _case("sample_1", "sample", rows=1, vocab=152001, dtype="f32"),
+        # a full batch's next tokens, every row with settings of its own
+        _case("sample_64", "sample", rows=64, vocab=152001, dtype="f32"),
+        # 64 verification windows of five rows
+        _case("sample_320", "sample", rows=320, vocab=32003, dtype="bf16"),
+    ]
+
+
+def _log_uniform(rng, lo, hi):
+    return min(hi, max(lo, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def _fits(case):
+    """No more work than the largest listed case of the kind, in a pool and in padded products of
+    its order of size (a window leaves most of a pool unread)."""
+    if case["kind"] != "sample":
+        last = case["past_hi"] + case["new_hi"]
+        if case["seqs"] * last * case["kv_heads"] * case["dim"] > 1 << 30:
+            return False
+        if case["seqs"] * last * case["heads"] * case["new_hi"] > 1 << 32:
+            return False
+    w = work(case)
+    most = [work(c) for c in listed() if c["kind"] == case["kind"]]
+    return all(w[k] <= max(m[k] for m in most) for k in w)
+
+
+def draw(rng):
+    while True:
+        kind = rng.choice(["append", "attend", "attend", "sample"])
+        if kind == "sample":
+            case = {"kind": kind, "rows": _log_uniform(rng, 1, 320),
+                    "vocab": _log_uniform(rng, 1000, 262144), "dtype": rng.choice(["f32", "bf16", "f16"])}
+        else:
+            dtype, dim = rng.choice(["bf16", "f16"]), rng.choice([64, 128, 128, 256])
+            kv = rng.choice([1, 2, 4, 8])
+            form = rng.choice(["token", "window", "chunks"])
+            seqs = _log_uniform(rng, 1, 64 if form != "chunks" else 12)
+            new = {"token": 1, "window": rng.randint(2, 8)}.get(form) or _log_uniform(rng, 9, 2048)
+            past = _log_uniform(rng, 1, 131072 if kind == "attend" else 8192)
+            case = {"kind": kind, "dtype": dtype, "dim": dim, "kv_heads": kv,
+                    "heads": kv * rng.choice([1, 2, 4, 5, 8]), "page": rng.choice([16, 32, 64, 128]),
+                    "window": rng.choice([0, 0, _log_uniform(rng, 100, 4096)]) if kind == "attend" else 0,
+                    "input": rng.choice([dtype, "f32"]) if kind == "append" else dtype,
+                    "rope_dim": rng.choice([dim, dim // 2]), "theta": rng.choice([1e4, 1e6]),
+                    "adjacent": rng.random() < 0.5, "seqs": seqs,
+                    "new_lo": new if form != "chunks" else rng.randint(1, new), "new_hi": new,
+                    "past_lo": rng.randint(0, past), "past_hi": past}
+        if _fits(case):
+            return case
+
+
+def _lengths(case):
+    """(new tokens, tokens before them) of every sequence, from the case alone."""
+    rng = random.Random(repr(sorted((k, v) for k, v in case.items() if k != "name")))
+    return [(rng.randint(case["new_lo"], case["new_hi"]), rng.randint(case["past_lo"], case["past_hi"]))
+            for _ in range(case["seqs"])]
+
+
+def _visible(first, last, window):
+    """Sum over positions first .. last - 1 of the keys that a token there sees."""
+    total = lambda n: n * (n + 1) // 2  # noqa: E731
+    pairs = total(last) - total(first)
+    if window:
+        over = lambda n: total(max(0, n - window))  # noqa: E731
+        pairs -= over(last) - over(first)
+    return pairs
+
+
+def work(case):
+    if case["kind"] == "sample":
+        size = {"f32": 4, "bf16": 2, "f16": 2}[case["dtype"]]
+        return {"bytes": case["rows"] * (case["vocab"] * size + 28), "flops": 2 * case["rows"] * case["vocab"]}
+    hq, hk, d = case["heads"], case["kv_heads"], case["dim"]
+    lengths = _lengths(case)
+    new = sum(n for n, _ in lengths)
+    if case["kind"] == "append":
+        size = 4 if case["input"] == "f32" else 2
+        return {"bytes": new * (hq + 2 * hk) * d * (size + 2),
+                "flops": new * (hq + hk) * case["rope_dim"] * 3}
+    w = case["window"]
+    keys = sum(min(n + p, n + w - 1) if w else n + p for n, p in lengths)
+    pairs = sum(_visible(p, n + p, w) for n, p in lengths)
+    return {"bytes": 2 * (2 * new * hq * d + 2 * keys * hk * d), "flops": 4 * d * hq * pairs}
+
+
+def prepare(case, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    randn = lambda *s, t=torch.float32: torch.randn(*s, generator=g, device="cuda", dtype=t)  # noqa: E731
+    rand = lambda *s: torch.rand(*s, generator=g, device="cuda")  # noqa: E731
+    state = {"case": case}
+    if case["kind"] == "sample":
+        rows, vocab = case["rows"], case["vocab"]
+        # a bulk of unlikely tokens, a tail of likely ones, some that a grammar forbids
+        z = 2.0 * randn(rows, vocab) - 2.0 * torch.log(rand(rows, vocab) + 1e-6)
+        z[rand(rows, vocab) < 0.01] = float("-inf")
+        state["logits"] = z.to(TYPES[case["dtype"]])
+        kind = rand(4, rows)
+        state["temperature"] = torch.where(kind[0] < 0.1, 0.0, 0.5 + rand(rows))
+        state["top_k"] = torch.where(kind[1] < 0.4, 0.0, torch.exp(rand(rows) * 7.0)).to(torch.int32)
+        state["top_p"] = torch.where(kind[2] < 0.4, 1.0, 0.5 + 0.5 * rand(rows))
+        state["min_p"] = torch.where(kind[3] < 0.5, 0.0, 0.1 * rand(rows))
+        state["u"] = rand(rows)
+        return state
+    t, hq, hk, d, page = TYPES[case["dtype"]], case["heads"], case["kv_heads"], case["dim"], case["page"]
+    lengths = _lengths(case)
+    new, total = [n for n, _ in lengths], [n + p for n, p in lengths]
+    counts = [-(-x // page) for x in total]
+    n_pages, width = sum(counts) + 3, max(counts)
+    order = torch.randperm(n_pages, generator=torch.Generator().manual_seed(seed)).to(torch.int32)
+    pages = torch.zeros(len(total), width, dtype=torch.int32)
+    at = 0
+    for s, c in enumerate(counts):  # every sequence's pages lie anywhere in the pool
+        pages[s, :c] = order[at:at + c]
+        at += c
+    state["pages"] = pages.cuda()
+    state["starts"] = torch.tensor([0] + list(np.cumsum(new)), dtype=torch.int32, device="cuda")
+    state["lengths"] = torch.tensor(total, dtype=torch.int32, device="cuda")
+    state["most_new"], tokens = max(new), sum(new)
+    state["keys"] = randn(n_pages, hk, d // 8, page, 8, t=t)
+    state["values"] = randn(n_pages, hk, page // 8, d, 8, t=t)
+    half = case["rope_dim"] // 2
+    state["freqs"] = torch.tensor([case["theta"] ** (-i / half) for i in range(half)], dtype=torch.float64,
+                                  device="cuda")
+    kind = TYPES[case["input"]]
+    state["q"] = (2.0 * randn(tokens, hq, d)).to(kind)
+    if case["kind"] == "append":
+        state["k"], state["v"] = randn(tokens, hk, d, t=kind), randn(tokens, hk, d, t=kind)
+    if own:
+        from paper_2607_09686_amd import KvCache
+        state["cache"] = KvCache(n_layers=1, n_heads=hq, n_kv_heads=hk, head_dim=d, page_tokens=page,
+                                 n_pages=n_pages, dtype=t, rope_theta=case["theta"],
+                                 rope_dim=case["rope_dim"], rope_adjacent=case["adjacent"],
+                                 window=case["window"], keys=state["keys"][None],
+                                 values=state["values"][None])
+    return state
+
+
+def run(state):
+    return {"append": _append, "attend": _attend, "sample": _sample}[state["case"]["kind"]](state)
+
+
+def _append(state):
+    case = state["case"]
+    if own:
+        q = state["cache"].append(state["k"], state["v"], state["pages"], state["starts"], state["lengths"],
+                                  q=state["q"])
+        return {"q": q, "keys": state["keys"], "values": state["values"]}
+    t, page = TYPES[case["dtype"]], case["page"]
+    rows = torch.arange(state["q"].shape[0], device="cuda", dtype=torch.int32)
+    seq = torch.searchsorted(state["starts"], rows, right=True) - 1
+    position = state["lengths"][seq] - state["starts"][seq + 1] + rows
+    angle = position.double()[:, None] * state["freqs"]
+    cos, sin = angle.cos().float()[:, None], angle.sin().float()[:, None]
+    r = case["rope_dim"]
+
+    def rotated(x):
+        x = x.float()
+        y = x.clone()
+        a, b = (slice(0, r, 2), slice(1, r, 2)) if case["adjacent"] else (slice(0, r // 2), slice(r // 2, r))
+        y[..., a] = x[..., a] * cos - x[..., b] * sin
+        y[..., b] = x[..., b] * cos + x[..., a] * sin
+        return y.to(t)
+
+    k, v = rotated(state["k"]), state["v"].to(t)
+    tokens, hk, d = k.shape
+    where, at = state["pages"][seq, (position // page).long()].long(), (position % page).long()
+    state["keys"][where, :, :, at] = k.view(tokens, hk, d // 8, 8)
+    state["values"][where, :, at // 8, :, at % 8] = v
+    return {"q": rotated(state["q"]), "keys": state["keys"], "values": state["values"]}
+
+
+def _attend(state):
+    case = state["case"]
+    if own:
+        return state["cache"].attend(state["q"], state["pages"], state["starts"], state["lengths"])
+    hq, hk, d, page = case["heads"], case["kv_heads"], case["dim"], case["page"]
+    group, most, seqs = hq // hk, state["most_new"], case["seqs"]
+    pages = state["pages"].long()
+    span = pages.shape[1] * page
+    k = state["keys"][pages].permute(0, 2, 1, 4, 3, 5).reshape(seqs, hk, span, d).float()
+    v = state["values"][pages].permute(0, 2, 1, 3, 5, 4).reshape(seqs, hk, span, d).float()
+    at = torch.arange(span, device="cuda")
+    count = state["starts"][1:] - state["starts"][:-1]
+    j = torch.arange(most, device="cuda")
+    real = j < count[:, None]
+    row = (state["starts"][:-1, None] + j).clamp_max(state["q"].shape[0] - 1)
+    q = state["q"][row].view(seqs, most, hk, group, d).permute(0, 2, 3, 1, 4).reshape(seqs, hk, group * most, d)
+    s = torch.matmul(q.float(), k.transpose(2, 3).contiguous()).mul_(d ** -0.5)
+    position = (state["lengths"] - count)[:, None] + j
+    seen = (at <= position[..., None]) & real[..., None]
+    if case["window"]:
+        seen &= at > position[..., None] - case["window"]
+    s = s.view(seqs, hk, group, most, span).masked_fill_(~seen[:, None, None], float("-inf"))
+    p = s.sub_(s.amax(-1, keepdim=True)).exp_()
+    total = p.sum(-1, keepdim=True)
+    o = torch.matmul(p.view(seqs, hk, group * most, span), v).view(seqs, hk, group, most, d) / total
+    return o.permute(0, 3, 1, 2, 4).reshape(seqs, most, hq, d)[real].to(TYPES[case["dtype"]])
+
+
+def _sample(state):
+    z, u, temperature = state["logits"], state["u"], state["temperature"]
+    if own:
+        from paper_2607_09686_amd import sample
+        tokens, probs = sample(z, u, temperature=temperature, top_k=state["top_k"], top_p=state["top_p"],
+                               min_p=state["min_p"])
+        return {"tokens": tokens, "probs": probs}
+    vocab = z.shape[1]
+    z, order = torch.sort(z.double(), dim=1, descending=True, stable=True)
+    greedy = (temperature <= 0)[:, None]
+    w = torch.exp((z - z[:, :1]) / torch.where(greedy[:, 0], 1.0, temperature).double()[:, None])
+    rank = torch.arange(vocab, device="cuda")
+    top_k = torch.where(state["top_k"] > 0, state["top_k"], vocab)[:, None]
+    w = torch.where(rank < torch.where(greedy, 1, top_k), w, 0.0)
+    before = torch.cumsum(w, 1) - w
+    top_p = state["top_p"].double()[:, None]
+    w = torch.where((top_p >= 1) | (rank == 0) | (before < top_p * w.sum(1, keepdim=True)), w, 0.0)
+    w = torch.where(w >= state["min_p"].double()[:, None], w, 0.0)
+    w = torch.zeros_like(w).scatter_(1, order, w)
+    up = torch.cumsum(w, 1)
+    tokens = torch.searchsorted(up, u.double()[:, None] * up[:, -1:], right=True)
+    probs = w.gather(1, tokens) / up[:, -1:]
+    return {"tokens": tokens[:, 0].to(torch.int32), "probs": probs[:, 0].float()}
+
+
+def exact(case, seed):
+    state = prepare(case, seed)
+    if case["kind"] == "sample":
+        return _exact_sample(state)
+    if case["kind"] == "append":
+        return _exact_append(state)
+    return _exact_attend(state)
+
+
+def _exact_append(state):
+    case = state["case"]
+    page, r, half = case["page"], case["rope_dim"], case["rope_dim"] // 2
+    starts, lengths, pages = (state[k].tolist() for k in ("starts", "lengths", "pages"))
+    keys, values = state["keys"].double(), state["values"].double()
+    q, k, v = state["q"].double(), state["k"].double(), state["v"].double()
+    freq = torch.tensor([case["theta"] ** (-i / half) for i in range(half)], dtype=torch.float64, device="cuda")
+    for s, length in enumerate(lengths):
+        lo, hi = starts[s], starts[s + 1]
+        position = torch.arange(length - (hi - lo), length, device="cuda")
+        turn = torch.exp(1j * position.double()[:, None] * freq)
+        for x in (q, k):
+            part = x[lo:hi, :, :r]
+            pair = part.unflatten(2, (half, 2)) if case["adjacent"] else part.unflatten(2, (2, half)).transpose(2, 3)
+            z = torch.complex(pair[..., 0].contiguous(), pair[..., 1].contiguous()) * turn[:, None]
+            pair = torch.view_as_real(z)
+            x[lo:hi, :, :r] = (pair if case["adjacent"] else pair.transpose(2, 3)).flatten(2)
+        table = torch.tensor(pages[s], device="cuda")[position // page]
+        at = position % page
+        keys[table, :, :, at] = k[lo:hi].unflatten(2, (-1, 8))
+        values[table, :, at // 8, :, at % 8] = v[lo:hi]
+    return {"q": q, "keys": keys, "values": values}
+
+
+def _exact_attend(state):
+    case = state["case"]
+    hk, d, group = case["kv_heads"], case["dim"], case["heads"] // case["kv_heads"]
+    starts, lengths, page = state["starts"].tolist(), state["lengths"].tolist(), case["page"]
+    out = torch.empty(state["q"].shape, dtype=torch.float64, device="cuda")
+    for s, length in enumerate(lengths):
+        table = state["pages"][s, :-(-length // page)].long()
+        lo, hi = starts[s], starts[s + 1]
+        position = torch.arange(length - (hi - lo), length, device="cuda")
+        at = torch.arange(length, device="cuda")
+        hidden = at > position[:, None]
+        if case["window"]:
+            hidden |= at <= position[:, None] - case["window"]
+        for h in range(hk):
+            k = state["keys"][table, h].transpose(1, 2).reshape(-1, d)[:length].double()
+            v = state["values"][table, h].transpose(2, 3).reshape(-1, d)[:length].double()
+            kt = k.t().contiguous()
+            for i in range(h * group, (h + 1) * group):
+                x = state["q"][lo:hi, i].double().contiguous() @ kt / math.sqrt(d)
+                out[lo:hi, i] = torch.softmax(x.masked_fill_(hidden, -math.inf), 1) @ v
+    return out
+
+
+def _exact_sample(state):
+    z = state["logits"].double().cpu().numpy()
+    setting = {k: state[k].double().cpu().numpy() for k in ("u", "temperature", "top_k", "top_p", "min_p")}
+    tokens, probs = np.empty(len(z), np.int32), np.empty(len(z))
+    for r, row in enumerate(z):
+        u, t, k, p, least = (float(setting[n][r]) for n in ("u", "temperature", "top_k", "top_p", "min_p"))
+        if t <= 0:
+            tokens[r], probs[r] = int(np.argmax(row)), 1.0
+            continue
+        order = np.lexsort((np.arange(row.size), -row))  # falling logits, ties by rising index
+        if k > 0:
+            order = order[:int(k)]
+        w = np.exp((row[order] - row[order[0]]) / t)
+        if p < 1:
+            before = np.concatenate([[0.0], np.cumsum(w)[:-1]])
+            keep = before < p * w.sum()
+            keep[0] = True
+            order, w = order[keep], w[keep]
+        order, w = order[w >= least], w[w >= least]
+        by = np.argsort(order)
+        order, w = order[by], w[by]
+        up = np.cumsum(w)
+        i = int(np.searchsorted(up, u * up[-1], side="right"))
+        tokens[r], probs[r] = order[i], w[i] / up[-1]
+    return {"tokens": torch.from_numpy(tokens), "probs": torch.from_numpy(probs)}
