@@ -6,8 +6,8 @@ and the choice of the next tokens from logits.
 is true, through the package.  `exact` computes the same from the definitions in 64 bits.
 
 The cache's layout (one layer; D = head size, P = tokens per page, eight elements to 16 bytes):
-    keys   [page][kv head][D / 8][P][8]      element d of token t at [d / 8][t][d % 8]
-    values [page][kv head][P / 8][D][8]      element d of token t at [t / 8][d][t % 8]
+    keys   [page][kv head][P / 16][D / 8][16][8]  element d of token t at [t / 16][d / 8][t % 16][d % 8]
+    values [page][kv head][P / 16][2][D][8]       element d of token t at [t / 16][t / 8 % 2][d][t % 8]
 A sequence's token t lies in page pages[sequence][t / P], at t % P.  The new tokens' rows of
 sequence s are starts[s] .. starts[s + 1], its length (the new ones counted) lengths[s].
 """
@@ -176,8 +176,8 @@ def prepare(case, seed):
     state["starts"] = torch.tensor([0] + list(np.cumsum(new)), dtype=torch.int32, device="cuda")
     state["lengths"] = torch.tensor(total, dtype=torch.int32, device="cuda")
     state["most_new"], tokens = max(new), sum(new)
-    state["keys"] = randn(n_pages, hk, d // 8, page, 8, t=t)
-    state["values"] = randn(n_pages, hk, page // 8, d, 8, t=t)
+    state["keys"] = randn(n_pages, hk, page // 16, d // 8, 16, 8, t=t)
+    state["values"] = randn(n_pages, hk, page // 16, 2, d, 8, t=t)
     half = case["rope_dim"] // 2
     state["freqs"] = torch.tensor([case["theta"] ** (-i / half) for i in range(half)], dtype=torch.float64,
                                   device="cuda")
@@ -224,8 +224,8 @@ def _append(state):
     k, v = rotated(state["k"]), state["v"].to(t)
     tokens, hk, d = k.shape
     where, at = state["pages"][seq, (position // page).long()].long(), (position % page).long()
-    state["keys"][where, :, :, at] = k.view(tokens, hk, d // 8, 8)
-    state["values"][where, :, at // 8, :, at % 8] = v
+    state["keys"][where, :, at // 16, :, at % 16] = k.view(tokens, hk, d // 8, 8)
+    state["values"][where, :, at // 16, at // 8 % 2, :, at % 8] = v
     return {"q": rotated(state["q"]), "keys": state["keys"], "values": state["values"]}
 
 
@@ -237,8 +237,8 @@ def _attend(state):
     group, most, seqs = hq // hk, state["most_new"], case["seqs"]
     pages = state["pages"].long()
     span = pages.shape[1] * page
-    k = state["keys"][pages].permute(0, 2, 1, 4, 3, 5).reshape(seqs, hk, span, d).float()
-    v = state["values"][pages].permute(0, 2, 1, 3, 5, 4).reshape(seqs, hk, span, d).float()
+    k = state["keys"][pages].permute(0, 2, 1, 3, 5, 4, 6).reshape(seqs, hk, span, d).float()
+    v = state["values"][pages].permute(0, 2, 1, 3, 4, 6, 5).reshape(seqs, hk, span, d).float()
     at = torch.arange(span, device="cuda")
     count = state["starts"][1:] - state["starts"][:-1]
     j = torch.arange(most, device="cuda")
@@ -310,8 +310,8 @@ def _exact_append(state):
             x[lo:hi, :, :r] = (pair if case["adjacent"] else pair.transpose(2, 3)).flatten(2)
         table = torch.tensor(pages[s], device="cuda")[position // page]
         at = position % page
-        keys[table, :, :, at] = k[lo:hi].unflatten(2, (-1, 8))
-        values[table, :, at // 8, :, at % 8] = v[lo:hi]
+        keys[table, :, at // 16, :, at % 16] = k[lo:hi].unflatten(2, (-1, 8))
+        values[table, :, at // 16, at // 8 % 2, :, at % 8] = v[lo:hi]
     return {"q": q, "keys": keys, "values": values}
 
 
@@ -329,8 +329,8 @@ def _exact_attend(state):
         if case["window"]:
             hidden |= at <= position[:, None] - case["window"]
         for h in range(hk):
-            k = state["keys"][table, h].transpose(1, 2).reshape(-1, d)[:length].double()
-            v = state["values"][table, h].transpose(2, 3).reshape(-1, d)[:length].double()
+            k = state["keys"][table, h].transpose(2, 3).reshape(-1, d)[:length].double()
+            v = state["values"][table, h].transpose(3, 4).reshape(-1, d)[:length].double()
             kt = k.t().contiguous()
             for i in range(h * group, (h + 1) * group):
                 x = state["q"][lo:hi, i].double().contiguous() @ kt / math.sqrt(d)
