@@ -289,6 +289,139 @@ int moe_probe_h2d(const void *host_src, uint64_t chunk_bytes, int32_t n_chunks, 
  * MOE_EHIP on a HIP failure. */
 int moe_probe_hbm_read(uint64_t bytes, int32_t iters, double *read_us, double *empty_us);
 
+/* ------------------------------------------------------------------------
+ * Beside the layer calls: what a decoder needs between and after them.  The
+ * attention half of a layer, over a paged key/value cache whose bytes are the
+ * K(n) of the budget plan below, and the choice of the next tokens from logits.
+ *
+ * These functions keep no state: every pointer is the caller's.  They queue
+ * their kernels on hip_stream (NULL: the null stream of the current device),
+ * on that stream's device, allocate nothing, never wait and never read device
+ * memory on the host, so they may be captured into a HIP graph and replayed
+ * with other contents at the same addresses.  Calls on several streams at once
+ * are independent as long as their outputs, workspaces and written pages are.
+ * ------------------------------------------------------------------------ */
+#define MOE_F32 0
+#define MOE_F16 1
+#define MOE_BF16 30
+
+/* One layer's paged cache and a batch of new tokens.
+ *
+ * A page holds page_tokens consecutive tokens of one sequence, for every KV
+ * head.  keys is [n_pages][n_kv_heads][page_tokens/16][head_dim/8][16][8]: element
+ * d of the token at place t of the page is at [t/16][d/8][t%16][d%8].  values is
+ * [n_pages][n_kv_heads][page_tokens/16][2][head_dim][8]: [t/16][t/8%2][d][t%8].
+ * (The order in which the matrix cores take them: 16 tokens' keys, or values,
+ * are one contiguous run.)  Token t of sequence s lies in page
+ * pages[s][t / page_tokens], at place t % page_tokens.
+ *
+ * The new tokens of sequence s are rows starts[s] .. starts[s+1]-1 of q, k, v
+ * and out; lengths[s] counts the sequence's tokens with the new ones in, so new
+ * token j has position lengths[s] - (starts[s+1] - starts[s]) + j.  starts must
+ * rise from 0; rows from starts[n_seqs] to n_tokens (a padded batch) are neither
+ * read nor written.  A sequence without new tokens costs nothing, whatever its
+ * length says.
+ *
+ * The device arrays are checked on the device, since the host never sees them.
+ * A sequence whose length is less than its new tokens or more than its table
+ * holds is not served: its rows of q_out and out become NaN and nothing of it
+ * is written to the cache.  A page id outside [0, n_pages): the new tokens on it
+ * are not written, and the rows of out that read it become NaN (rows computed
+ * together with them may too).  *status, if given, gets MOE_KV_BAD_LENGTH or
+ * MOE_KV_BAD_PAGE or-ed in (the library never clears it).  No access leaves the
+ * arrays' stated sizes whatever they hold. */
+#define MOE_KV_BAD_PAGE 1
+#define MOE_KV_BAD_LENGTH 2
+typedef struct {
+  int32_t dtype;       /* MOE_BF16 or MOE_F16: cache, q of moe_kv_attend, q_out, out */
+  int32_t n_heads;     /* query heads, a multiple of n_kv_heads, <= 1024: query head h reads KV
+                          head h / (n_heads / n_kv_heads) */
+  int32_t n_kv_heads;
+  int32_t head_dim;    /* 64, 128 or 256 */
+  int32_t page_tokens; /* a power of two, 16..1024 */
+  int32_t n_pages;     /* pages in the pool */
+  int32_t max_pages;   /* width of the page table; max_pages * page_tokens <= 2^30 */
+  int32_t n_seqs;      /* 0..65536; n_seqs * n_kv_heads <= 2^22 */
+  int32_t n_tokens;    /* rows of q, k, v, out: 0..2^24; n_tokens * n_heads <= 2^27 */
+  int32_t pad;
+  void *keys, *values;    /* device, 16-byte aligned; one layer's pools */
+  const int32_t *pages;   /* device [n_seqs][max_pages]; entries past a sequence's length are not read */
+  const int32_t *starts;  /* device [n_seqs + 1] */
+  const int32_t *lengths; /* device [n_seqs] */
+  int32_t *status;        /* device, nullable */
+  void *hip_stream;
+} moe_kv_batch;
+
+/* The rotation of queries and keys by their position p: the pair (a, b) of
+ * elements turns by p * freq[i], (a cos - b sin, b cos + a sin).  dim elements of
+ * a head turn, the rest pass: pair i is elements (i, i + dim/2), or with
+ * adjacent != 0 elements (2i, 2i + 1).  The angle is taken in 64 bits. */
+typedef struct {
+  int32_t dim;        /* a multiple of 16, 0..head_dim */
+  int32_t adjacent;
+  const double *freq; /* device [dim/2], radians per position */
+} moe_kv_rope;
+
+/* Turn the new tokens' keys and write them and the values to the cache; turn q
+ * (nullable) into q_out in the same launch.  k, v: device, in_dtype (the cache's
+ * dtype or MOE_F32), token rows of [n_kv_heads][head_dim], k_stride and v_stride
+ * elements apart; q likewise with n_heads; q_out in the cache's dtype.  Pointers
+ * and strides are multiples of 16 bytes, strides at most 2^32 elements.  q_out may be q itself (same dtype and
+ * stride).  rope NULL: nothing turns.  Each value is rounded once.  Two
+ * sequences must not have new tokens at one place of one page (either may end up
+ * there). */
+int moe_kv_append(const moe_kv_batch *b, const moe_kv_rope *rope, int32_t in_dtype, const void *k, int64_t k_stride,
+                  const void *v, int64_t v_stride, const void *q, int64_t q_stride, void *q_out,
+                  int64_t q_out_stride);
+
+/* Attention of the new tokens over the cache (which holds them already):
+ *   out = sum_t softmax_t(scale * q . k_t) v_t
+ * over the sequence's tokens t at or before the row's own position and, with
+ * window > 0, after position - window.  What a row does not see has no effect on
+ * it, whatever it holds.  q, out: device, token rows of [n_heads][head_dim] in
+ * the batch's dtype, strides in elements, multiples of 16 bytes; out must not
+ * overlap q.  Sums and softmax in fp32; probabilities are rounded to the dtype
+ * for their product with the values.  Results do not depend on where a
+ * sequence's pages lie; they may differ in rounding with what else is in the
+ * batch (the work is cut by the batch's lengths), never from run to run.
+ * workspace: device scratch of the size that moe_kv_attend_workspace gives for
+ * the same batch (its counts matter, not its arrays), 16-byte aligned, contents
+ * irrelevant; calls that may overlap in time need one each. */
+int moe_kv_attend(const moe_kv_batch *b, int32_t window, float scale, const void *q, int64_t q_stride, void *out,
+                  int64_t out_stride, void *workspace, uint64_t workspace_bytes);
+int moe_kv_attend_workspace(const moe_kv_batch *b, uint64_t *bytes);
+
+/* Choose one token from each row of logits.  Per row, in this order: weights
+ * exp((z - max) / temperature); the top_k largest; of those, in falling order,
+ * the ones before which less than top_p of their mass lies; of those, the ones of
+ * at least min_p times the largest weight; then the first one, by rising index,
+ * at which the running mass exceeds u times the mass.  Equal logits rank by rising
+ * index.  temperature not above 0 (or NaN): the largest logit, probability 1.  Off:
+ * top_k <= 0 or >= vocab, top_p >= 1 or NaN, min_p <= 0 or NaN, NULL arrays
+ * (temperature NULL: 1).  The largest logit is never filtered out.  NaN and -inf
+ * logits are never chosen; +inf logits share all of the mass; a row with nothing
+ * else than NaN and -inf gives token -1, probability 0.  u outside [0, 1) acts as
+ * the nearest end, NaN as 0.  Decisions are taken on weights of 64 bits, held to
+ * 2^-42 or better of the largest; the same inputs give the same tokens however
+ * the rows are split over the device. */
+typedef struct {
+  int32_t dtype;            /* of the logits: MOE_F32, MOE_BF16 or MOE_F16 */
+  int32_t n_rows;           /* 0..2^20 */
+  int32_t vocab;            /* 1..2^20 */
+  int32_t pad;
+  const void *logits;       /* device, [n_rows] rows of vocab elements, row_stride elements apart */
+  int64_t row_stride;
+  const float *temperature; /* device [n_rows], nullable */
+  const int32_t *top_k;     /* device [n_rows], nullable */
+  const float *top_p;       /* device [n_rows], nullable */
+  const float *min_p;       /* device [n_rows], nullable */
+  const float *u;           /* device [n_rows], uniform in [0, 1) */
+  void *hip_stream;
+} moe_sample_batch;
+/* token: device [n_rows]; prob: device [n_rows], nullable: the chosen token's
+ * share of the mass that the filters left. */
+int moe_sample(const moe_sample_batch *b, int32_t *token, float *prob);
+
 /* Static budget plan (no HIP dependency, no allocation).  The paper's Native
  * Serving Path section derives the slot count of the routed layers from the
  * requested cache bytes, the routed layer count, the bytes of one expert block,

@@ -6,7 +6,8 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmoecache.so")
-SOURCES = ["wide_q6_k.hip", "wide_q4_k.hip", "wide_q8_0.hip", "wide_q4_0.hip", "kernels.hip", "tables.hip", "probe.hip", "moecache.cpp", "slot_lru.cpp", "planner.cpp", "policy.cpp", "pack.cpp"]
+SOURCES = ["wide_q6_k.hip", "wide_q4_k.hip", "wide_q8_0.hip", "wide_q4_0.hip", "kernels.hip", "tables.hip", "probe.hip", "moecache.cpp", "slot_lru.cpp", "planner.cpp", "policy.cpp", "pack.cpp",
+           "serve/attend_d256.hip", "serve/attend_d128.hip", "serve/attend_d64.hip", "serve/append.hip", "serve/sample.hip", "serve/serve.cpp"]
 ARCH = os.environ.get("MOECACHE_ARCH", "gfx950")
 # packed fp32 instructions are disabled: the compiler must not emit them
 HIPFLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-Wall",
@@ -26,7 +27,7 @@ def build(verbose=False, jobs=4):
     os.makedirs(objdir, exist_ok=True)
     procs, objs = [], []
     for src in SOURCES:
-        obj = os.path.join(objdir, src + ".o")
+        obj = os.path.join(objdir, src.replace("/", "_") + ".o")
         lang = [] if src.endswith(".hip") else ["-x", "hip"]
         cmd = [hipcc, *HIPFLAGS, *lang, "-c", os.path.join(CSRC, src), "-o", obj]
         if verbose:

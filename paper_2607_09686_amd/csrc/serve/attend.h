@@ -1,0 +1,738 @@
+// Attention of new tokens over a paged key/value cache (causal, optional sliding window, query
+// heads sharing KV heads), for gfx950.
+//
+//   o_r = sum_t softmax_t(scale q_r . k_t) v_t,   t <= p_r (and t > p_r - window)
+//
+// A tile is up to M rows (new token, query head of one KV head's group), token-major, of one
+// sequence: the heads that share a KV head share its keys and values.  The scores are computed
+// transposed, S^T = K Q^T with v_mfma_f32_32x32x16, so that a lane holds 16 keys of ONE row: the
+// row maximum and sum are lane-local but for one exchange between the wave's halves.  Row m of
+// the product is fed key pi(m), pi swapping bits 2 and 3, after which a lane's eight
+// consecutive accumulators are eight consecutive keys: exactly the B operand of the second
+// product O^T = V^T P^T, which therefore takes the probabilities from the registers they
+// were computed in, with no pass through shared memory.
+//
+// The cache is laid out for these operands, 16 tokens at a time: a group's keys as [D/8][16][8] and
+// its values as [2][D][8] (per page and head, P/16 groups).  Every operand load is 16 bytes per
+// lane at a constant offset within a group, a group's operands are 32 D contiguous bytes, and a
+// page's size only decides where its groups lie.
+//
+// Work is cut into units of (tile, range of keys).  The lengths are on the device only, so each
+// block derives the cut from them itself: with W = sum over tiles of the keys they span, a unit
+// takes C = max(min_keys, ceil(W * kv_heads / target)) keys, which bounds the number of units by
+// target / kv_heads + tiles whatever the lengths are (the grid), and evens out ragged
+// batches.  A tile of several units leaves partial (m, l, o) rows in the workspace, joined by a
+// second launch.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "serve.h"
+
+namespace moecache {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+
+template <class E>
+struct Vec {
+  typedef E x8 __attribute__((ext_vector_type(8)));
+  typedef E x4 __attribute__((ext_vector_type(4)));
+};
+
+__device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c, __bf16) {
+  typedef Vec<__bf16>::x8 x8;
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c, _Float16) {
+  typedef Vec<_Float16>::x8 x8;
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
+}
+
+constexpr int kLanes = 64;
+constexpr int kThreads = 256, kWaves = kThreads / kLanes;
+constexpr int kIds = 1024;  // page ids of a unit held in LDS at a time
+constexpr float kNegInf = -__builtin_inff();
+
+__device__ __forceinline__ int64_t wave_sum(int64_t v) {
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+
+// One sequence's share of the batch, read defensively: whatever starts and lengths hold, rows
+// stay within [0, n_tokens) and keys within the table.
+struct Seq {
+  int first, count, length;  // rows first .. first + count - 1; keys 0 .. length - 1
+  bool bad;                  // a length its table cannot hold, or shorter than its new tokens
+};
+__device__ __forceinline__ Seq seq_of(const KvView &kv, int s) {
+  const int a = min(max(kv.starts[s], 0), kv.n_tokens), b = min(max(kv.starts[s + 1], a), kv.n_tokens);
+  const int len = kv.lengths[s];
+  const bool bad = len < b - a || len > (kv.max_pages << kv.page_shift);
+  return Seq{a, b - a, bad ? 0 : len, bad};
+}
+
+// Tiles of a sequence, and the keys that one of them can span (its window starts at a multiple of
+// 64 at or below the first row's).
+template <int M>
+__device__ __forceinline__ int tiles_of(const AttendArgs &a, const Seq &q) {
+  return (int)(((int64_t)q.count * a.kv.group + M - 1) / M);
+}
+template <int M>
+__device__ __forceinline__ int span_of(const AttendArgs &a, const Seq &q) {
+  if (!a.window) return q.length;
+  const int64_t reach = (int64_t)a.window + (M - 1) / a.kv.group + 1 + 64;
+  return (int)min((int64_t)q.length, reach);
+}
+__device__ __forceinline__ int units_of(int span, int C) { return max(1, (span + C - 1) / C); }
+
+// Keys of a unit, from the whole batch.  All lanes of a wave get the same value.
+template <int M>
+__device__ __forceinline__ int plan_keys(const AttendArgs &a, int *widest) {
+  int64_t work = 0;
+  int wide = 0;
+  for (int s = threadIdx.x % kLanes; s < a.kv.n_seqs; s += kLanes) {
+    const Seq q = seq_of(a.kv, s);
+    const int t = tiles_of<M>(a, q), span = span_of<M>(a, q);
+    work += (int64_t)t * span;
+    if (t) wide = max(wide, span);
+  }
+  work = wave_sum(work);
+  for (int o = 32; o; o >>= 1) wide = max(wide, __shfl_xor(wide, o));
+  *widest = wide;
+  const int64_t c = (work * a.kv.kv_heads + a.target - 1) / a.target;
+  return (int)min((int64_t)1 << 30, max((int64_t)a.min_keys, (c + 63) & ~(int64_t)63));
+}
+
+// Where a unit (or a sequence's first one) stands.
+struct Place {
+  int seq, index;   // index: the unit's number within its sequence
+  int64_t slot;     // first partial-result slot of the sequence
+  Seq q;
+};
+// The sequence holding unit `want` (by_seq: the sequence `want` itself).  False past the last one.
+template <int M>
+__device__ __forceinline__ bool plan_find(const AttendArgs &a, int C, int want, bool by_seq, Place *out) {
+  int64_t units = 0, slots = 0;
+  const int lane = threadIdx.x % kLanes;
+  for (int s0 = 0; s0 < a.kv.n_seqs; s0 += kLanes) {
+    Seq q{0, 0, 0, false};
+    if (s0 + lane < a.kv.n_seqs) q = seq_of(a.kv, s0 + lane);
+    const int per = units_of(span_of<M>(a, q), C);
+    const int64_t n = (int64_t)tiles_of<M>(a, q) * per, m = per > 1 ? n : 0;
+    int64_t nu = n, ns = m;  // inclusive prefix sums over the lanes
+    for (int o = 1; o < kLanes; o <<= 1) {
+      const int64_t u = __shfl_up(nu, o), v = __shfl_up(ns, o);
+      if (lane >= o) nu += u, ns += v;
+    }
+    const bool hit = by_seq ? s0 + lane == want : want < units + nu;
+    const uint64_t any = __ballot(hit);
+    if (any) {
+      const int at = __ffsll((unsigned long long)any) - 1;
+      out->seq = s0 + at;
+      out->index = (int)(want - (units + __shfl(nu - n, at)));
+      out->slot = slots + __shfl(ns - m, at);
+      out->q = Seq{__shfl(q.first, at), __shfl(q.count, at), __shfl(q.length, at), (bool)__shfl((int)q.bad, at)};
+      return true;
+    }
+    units += __shfl(nu, kLanes - 1);
+    slots += __shfl(ns, kLanes - 1);
+  }
+  return false;
+}
+
+// Keys lo .. hi - 1 that rows of a tile see, lo rounded down to a multiple of 64; the tile's units
+// cut this range from lo on.
+struct Range {
+  int lo, hi;
+};
+template <int M>
+__device__ __forceinline__ Range range_of(const AttendArgs &a, const Seq &q, int tile) {
+  const int rows = q.count * a.kv.group;
+  const int t0 = tile * M / a.kv.group, t1 = min(tile * M + M, rows) - 1;
+  const int before = q.length - q.count;
+  Range r;
+  r.hi = before + t1 / a.kv.group + 1;
+  r.lo = a.window ? max(0, before + t0 - a.window + 1) & ~63 : 0;
+  return r;
+}
+
+// The rows' state in one wave: 32 rows, lane n and lane n + 32 hold row n.
+template <int D>
+struct Rows {
+  f32x16 acc[D / 32];  // o^T: d = 32 i + 8 (r / 4) + 4 half + r % 4
+  float m, l;          // running maximum (log2 units, both halves alike), this lane's share of the sum
+};
+
+// Key (within its 32) of accumulator r of a score product, for this lane's half.
+__device__ __forceinline__ int key_of(int r, int half) { return 16 * (r / 8) + 8 * half + r % 8; }
+
+// Scores of keys that their row does not see become -inf.
+template <int N>
+__device__ __forceinline__ void mask_scores(f32x16 (&s)[N], int t0, int pos, int floor) {
+  const int half = threadIdx.x % kLanes / 32;
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int t = t0 + 32 * n + key_of(r, half);
+      if (t > pos || t <= floor) s[n][r] = kNegInf;
+    }
+}
+
+// Scores to probabilities over 32 * N keys: takes the new maximum, rescales the rows only where
+// some row's maximum rose, and packs the B operands of the second product.
+// Probabilities are rounded to the cache's type, the type the matrix cores multiply; the sum
+// is taken in fp32 before that.
+template <class E, int D, int N>
+__device__ __forceinline__ void softmax_step(f32x16 (&s)[N], Rows<D> &st, u32x4 (&p)[2 * N], float scale) {
+  float mx = s[0][0];
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[n][r]);
+  mx = fmaxf(mx, __shfl_xor(mx, 32));
+  const float top = fmaxf(st.m, mx * scale);
+  const float base = top == kNegInf ? 0.f : top;
+  if (__any(top > st.m)) {
+    const float shrink = __builtin_amdgcn_exp2f(st.m - base);
+    st.l *= shrink;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) st.acc[i][r] *= shrink;
+    st.m = top;
+  }
+  typedef typename Vec<E>::x8 x8;
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      x8 e;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float v = __builtin_amdgcn_exp2f(fmaf(s[n][8 * c + j], scale, -base));
+        st.l += v;
+        e[j] = (E)v;
+      }
+      p[2 * n + c] = __builtin_bit_cast(u32x4, e);
+    }
+}
+
+// v with the elements that are not among the first n (of its 8) cleared
+__device__ __forceinline__ u32x4 keep_first(u32x4 v, int n) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] &= n >= 2 * i + 2 ? 0xffffffffu : n == 2 * i + 1 ? 0xffffu : 0u;
+  return v;
+}
+
+// Values that are not finite, as numbers whose sums over 16 keys tell which kinds were among
+// them: +inf 1, -inf 128, NaN 16384, 0 for a finite value; all exact in the type E.
+template <class E>
+struct Odd;
+template <>
+struct Odd<__bf16> {
+  static constexpr uint32_t exponent = 0x7f80, one = 0x3f80, inf = 0x3f80, minus = 0x4300, nan = 0x4680;
+};
+template <>
+struct Odd<_Float16> {
+  static constexpr uint32_t exponent = 0x7c00, one = 0x3c00, inf = 0x3c00, minus = 0x5800, nan = 0x7400;
+};
+template <class E>
+__device__ __forceinline__ bool any_odd(u32x4 v) {
+  constexpr uint32_t x = Odd<E>::exponent;
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) odd |= (v[i] & x) == x || (v[i] >> 16 & x) == x;
+  return odd;
+}
+template <class E>
+__device__ __forceinline__ uint32_t odd_code(uint32_t e) {  // of one element's bits
+  constexpr uint32_t x = Odd<E>::exponent;
+  return (e & x) != x ? 0u : (e & 0x7fffu) != x ? Odd<E>::nan : e & 0x8000u ? Odd<E>::minus : Odd<E>::inf;
+}
+
+// Makes the values of 16 keys from t0 on fit for the second product in a step some of whose keys
+// some rows do not see.  Keys at or past `end` hold whatever the page held: their values are
+// cleared.  A value that is not finite must not reach rows that do not see its key (0 * inf is a
+// NaN), so such values are cleared too, and a product of their kinds with which row sees which key
+// says which rows they do reach (their weight there is positive: an infinity stays the infinity
+// it was).
+template <class E, int D>
+__device__ __forceinline__ void clean_values(u32x4 (&v)[D / 32], Rows<D> &st, int t0, int end, int pos, int floor) {
+  const int half = threadIdx.x % kLanes / 32, t = t0 + 8 * half;
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) {
+    v[i] = keep_first(v[i], min(8, max(0, end - t)));
+    odd |= any_odd<E>(v[i]);
+  }
+  if (__any(odd)) {
+    u32x4 sees;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int t2 = t + 2 * j;
+      sees[j] = (t2 <= pos && t2 > floor ? Odd<E>::one : 0u) |
+                (t2 + 1 <= pos && t2 + 1 > floor ? Odd<E>::one << 16 : 0u);
+    }
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+      u32x4 code;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t lo = odd_code<E>(v[i][j] & 0xffffu), hi = odd_code<E>(v[i][j] >> 16);
+        code[j] = lo | hi << 16;
+        v[i][j] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
+      }
+      const f32x16 kinds = mma(code, sees, f32x16{}, E());
+      __builtin_amdgcn_sched_barrier(0);  // one product's registers at a time
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int k = (int)kinds[r];
+        const bool nan = k >= 16384, minus = k & 0x3f80, plus = k & 0x7f;
+        st.acc[i][r] += nan || (minus && plus) ? __builtin_nanf("")
+                        : minus                ? kNegInf
+                        : plus                 ? __builtin_inff()
+                                               : 0.f;
+      }
+    }
+  }
+}
+
+// This lane's row of the tile as the B operand of S^T = K Q^T: q[c] = elements 16 c + 8 half ...
+template <int D>
+__device__ __forceinline__ void load_q(const AttendArgs &a, const Seq &q, int kvh, int row, u32x4 (&out)[D / 16]) {
+  const int half = threadIdx.x % kLanes / 32, rows = q.count * a.kv.group;
+  if (row < rows) {
+    const int tok = q.first + row / a.kv.group, head = kvh * a.kv.group + row % a.kv.group;
+    const uint16_t *src = (const uint16_t *)a.q + (int64_t)tok * a.q_stride + (int64_t)head * D + 8 * half;
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) out[c] = *(const u32x4 *)(src + 16 * c);
+  } else {
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) out[c] = u32x4{};
+  }
+}
+
+// Writes four consecutive elements of a finished row.
+template <class E, int D>
+__device__ __forceinline__ void store_out(const AttendArgs &a, const Seq &q, int kvh, int row, int d, f32x4 v) {
+  const int tok = q.first + row / a.kv.group, head = kvh * a.kv.group + row % a.kv.group;
+  typename Vec<E>::x4 e;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) e[i] = (E)v[i];
+  *(typename Vec<E>::x4 *)((E *)a.out + (int64_t)tok * a.out_stride + (int64_t)head * D + d) = e;
+}
+
+// Partial results: o rows of slot (slot, kvh), then (m, l) pairs of all slots.
+template <int D, int M>
+__device__ __forceinline__ float *part_o(const AttendArgs &a, int64_t slot, int kvh, int row) {
+  return a.part + ((slot * a.kv.kv_heads + kvh) * M + row) * D;
+}
+template <int D, int M>
+__device__ __forceinline__ float *part_ml(const AttendArgs &a, int64_t slot, int kvh, int row) {
+  return a.part + (int64_t)a.max_slots * a.kv.kv_heads * M * D + ((slot * a.kv.kv_heads + kvh) * M + row) * 2;
+}
+
+// The ids of the unit's pages pg0 .. , at most kIds of them, into LDS; an id outside the pool is
+// taken as page 0 and reported.  Ends with a barrier.
+__device__ __forceinline__ void load_ids(const KvView &kv, int seq, int pg0, int pg_last, int *ids, int *bad) {
+  const int n = min(kIds, pg_last - pg0 + 1);
+  for (int i = threadIdx.x; i < n; i += kThreads) {
+    const int id = kv.pages[(int64_t)seq * kv.max_pages + pg0 + i];
+    const bool ok = (unsigned)id < (unsigned)kv.n_pages;
+    ids[i] = ok ? id : 0;
+    if (!ok) {
+      *bad = 1;
+      if (kv.status) atomicOr(kv.status, kKvBadPage);
+    }
+  }
+  __syncthreads();
+}
+
+// What a block works on.
+struct Unit {
+  int seq, kvh, tile, k0, k1;  // keys k0 .. k1 - 1, k0 a multiple of 64
+  int64_t slot;                // partial-result slot, -1: the tile is this unit's alone
+  Seq q;
+};
+template <int M>
+__device__ __forceinline__ bool unit_of(const AttendArgs &a, Unit *u) {
+  int widest;
+  const int C = plan_keys<M>(a, &widest);
+  Place pl;
+  u->kvh = blockIdx.x % a.kv.kv_heads;
+  if (!plan_find<M>(a, C, blockIdx.x / a.kv.kv_heads, false, &pl)) return false;
+  const int per = units_of(span_of<M>(a, pl.q), C);
+  // the tiles with the most keys first
+  const int order = pl.index / per, split = pl.index % per;
+  u->seq = pl.seq;
+  u->q = pl.q;
+  u->tile = tiles_of<M>(a, pl.q) - 1 - order;
+  const Range r = range_of<M>(a, pl.q, u->tile);
+  const int real = units_of(r.hi - r.lo, C);  // the tile's units that have keys
+  if (split >= real) return false;
+  u->k0 = r.lo + split * C;
+  u->k1 = min(r.hi, u->k0 + C);
+  u->slot = real > 1 ? pl.slot + pl.index : -1;
+  if (u->slot >= a.max_slots) return false;  // starts out of order can ask for more than there are
+  return true;
+}
+
+// Rows of a sequence that cannot be served become NaN.
+template <class E, int D, int M>
+__device__ __forceinline__ void refuse(const AttendArgs &a, const Unit &u) {
+  const int rows = min(M, u.q.count * a.kv.group - u.tile * M);
+  const float nan = __builtin_nanf("");
+  for (int i = threadIdx.x; i < rows * (D / 4); i += kThreads)
+    store_out<E, D>(a, u.q, u.kvh, u.tile * M + i / (D / 4), i % (D / 4) * 4, f32x4{nan, nan, nan, nan});
+  if (threadIdx.x == 0 && a.kv.status) atomicOr(a.kv.status, kKvBadLength);
+}
+
+__device__ __forceinline__ float finish(float l) { return l == 0.f ? 0.f : 1.f / l; }
+
+// ---------------------------------------------------------------------------------------------
+// Few rows per sequence: decode and verification windows.  Bound by the bytes of the cache.  The
+// four waves of a block take the unit's 32-key steps in turn, each with all 32 rows, straight
+// from memory into the operand registers (every byte is used by one wave only, so LDS would only
+// add a copy); a step's keys are requested while the step before is multiplied.
+// ---------------------------------------------------------------------------------------------
+template <class E, int D>
+__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_few_kernel(AttendArgs a) {
+  constexpr int M = kFewRows;
+  __shared__ __align__(16) float sums[kWaves][D / 32 * 4][kLanes][4];
+  __shared__ float stat[kWaves][M][2];
+  __shared__ int ids[kIds];
+  __shared__ int bad;
+  Unit u;
+  if (!unit_of<M>(a, &u)) return;
+  if (u.q.bad) {
+    refuse<E, D, M>(a, u);
+    return;
+  }
+  const KvView &kv = a.kv;
+  const int lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes, half = lane / 32, n = lane % 32;
+  if (threadIdx.x == 0) bad = 0;
+  const int rows = u.q.count * kv.group, row = u.tile * M + n, before = u.q.length - u.q.count;
+  const int pos = row < rows ? before + row / kv.group : -1;
+  const int floor = a.window ? pos - a.window : -1;
+  const int first = before + u.tile * M / kv.group, last = before + (min(u.tile * M + M, rows) - 1) / kv.group;
+  u32x4 q[D / 16];
+  load_q<D>(a, u.q, u.kvh, row, q);
+
+  Rows<D> st;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) st.acc[i] = f32x16{};
+  st.m = kNegInf;
+  st.l = 0.f;
+
+  const int shift = kv.page_shift, P = 1 << shift;
+  const int key = (lane & 19) | (lane & 4) << 1 | (lane & 8) >> 1;  // pi(lane): bits 2 and 3 swapped
+  const int64_t head_elems = (int64_t)D << shift, page_elems = head_elems * kv.kv_heads;
+  const uint16_t *keys = kv.keys + u.kvh * head_elems, *values = kv.values + u.kvh * head_elems;
+  const int pg_last = (u.k1 - 1) >> shift;
+
+  for (int pg0 = u.k0 >> shift; pg0 <= pg_last; pg0 += kIds) {
+    __syncthreads();  // the ids of the round before have been read
+    load_ids(kv, u.seq, pg0, pg_last, ids, &bad);
+    const int begin = max(u.k0, pg0 << shift);
+    const int end = (int)min((int64_t)u.k1, ((int64_t)pg0 + kIds) << shift);
+    const int id_last = min(pg_last, pg0 + kIds - 1) - pg0;
+    u32x4 k[D / 16], v[2][D / 32];
+    auto load_k = [&](int t0) {
+      const int t = t0 + key;
+      const int id = ids[min((t >> shift) - pg0, id_last)];
+      const uint16_t *src = keys + id * page_elems + (t & (P - 1) & ~15) * D + (16 * half + t % 16) * 8;
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) k[c] = *(const u32x4 *)(src + 2 * c * 16 * 8);
+    };
+    auto load_v = [&](int t0) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const int t = t0 + 16 * c;
+        const int id = ids[min((t >> shift) - pg0, id_last)];
+        const uint16_t *src = values + id * page_elems + (t & (P - 1)) * D + (half * D + n) * 8;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) v[c][i] = *(const u32x4 *)(src + 32 * i * 8);
+      }
+    };
+    int t0 = begin + 32 * wave;
+    if (t0 < end) load_k(t0), load_v(t0);
+    for (; t0 < end; t0 += 32 * kWaves) {
+      const int next = t0 + 32 * kWaves;
+      f32x16 s[1] = {};
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) s[0] = mma(k[c], q[c], s[0], E());
+      if (next < end) load_k(next);
+      // whether some row does not see some key of the step
+      const bool edge = t0 + 31 > first || (a.window && t0 <= last - a.window);
+      if (edge) mask_scores<1>(s, t0, pos, floor);
+      u32x4 p[2];
+      softmax_step<E, D, 1>(s, st, p, a.scale_log2);
+      if (edge) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) clean_values<E, D>(v[c], st, t0 + 16 * c, u.q.length, pos, floor);
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) st.acc[i] = mma(v[c][i], p[c], st.acc[i], E());
+      if (next < end) load_v(next);
+    }
+  }
+
+  // join the four waves
+  st.l += __shfl_xor(st.l, 32);
+  if (half == 0) stat[wave][n][0] = st.m, stat[wave][n][1] = st.l;
+  __syncthreads();
+  float top = kNegInf;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, stat[w][n][0]);
+  const float base = top == kNegInf ? 0.f : top, mine = __builtin_amdgcn_exp2f(st.m - base);
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *(f32x4 *)sums[wave][4 * i + g][lane] = f32x4{st.acc[i][4 * g] * mine, st.acc[i][4 * g + 1] * mine,
+                                                    st.acc[i][4 * g + 2] * mine, st.acc[i][4 * g + 3] * mine};
+  float l = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) l += stat[w][n][1] * __builtin_amdgcn_exp2f(stat[w][n][0] - base);
+  __syncthreads();
+  if (bad) l = __builtin_nanf("");
+  if (row >= rows) return;
+  if (u.slot >= 0 && threadIdx.x < 32) {
+    float *ml = part_ml<D, M>(a, u.slot, u.kvh, n);
+    ml[0] = top, ml[1] = l;
+  }
+  const float inv = finish(l);
+#pragma unroll
+  for (int i = wave; i < D / 8; i += kWaves) {
+    f32x4 o{};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) o += *(const f32x4 *)sums[w][i][lane];
+    const int d = 32 * (i / 4) + 8 * (i % 4) + 4 * half;
+    if (u.slot >= 0)
+      *(f32x4 *)(part_o<D, M>(a, u.slot, u.kvh, n) + d) = o;
+    else
+      store_out<E, D>(a, u.q, u.kvh, row, d, o * inv);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Many rows per sequence: prompts and their chunks.  Bound by the matrix cores and the softmax's
+// vector work.  The four waves of a block take 32 rows each and share the keys: tiles of 64 keys
+// and values go from memory into LDS by direct loads, the next tile while this one is multiplied.
+// ---------------------------------------------------------------------------------------------
+typedef __attribute__((address_space(3))) void lds_void;
+typedef const __attribute__((address_space(1))) void global_void;
+
+template <class E, int D>
+__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_many_kernel(AttendArgs a) {
+  constexpr int M = kManyRows, KT = 64;
+  constexpr int kTileBytes = KT * D * 2;
+  __shared__ __align__(16) uint8_t lds[4 * kTileBytes];  // [2][K tile, V tile], each four groups
+  __shared__ int ids[kIds];
+  __shared__ int bad;
+  Unit u;
+  if (!unit_of<M>(a, &u)) return;
+  if (u.q.bad) {
+    refuse<E, D, M>(a, u);
+    return;
+  }
+  const KvView &kv = a.kv;
+  const int lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes, half = lane / 32, n = lane % 32;
+  if (threadIdx.x == 0) bad = 0;
+  const int rows = u.q.count * kv.group, wrow = u.tile * M + 32 * wave, row = wrow + n;
+  const int before = u.q.length - u.q.count;
+  const int pos = row < rows ? before + row / kv.group : -1;
+  const int floor = a.window ? pos - a.window : -1;
+  // positions of this wave's first and last row (none: last below every key)
+  const int first = before + wrow / kv.group;
+  const int last = wrow < rows ? before + (min(wrow + 32, rows) - 1) / kv.group : -1;
+  u32x4 q[D / 16];
+  load_q<D>(a, u.q, u.kvh, row, q);
+
+  Rows<D> st;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) st.acc[i] = f32x16{};
+  st.m = kNegInf;
+  st.l = 0.f;
+
+  const int shift = kv.page_shift, P = 1 << shift;
+  const int key = (lane & 19) | (lane & 4) << 1 | (lane & 8) >> 1;  // pi(lane): bits 2 and 3 swapped
+  const int64_t head_elems = (int64_t)D << shift, page_elems = head_elems * kv.kv_heads;
+  const uint16_t *keys = kv.keys + u.kvh * head_elems, *values = kv.values + u.kvh * head_elems;
+  const int pg_last = (u.k1 - 1) >> shift;
+
+  for (int pg0 = u.k0 >> shift; pg0 <= pg_last; pg0 += kIds) {
+    __syncthreads();  // ids and tiles of the round before have been read
+    load_ids(kv, u.seq, pg0, pg_last, ids, &bad);
+    const int begin = max(u.k0, pg0 << shift);
+    const int end = (int)min((int64_t)u.k1, ((int64_t)pg0 + kIds) << shift);
+    // tile t0 into buffer b: four groups' keys and values as they lie in memory, one group to
+    // a wave; a group past the end is read from the last one's place
+    auto stage = [&](int t0, int b) {
+      const int t = min(t0 + 16 * wave, (end - 1) & ~15);
+      const int64_t at = ids[(t >> shift) - pg0] * page_elems + (t & (P - 1)) * D + lane * 8;
+      uint8_t *dst = lds + b * 2 * kTileBytes + wave * 16 * D * 2;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) {
+        __builtin_amdgcn_global_load_lds((global_void *)(keys + at + i * 512), (lds_void *)(dst + i * 1024), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((global_void *)(values + at + i * 512),
+                                         (lds_void *)(dst + kTileBytes + i * 1024), 16, 0, 0);
+      }
+    };
+    // this lane's operands within 32 keys' and 16 values' bytes
+    const int koff = key / 16 * 32 * D + (16 * half + key % 16) * 16, voff = (half * D + n) * 16;
+    stage(begin, 0);
+    int b = 0;
+    for (int t0 = begin; t0 < end; t0 += KT, b ^= 1) {
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's part of the tile has landed
+      __builtin_amdgcn_s_barrier();        // everyone's has, and the other buffer is free
+      asm volatile("" ::: "memory");
+      if (t0 + KT < end) stage(t0 + KT, b ^ 1);
+      if (t0 > last || (a.window && t0 + KT - 1 <= first - a.window)) continue;  // none of the wave's rows sees it
+      const uint8_t *kt = lds + b * 2 * kTileBytes, *vt = kt + kTileBytes;
+      f32x16 s[2] = {};
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          s[j] = mma(*(const u32x4 *)(kt + j * 64 * D + c * 512 + koff), q[c], s[j], E());
+      const bool edge = t0 + KT - 1 > first || (a.window && t0 <= last - a.window);
+      if (edge) mask_scores<2>(s, t0, pos, floor);
+      u32x4 p[4];
+      softmax_step<E, D, 2>(s, st, p, a.scale_log2);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        u32x4 v[D / 32];
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) v[i] = *(const u32x4 *)(vt + c * 32 * D + i * 512 + voff);
+        if (edge) clean_values<E, D>(v, st, t0 + 16 * c, u.q.length, pos, floor);
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) st.acc[i] = mma(v[i], p[c], st.acc[i], E());
+      }
+    }
+  }
+
+  if (row >= rows) return;
+  float l = st.l + __shfl_xor(st.l, 32);
+  if (bad) l = __builtin_nanf("");
+  const int trow = 32 * wave + n;
+  if (u.slot >= 0 && half == 0) {
+    float *ml = part_ml<D, M>(a, u.slot, u.kvh, trow);
+    ml[0] = st.m, ml[1] = l;
+  }
+  const float inv = finish(l);
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f32x4 o{st.acc[i][4 * g], st.acc[i][4 * g + 1], st.acc[i][4 * g + 2], st.acc[i][4 * g + 3]};
+      const int d = 32 * i + 8 * g + 4 * half;
+      if (u.slot >= 0)
+        *(f32x4 *)(part_o<D, M>(a, u.slot, u.kvh, trow) + d) = o;
+      else
+        store_out<E, D>(a, u.q, u.kvh, row, d, o * inv);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Joins the units of split tiles: one row (new token, query head) per block and round, the row's
+// units spread over the block's groups of D / 4 lanes.
+// ---------------------------------------------------------------------------------------------
+constexpr int kJoinThreads = 512;
+
+template <class E, int D, int M>
+__global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a) {
+  constexpr int kPer = D / 4, kGroups = kJoinThreads / kPer;
+  __shared__ __align__(16) float sum[kGroups][D];
+  __shared__ float sums_l[kGroups];
+  int widest;
+  const int C = plan_keys<M>(a, &widest);
+  if (widest <= C) return;  // no tile was split
+  const KvView &kv = a.kv;
+  const int g = threadIdx.x / kPer, d = threadIdx.x % kPer * 4, lane = threadIdx.x % kLanes;
+  for (int64_t item = blockIdx.x; item < (int64_t)kv.n_tokens * kv.heads; item += gridDim.x) {
+    const int tok = (int)(item / kv.heads), head = (int)(item % kv.heads), kvh = head / kv.group;
+    // the sequence of this token: the last one starting at or before it
+    int seq = -1;
+    for (int s0 = 0; s0 < kv.n_seqs; s0 += kLanes) {
+      bool in = false;
+      if (s0 + lane < kv.n_seqs) {
+        const Seq q = seq_of(kv, s0 + lane);
+        in = tok >= q.first && tok < q.first + q.count;
+      }
+      const uint64_t any = __ballot(in);
+      if (any) {
+        seq = s0 + __ffsll((unsigned long long)any) - 1;
+        break;
+      }
+    }
+    if (seq < 0) continue;
+    Place pl;
+    if (!plan_find<M>(a, C, seq, true, &pl) || pl.q.bad) continue;
+    const int row = (tok - pl.q.first) * kv.group + head % kv.group, tile = row / M;
+    const Range r = range_of<M>(a, pl.q, tile);
+    const int real = units_of(r.hi - r.lo, C), per = units_of(span_of<M>(a, pl.q), C);
+    if (real <= 1) continue;
+    const int64_t slot = pl.slot + (int64_t)(tiles_of<M>(a, pl.q) - 1 - tile) * per;
+    if (slot + real > a.max_slots) continue;
+    float top = kNegInf;
+    for (int i = lane; i < real; i += kLanes) top = fmaxf(top, part_ml<D, M>(a, slot + i, kvh, row % M)[0]);
+    for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    const float base = top == kNegInf ? 0.f : top;
+    f32x4 o{};
+    float l = 0.f;
+#pragma unroll 4
+    for (int i = g; i < real; i += kGroups) {
+      const float *ml = part_ml<D, M>(a, slot + i, kvh, row % M);
+      const float w = __builtin_amdgcn_exp2f(ml[0] - base);
+      l += w * ml[1];
+      o += w * *(const f32x4 *)(part_o<D, M>(a, slot + i, kvh, row % M) + d);
+    }
+    *(f32x4 *)&sum[g][d] = o;
+    if (d == 0) sums_l[g] = l;
+    __syncthreads();
+    if (g == 0) {
+      o = f32x4{};
+      l = 0.f;
+      for (int i = 0; i < kGroups; ++i) {
+        o += *(const f32x4 *)&sum[i][d];
+        l += sums_l[i];
+      }
+      store_out<E, D>(a, pl.q, kvh, row, d, o * finish(l));
+    }
+    __syncthreads();
+  }
+}
+
+template <class E, int D, int M>
+hipError_t launch_kernels(const AttendArgs &a, hipStream_t s) {
+  void *args[] = {const_cast<AttendArgs *>(&a)};
+  const dim3 grid((unsigned)((int64_t)a.max_units * a.kv.kv_heads));
+  const void *fn = M == kFewRows ? (const void *)attend_few_kernel<E, D> : (const void *)attend_many_kernel<E, D>;
+  hipError_t e = hipLaunchKernel(fn, grid, dim3(kThreads), args, 0, s);
+  if (e != hipSuccess) return e;
+  const int64_t rows = (int64_t)a.kv.n_tokens * a.kv.heads;
+  return hipLaunchKernel((const void *)attend_join_kernel<E, D, M>, dim3((unsigned)(rows < 2048 ? rows : 2048)),
+                         dim3(kJoinThreads), args, 0, s);
+}
+
+}  // namespace
+
+template <int D>
+hipError_t launch_attend(const AttendArgs &a, bool half, bool many, hipStream_t s) {
+  if (half)
+    return many ? launch_kernels<_Float16, D, kManyRows>(a, s) : launch_kernels<_Float16, D, kFewRows>(a, s);
+  return many ? launch_kernels<__bf16, D, kManyRows>(a, s) : launch_kernels<__bf16, D, kFewRows>(a, s);
+}
+
+}  // namespace moecache

@@ -23,6 +23,8 @@ COPY_MODES = {"kernel": 0, "split": MOE_F_SPLIT_COPY, "side": MOE_F_SIDE_COPY, "
 KIND_ROUTER, KIND_GATEUP, KIND_DOWN, KIND_COPY = 0, 1, 2, 3
 KIND_NAMES = {KIND_ROUTER: "router", KIND_GATEUP: "gateup", KIND_DOWN: "down", KIND_COPY: "copy"}
 MOE_Q4_K, MOE_Q6_K = 12, 14
+MOE_F32, MOE_F16, MOE_BF16 = 0, 1, 30
+MOE_KV_BAD_PAGE, MOE_KV_BAD_LENGTH = 1, 2
 # model type: the gate/up format's code, the down format's in the next byte when it differs
 QTYPES = {"q8_0": MOE_Q8_0, "q4_0": MOE_Q4_0, "q4_k": MOE_Q4_K, "q6_k": MOE_Q6_K,
           "q4_k_m": MOE_Q4_K | (MOE_Q6_K << 8)}
@@ -79,6 +81,30 @@ class PlanOut(ctypes.Structure):
 
     def as_dict(self):
         return {f: getattr(self, f) for f, _ in self._fields_ if f != "pad"}
+
+
+class KvBatch(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("n_heads", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page_tokens", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("n_seqs", ctypes.c_int32),
+                ("n_tokens", ctypes.c_int32), ("pad", ctypes.c_int32),
+                ("keys", ctypes.c_void_p), ("values", ctypes.c_void_p),
+                ("pages", ctypes.c_void_p), ("starts", ctypes.c_void_p),
+                ("lengths", ctypes.c_void_p), ("status", ctypes.c_void_p),
+                ("hip_stream", ctypes.c_void_p)]
+
+
+class KvRope(ctypes.Structure):
+    _fields_ = [("dim", ctypes.c_int32), ("adjacent", ctypes.c_int32), ("freq", ctypes.c_void_p)]
+
+
+class SampleBatch(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("n_rows", ctypes.c_int32), ("vocab", ctypes.c_int32),
+                ("pad", ctypes.c_int32), ("logits", ctypes.c_void_p), ("row_stride", ctypes.c_int64),
+                ("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p),
+                ("top_p", ctypes.c_void_p), ("min_p", ctypes.c_void_p), ("u", ctypes.c_void_p),
+                ("hip_stream", ctypes.c_void_p)]
 
 
 class PackInfo(ctypes.Structure):
@@ -145,6 +171,10 @@ def lib():
         "moe_plan_percent": ([P(PlanIn), ctypes.c_double, i64, P(PlanOut)], ctypes.c_int),
         "moe_plan_bytes": ([P(PlanIn), u64, i64, P(PlanOut)], ctypes.c_int),
         "moe_policy_min": ([P(i32), P(i64), i64, i32, i32, P(u64)], ctypes.c_int),
+        "moe_kv_append": ([P(KvBatch), P(KvRope), i32, vp, i64, vp, i64, vp, i64, vp, i64], ctypes.c_int),
+        "moe_kv_attend": ([P(KvBatch), i32, ctypes.c_float, vp, i64, vp, i64, vp, u64], ctypes.c_int),
+        "moe_kv_attend_workspace": ([P(KvBatch), P(u64)], ctypes.c_int),
+        "moe_sample": ([P(SampleBatch), vp, vp], ctypes.c_int),
         "moe_pack_gguf": ([ctypes.c_char_p] * 4 + [P(PackInfo)], ctypes.c_int),
     }
     for name, (args, res) in sig.items():

@@ -1,0 +1,409 @@
+"""GPU tests of the paged cache: appending rotated keys and values, and attention over it,
+against the fp64 oracle."""
+import numpy as np
+import pytest
+
+from gpu_common import log, torch_cuda
+from oracle import serving as ref
+from serving_common import Batch, half_step
+
+pytestmark = pytest.mark.gpu
+
+EDGES = [(1, n - 1) for n in (1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 129, 257, 1000)]
+
+
+def types():
+    torch = torch_cuda()
+    return {"bf16": torch.bfloat16, "f16": torch.float16}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("group,page", [(1, 16), (3, 64), (8, 32), (40, 1024)])
+def test_one_new_token(dtype, dim, group, page):
+    torch = torch_cuda()
+    log(f"one new token {dtype} dim {dim} group {group} page {page}")
+    b = Batch(torch, EDGES, 2 * group, 2, dim, page, types()[dtype], seed=dim + group)
+    worst = b.check(b.cache().attend(b.q_gpu(), b.pages, b.starts, b.lengths))
+    log(f"  worst error / tolerance {worst:.3f}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("group,page,window", [(1, 16, 0), (4, 64, 0), (5, 32, 50), (2, 128, 1), (8, 16, 200),
+                                               (4, 256, 64)])
+def test_chunks(dtype, dim, group, page, window):
+    torch = torch_cuda()
+    log(f"chunks {dtype} dim {dim} group {group} page {page} window {window}")
+    seqs = [(70, 0), (1, 300), (33, 31), (64, 64), (0, 100), (129, 190), (5, 640)]
+    b = Batch(torch, seqs, group, 1, dim, page, types()[dtype], seed=dim + window)
+    worst = b.check(b.cache(window=window).attend(b.q_gpu(), b.pages, b.starts, b.lengths), window)
+    log(f"  worst error / tolerance {worst:.3f}")
+
+
+@pytest.mark.parametrize("window", [0, 1, 33, 100])
+@pytest.mark.parametrize("new", [2, 5, 8])
+def test_verification_windows(new, window):
+    torch = torch_cuda()
+    seqs = [(new, p) for p in (0, 1, 30, 31, 64, 250, 700)]
+    b = Batch(torch, seqs, 16, 2, 128, 16, torch.bfloat16, seed=new)
+    b.check(b.cache(window=window, scale=0.2).attend(b.q_gpu(), b.pages, b.starts, b.lengths), window, scale=0.2)
+
+
+@pytest.mark.parametrize("seqs", [[(1, 20000)], [(1, 9000), (1, 3)] * 3, [(40, 6000)], [(1, 50)] * 300,
+                                  [(1, 7), (300, 2000), (1, 3000)] + [(1, 100)] * 70])
+def test_split_and_ragged_batches(seqs):
+    torch = torch_cuda()
+    log(f"split: {seqs[:3]} x {len(seqs)}")
+    b = Batch(torch, seqs, 8, 2, 64, 32, torch.float16, seed=len(seqs))
+    out = b.cache().attend(b.q_gpu(), b.pages, b.starts, b.lengths)
+    b.check(out)
+    again = b.cache().attend(b.q_gpu(), b.pages, b.starts, b.lengths)
+    assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("seqs,new,before", [(1100, 1, 19999), (300, 70, 17000)])
+def test_small_pages_past_one_list_of_ids(seqs, new, before):
+    """Units of more than 1024 pages: so many sequences (over the same pages) that none is split."""
+    torch = torch_cuda()
+    log(f"{seqs} sequences of {new} new tokens over the same {before}")
+    b = Batch(torch, [(new, before)], 2, 1, 64, 16, torch.bfloat16, seed=4)
+    rng = np.random.default_rng(6)
+    q = torch.from_numpy(rng.standard_normal((seqs * new, 2, 64))).to(b.dtype)
+    pages = b.pages.expand(seqs, -1).contiguous()
+    starts = torch.arange(0, seqs * new + 1, new, dtype=torch.int32, device="cuda")
+    lengths = b.lengths.expand(seqs).contiguous()
+    out = b.cache().attend(q.cuda(), pages, starts, lengths)
+    for s in (0, 1, seqs // 2, seqs - 1):
+        b.q = q[s * new:(s + 1) * new].double().numpy()
+        b.check(out[s * new:(s + 1) * new])
+
+
+def test_pages_past_32_bit_offsets():
+    torch = torch_cuda()
+    page_elems = 8 * 1024 * 128
+    first = 2 ** 32 // page_elems + 5  # element offsets past 2^32
+    b = Batch(torch, [(1, 1500), (80, 1000)], 8, 8, 128, 1024, torch.bfloat16, first_page=first)
+    cache = b.cache(rope_dim=0)
+    b.check(cache.attend(b.q_gpu(), b.pages, b.starts, b.lengths))
+    k = torch.from_numpy(np.concatenate([x[-n:] for x, n in zip(b.k, b.new)])).to(b.dtype).cuda()
+    b.keys[:, first:] = 0
+    b.values[:, first:] = 0
+    cache.append(k, k, b.pages, b.starts, b.lengths)
+    page, place = b.table[1, 1079 // 1024], 1079 % 1024
+    got = b.keys[0, int(page), :, place // 16, :, place % 16].reshape(8, 128)
+    assert torch.equal(got, k[-1])
+
+
+def test_rows_behind_the_last_sequence_stay():
+    torch = torch_cuda()
+    for seqs in ([(1, 40), (3, 9)], [(100, 3)]):
+        b = Batch(torch, seqs, 4, 2, 64, 16, torch.bfloat16, pad_rows=37)
+        out = torch.full((b.n, 4, 64), 7.0, dtype=b.dtype, device="cuda")
+        cache = b.cache()
+        assert cache.attend(b.q_gpu(), b.pages, b.starts, b.lengths, out=out) is out
+        b.check(out)
+        assert (out[sum(b.new):] == 7).all()
+        keys = b.keys.clone()
+        k = torch.ones(b.n, 2, 64, dtype=b.dtype, device="cuda")
+        q_out = torch.full((b.n, 4, 64), 7.0, dtype=b.dtype, device="cuda")
+        cache.append(k, k, b.pages, b.starts, b.lengths, q=b.q_gpu(), q_out=q_out)
+        assert (q_out[sum(b.new):] == 7).all() and not (q_out[:sum(b.new)] == 7).all()
+        changed = (b.keys.view(torch.int16) != keys.view(torch.int16)).flatten(4).any(-1).sum()
+        assert int(changed) <= 2 * sum(-(-n // 16) + 1 for n in b.new)
+
+
+def test_nothing_to_do():
+    torch = torch_cuda()
+    b = Batch(torch, [(0, 5), (0, 0)], 4, 2, 64, 16, torch.bfloat16, pad_rows=3)
+    cache = b.cache()
+    out = torch.full((3, 4, 64), 7.0, dtype=b.dtype, device="cuda")
+    cache.attend(b.q_gpu(), b.pages, b.starts, b.lengths, out=out)
+    assert (out == 7).all()
+    none = torch.empty(0, 4, 64, dtype=b.dtype, device="cuda")
+    kv = torch.empty(0, 2, 64, dtype=b.dtype, device="cuda")
+    assert cache.attend(none, b.pages, b.starts, b.lengths).shape == (0, 4, 64)
+    assert cache.append(kv, kv, b.pages, b.starts, b.lengths, q=none).shape == (0, 4, 64)
+    zero = torch.zeros(1, dtype=torch.int32, device="cuda")
+    assert cache.attend(b.q_gpu(), b.pages[:0], zero, zero[:0], out=out) is out and (out == 7).all()
+
+
+@pytest.mark.parametrize("seqs,row", [([(5, 60)], 2), ([(120, 40)], 50), ([(120, 700)], 119)])
+@pytest.mark.parametrize("value", ["nan", "inf", "-inf", "both"])
+def test_what_a_row_does_not_see_has_no_effect(seqs, row, value):
+    """Token `row` of the new ones holds values that are not finite, in some elements: rows
+    before it do not see them, rows from it on get just those elements."""
+    torch = torch_cuda()
+    b = Batch(torch, seqs, 4, 2, 64, 16, torch.bfloat16, seed=row)
+    cache = b.cache()
+    q = b.q_gpu()
+    clean = cache.attend(q, b.pages, b.starts, b.lengths)
+    t = seqs[0][1] + row
+    page, place = int(b.table[0, t // 16]), t % 16
+    bad = {"nan": [float("nan")], "inf": [float("inf")], "-inf": [float("-inf")],
+           "both": [float("inf"), float("-inf")]}[value]
+    elements = (3, 40)
+    for j, x in enumerate(bad):  # both: +inf in this token, -inf in the one before
+        tt = t - j
+        pg, pl = int(b.table[0, tt // 16]), tt % 16
+        for d in elements:
+            b.values[0, pg, 1, 0, pl // 8, d, pl % 8] = x
+    out = cache.attend(q, b.pages, b.starts, b.lengths)
+    before = row - (len(bad) - 1)
+    assert torch.equal(out[:before], clean[:before])
+    assert torch.equal(out[:, :2], clean[:, :2])  # heads of the other KV head
+    want = {"nan": torch.isnan, "inf": torch.isposinf, "-inf": torch.isneginf, "both": torch.isnan}[value]
+    for d in range(64):
+        got = out[row:, 2:, d]
+        assert want(got).all() if d in elements else torch.equal(got, clean[row:, 2:, d])
+    # a key that is not finite: rows before it are unchanged, rows from it on are NaN
+    b.fill(0)
+    b.keys[0, page, 0, 0, 2, place, 1] = float("nan")
+    out = cache.attend(q, b.pages, b.starts, b.lengths)
+    assert torch.equal(out[:row], clean[:row]) and torch.isnan(out[row:, :2]).all()
+    assert torch.equal(out[:, 2:], clean[:, 2:])
+
+
+@pytest.mark.parametrize("new", [1, 90])
+def test_a_bad_length_is_refused_alone(new):
+    torch = torch_cuda()
+    for length in (-1, new - 1, 10 ** 6, -2 ** 31, 2 ** 31 - 1):
+        b = Batch(torch, [(new, 30), (new, 20), (2, 50)], 4, 2, 64, 16, torch.bfloat16)
+        b.lengths[1] = length
+        cache, status = b.cache(), torch.zeros(1, dtype=torch.int32, device="cuda")
+        out = cache.attend(b.q_gpu(), b.pages, b.starts, b.lengths, status=status)
+        assert torch.isnan(out[b.rows(1)]).all() and status.item() == 2
+        b.check(out, skip=(1,))
+        keys, status = b.keys.clone(), torch.zeros(1, dtype=torch.int32, device="cuda")
+        k = torch.ones(b.n, 2, 64, dtype=b.dtype, device="cuda")
+        q = cache.append(k, k, b.pages, b.starts, b.lengths, q=b.q_gpu(), status=status)
+        assert torch.isnan(q[b.rows(1)]).all() and status.item() == 2
+        assert not torch.isnan(q[b.rows(0)]).any() and not torch.isnan(q[b.rows(2)]).any()
+        own = torch.from_numpy(b.table[1, :-(-b.total[1] // 16)]).long().cuda()
+        assert torch.equal(b.keys[0, own].view(torch.int16), keys[0, own].view(torch.int16))
+
+
+@pytest.mark.parametrize("new", [1, 90])
+@pytest.mark.parametrize("page_id", [-1, -2 ** 31, 10 ** 9, 11])
+def test_a_bad_page_is_refused_alone(new, page_id):
+    torch = torch_cuda()
+    b = Batch(torch, [(new, 30), (new, 3000), (2, 50)], 4, 2, 64, 16, torch.bfloat16)
+    page_id = b.n_pages if page_id == 11 else page_id
+    b.pages[1, 3] = page_id
+    cache, status = b.cache(), torch.zeros(1, dtype=torch.int32, device="cuda")
+    out = cache.attend(b.q_gpu(), b.pages, b.starts, b.lengths, status=status)
+    assert torch.isnan(out[b.rows(1)]).all() and status.item() == 1
+    b.check(out, skip=(1,))
+    b.pages[0, (30 + new - 1) // 16] = page_id  # the page of sequence 0's last new token
+    keys, values = b.keys.clone(), b.values.clone()
+    k = torch.ones(b.n, 2, 64, dtype=b.dtype, device="cuda")
+    status.zero_()
+    q = cache.append(k, k, b.pages, b.starts, b.lengths, q=b.q_gpu(), status=status)
+    assert status.item() == 1 and not torch.isnan(q).any()
+    last = int(b.table[0, (30 + new - 1) // 16])
+    assert torch.equal(b.keys[0, last].view(torch.int16), keys[0, last].view(torch.int16))
+    assert torch.equal(b.values[0, last].view(torch.int16), values[0, last].view(torch.int16))
+
+
+def test_starts_out_of_order_stay_in_bounds():
+    """Whatever starts holds: the calls end, and rows outside the tensor's stay untouched."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(9)
+    for trial in range(12):
+        b = Batch(torch, [(3, 40), (60, 9), (1, 500)], 4, 2, 64, 16, torch.bfloat16, seed=trial)
+        wrong = rng.integers(-2 ** 31, 2 ** 31 - 1, 4) if trial % 2 else rng.integers(-5, b.n + 5, 4)
+        b.starts = torch.tensor(wrong, dtype=torch.int32, device="cuda")
+        whole = torch.full((b.n + 64, 4, 64), 7.0, dtype=b.dtype, device="cuda")
+        out = whole[32:32 + b.n]
+        cache = b.cache()
+        cache.attend(b.q_gpu(), b.pages, b.starts, b.lengths, out=out)
+        k = torch.ones(b.n, 2, 64, dtype=b.dtype, device="cuda")
+        cache.append(k, k, b.pages, b.starts, b.lengths, q=b.q_gpu(), q_out=out)
+        torch.cuda.synchronize()
+        assert (whole[:32] == 7).all() and (whole[32 + b.n:] == 7).all()
+
+
+def test_strided_rows():
+    """q, k and v as slices of one projection's output; out inside a wider row."""
+    torch = torch_cuda()
+    for seqs in ([(1, 77), (1, 5)], [(90, 20)]):
+        b = Batch(torch, seqs, 4, 2, 128, 64, torch.bfloat16)
+        flat = torch.zeros(b.n, (4 + 2 + 2) * 128, dtype=b.dtype, device="cuda")
+        flat[:, :512] = b.q_gpu().flatten(1)
+        flat[:, 512:768] = torch.from_numpy(np.concatenate([x[-n:] for x, n in zip(b.k, b.new)])).cuda().flatten(1)
+        flat[:, 768:] = torch.from_numpy(np.concatenate([x[-n:] for x, n in zip(b.v, b.new)])).cuda().flatten(1)
+        q, k, v = flat[:, :512].view(b.n, 4, 128), flat[:, 512:768].view(b.n, 2, 128), flat[:, 768:].view(b.n, 2, 128)
+        keys, values = b.keys.clone(), b.values.clone()
+        cache = b.cache(rope_dim=0)
+        got = cache.append(k, v, b.pages, b.starts, b.lengths, q=q)
+        assert torch.equal(got, q)
+        assert torch.equal(b.keys.view(torch.int16), keys.view(torch.int16))  # what was there already
+        assert torch.equal(b.values.view(torch.int16), values.view(torch.int16))
+        wide = torch.full((b.n, 6, 128), 7.0, dtype=b.dtype, device="cuda")
+        cache.attend(q, b.pages, b.starts, b.lengths, out=wide[:, 1:5])
+        b.check(wide[:, 1:5])
+        assert (wide[:, 0] == 7).all() and (wide[:, 5] == 7).all()
+
+
+@pytest.mark.parametrize("dtype,source", [("bf16", "bf16"), ("bf16", "f32"), ("f16", "f16"), ("f16", "f32")])
+@pytest.mark.parametrize("dim,rope_dim,adjacent,page", [(64, 64, False, 16), (128, 128, False, 64),
+                                                        (128, 64, True, 32), (256, 256, True, 16),
+                                                        (64, 16, False, 1024), (256, 0, False, 128)])
+def test_append(dtype, source, dim, rope_dim, adjacent, page):
+    """Each element: h |y| of its rounding, and three fp32 operations on sines and cosines off by at
+    most 2^-22 (a turn's part to 2^-26, times 2 pi, and the functions' own error): 2^-20 (|a| + |b|)."""
+    torch = torch_cuda()
+    log(f"append {dtype} from {source} dim {dim} rope {rope_dim} adjacent {adjacent} page {page}")
+    t, s = types()[dtype], torch.float32 if source == "f32" else types()[source]
+    seqs = [(1, 0), (1, 6), (9, 7), (0, 30), (40, 129), (16, 16), (3, 5000)]
+    b = Batch(torch, seqs, 6, 2, dim, page, t, seed=dim, filled=False, pad_rows=2)
+    rng = np.random.default_rng(5)
+    x = {n: torch.from_numpy(rng.standard_normal((b.n, h, dim))).to(s) for n, h in (("q", 6), ("k", 2), ("v", 2))}
+    x["k"][0] = 0.0
+    cache = b.cache(rope_dim=rope_dim, rope_adjacent=adjacent, rope_theta=5e5)
+    q_in = x["q"].cuda()
+    got_q = cache.append(x["k"].cuda(), x["v"].cuda(), b.pages, b.starts, b.lengths, q=q_in).double().cpu().numpy()
+    keys, values = b.keys[0].double().cpu().numpy(), b.values[0].double().cpu().numpy()
+    freqs = [5e5 ** (-2 * i / rope_dim) for i in range(rope_dim // 2)]
+    h, tiny = half_step(t), float(torch.finfo(t).smallest_normal) * torch.finfo(t).eps
+    d = np.arange(dim)
+    touched = 0
+    for i, (n, before) in enumerate(seqs):
+        r, pos = b.rows(i), b.positions(i)
+        for name in ("q", "k"):
+            a = x[name][r].double().numpy()
+            want = ref.rotate(a, pos, freqs, adjacent)
+            big = np.abs(a).max(initial=0.0) * 2
+            if name == "q":
+                got = got_q[r]
+            else:
+                got = np.empty_like(want)
+                for j, p in enumerate(pos):
+                    pg = b.table[i, p // page]
+                    got[j] = keys[pg][(slice(None),) + ref.key_place(p % page, d)]
+            err = np.abs(got - want)
+            assert (err <= h * np.abs(want) + 2.0 ** -20 * big + tiny).all(), (name, i, err.max())
+        for j, p in enumerate(pos):
+            pg = b.table[i, p // page]
+            got = values[pg][(slice(None),) + ref.value_place(p % page, d)]
+            np.testing.assert_array_equal(got, x["v"][r][j].to(t).double().numpy())
+        touched += n
+    # nothing else was written
+    assert np.isfinite(keys).sum() == np.isfinite(values).sum() == touched * 2 * dim
+
+
+def test_append_far_positions_and_own_frequencies():
+    """Positions near 2^20: the angle in 64 bits.  Every page-table entry names the same page."""
+    torch = torch_cuda()
+    n, page = 1 << 20, 1024
+    freqs = [1.0, 0.7, 0.013, 3e-7, 2.5, 1e-4, 0.5, 0.25]
+    from paper_2607_09686_amd import KvCache
+    cache = KvCache(3, 2, 1, 64, page, 2, dtype=torch.float16, rope_dim=16, rope_freqs=freqs)
+    cache.keys.fill_(9.0)
+    cache.values.fill_(9.0)
+    pages = torch.ones(1, n // page, dtype=torch.int32, device="cuda")
+    starts = torch.tensor([0, 3], dtype=torch.int32, device="cuda")
+    lengths = torch.tensor([n], dtype=torch.int32, device="cuda")
+    x = torch.randn(3, 2, 64, generator=torch.Generator().manual_seed(1))
+    q = cache.append(x[:, :1].cuda(), x[:, 1:].cuda(), pages, starts, lengths, layer=1, q=x.cuda())
+    want = ref.rotate(x.double().numpy(), np.arange(n - 3, n), freqs)
+    err = np.abs(q.double().cpu().numpy() - want)
+    assert (err <= 2.0 ** -11 * np.abs(want) + 2.0 ** -20 * 2 * x.abs().max().item() + 2.0 ** -24).all()
+    assert (cache.keys[[0, 2]] == 9).all() and (cache.values[[0, 2]] == 9).all()
+    assert (cache.keys[1, 0] == 9).all() and not (cache.keys[1, 1] == 9).all()
+    assert torch.equal(cache.values[1, 1, 0, 63, 1, :, 5:].T, x[:, 1].half().cuda())
+
+
+def test_q_out_may_be_q():
+    torch = torch_cuda()
+    b = Batch(torch, [(20, 3), (1, 9)], 4, 2, 128, 16, torch.bfloat16)
+    k = torch.randn(b.n, 2, 128, device="cuda").to(b.dtype)
+    q = b.q_gpu()
+    want = b.cache().append(k, k, b.pages, b.starts, b.lengths, q=q)
+    assert b.cache().append(k, k, b.pages, b.starts, b.lengths, q=q, q_out=q) is q
+    assert torch.equal(q, want)
+    assert b.cache().append(k, k, b.pages, b.starts, b.lengths) is None
+
+
+def test_shared_pages():
+    """Two sequences with the same first pages (a shared prompt)."""
+    torch = torch_cuda()
+    b = Batch(torch, [(1, 127), (1, 140)], 8, 2, 128, 64, torch.bfloat16)
+    b.pages[1, 0] = b.pages[0, 0]
+    b.k[1][:64], b.v[1][:64] = b.k[0][:64], b.v[0][:64]
+    b.check(b.cache().attend(b.q_gpu(), b.pages, b.starts, b.lengths))
+
+
+def test_streams_and_replayed_graphs():
+    """Two captured graphs, each replayed several times on new contents among eager calls."""
+    torch = torch_cuda()
+    side = torch.cuda.Stream()
+    graphs = []
+    for seed, seqs in ((1, [(1, 300), (1, 7000), (1, 40)]), (2, [(3, 90), (80, 200)])):
+        b = Batch(torch, seqs, 8, 2, 128, 32, torch.bfloat16, seed=seed, width=240, spare=20)
+        cache = b.cache(rope_dim=0)
+        q = b.q_gpu()
+        new_k = torch.from_numpy(np.concatenate([x[-n:] for x, n in zip(b.k, b.new)])).to(b.dtype).cuda()
+        new_v = torch.from_numpy(np.concatenate([x[-n:] for x, n in zip(b.v, b.new)])).to(b.dtype).cuda()
+
+        def step(b=b, cache=cache, q=q, k=new_k, v=new_v):
+            turned = cache.append(k, v, b.pages, b.starts, b.lengths, q=q)
+            return cache.attend(turned, b.pages, b.starts, b.lengths)
+
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            eager = step()
+        torch.cuda.current_stream().wait_stream(side)
+        b.check(eager)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = step()
+        graphs.append((b, g, out, q, step))
+    for r in range(4):
+        for b, g, out, q, step in graphs:
+            q.copy_(q.roll(1, 0))
+            if r == 2:  # another length at replay: the sequence loses its last tokens
+                b.lengths -= 1
+            want = step()
+            out.fill_(0)
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, want), (r, b.seqs)
+
+
+def test_refusals():
+    torch = torch_cuda()
+    from paper_2607_09686_amd import MoeError
+    b = Batch(torch, [(4, 9)], 4, 2, 64, 16, torch.bfloat16)
+    cache, q = b.cache(), b.q_gpu()
+    k = torch.zeros(4, 2, 64, dtype=b.dtype, device="cuda")
+    index = (b.pages, b.starts, b.lengths)
+    with pytest.raises(TypeError):
+        cache.attend(q.float(), *index)
+    with pytest.raises(ValueError):
+        cache.attend(q[:, :2], *index)
+    with pytest.raises(ValueError):
+        cache.attend(q.transpose(1, 2).contiguous().transpose(1, 2), *index)
+    with pytest.raises(ValueError):
+        cache.attend(q, b.pages, b.starts[:1], b.lengths)
+    with pytest.raises(TypeError):
+        cache.attend(q, b.pages.long(), b.starts, b.lengths)
+    with pytest.raises(ValueError):
+        cache.attend(q, b.pages.cpu(), b.starts, b.lengths)
+    with pytest.raises(ValueError):
+        cache.attend(q, *index, layer=1)
+    with pytest.raises(ValueError):
+        cache.append(k[:3], k, *index)
+    with pytest.raises(TypeError):
+        cache.append(k.half(), k.half(), *index)
+    with pytest.raises(TypeError):
+        cache.append(k, k.float(), *index)
+    with pytest.raises(ValueError):
+        cache.append(k, k, *index, q_out=q)
+    odd = torch.zeros(4 * 4 * 64 + 1, dtype=b.dtype, device="cuda")[1:].view(4, 4, 64)
+    with pytest.raises(MoeError):  # not on 16 bytes
+        cache.attend(odd, *index)
+    with pytest.raises(MoeError):
+        b.cache(window=-1).attend(q, *index)
+    with pytest.raises(MoeError):
+        b.cache(scale=0.0).attend(q, *index)
