@@ -406,7 +406,7 @@ int moe_kv_attend_workspace(const moe_kv_batch *b, uint64_t *bytes);
  * the rows are split over the device. */
 typedef struct {
   int32_t dtype;            /* of the logits: MOE_F32, MOE_BF16 or MOE_F16 */
-  int32_t n_rows;           /* 0..2^20 */
+  int32_t n_rows;           /* 0..65535 */
   int32_t vocab;            /* 1..2^20 */
   int32_t pad;
   const void *logits;       /* device, [n_rows] rows of vocab elements, row_stride elements apart */
@@ -419,8 +419,10 @@ typedef struct {
   void *hip_stream;
 } moe_sample_batch;
 /* token: device [n_rows]; prob: device [n_rows], nullable: the chosen token's
- * share of the mass that the filters left. */
-int moe_sample(const moe_sample_batch *b, int32_t *token, float *prob);
+ * share of the mass that the filters left.  workspace: as moe_kv_attend's, of the
+ * size that moe_sample_workspace gives (n_rows matters alone). */
+int moe_sample(const moe_sample_batch *b, int32_t *token, float *prob, void *workspace, uint64_t workspace_bytes);
+int moe_sample_workspace(const moe_sample_batch *b, uint64_t *bytes);
 
 /* Static budget plan (no HIP dependency, no allocation).  The paper's Native
  * Serving Path section derives the slot count of the routed layers from the

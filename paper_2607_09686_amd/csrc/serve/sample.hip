@@ -20,7 +20,23 @@
 namespace moecache {
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kThreads = 1024, kWaves = kThreads / 64;  // of the draw, a block per row
+constexpr int kSliceThreads = 256;                      // of the passes over slices of a row
+constexpr int kMaxSlices = 64;
+constexpr int kBins = 2048;
+constexpr int kCandidates = 4096;
+
+// Per row in the workspace.
+struct RowWork {
+  uint64_t best[kMaxSlices];     // slices' largest logit: rank key, then the smallest index
+  uint64_t sums[kMaxSlices][3];  // slices' masses, see collect_kernel
+  uint64_t mass[kBins];          // binned, in 2^-31
+  uint32_t count[kBins];
+  uint64_t list[kCandidates];    // codes of the elements that need ranking
+  int32_t n_list;                // how many there are, in the list or not
+  int32_t high, rank_bin;        // last bin of the top-p cut's; bin of the top-k cut (kBins: none)
+  uint32_t before_rank;          // elements in bins before rank_bin
+};
 
 template <class Z>
 __device__ __forceinline__ float logit(const void *row, int i) {
@@ -30,6 +46,40 @@ __device__ __forceinline__ float logit(const void *row, int i) {
 __device__ __forceinline__ uint32_t rank_key(float z) {
   const uint32_t b = __builtin_bit_cast(uint32_t, z);
   return z != z ? 0u : b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+
+__device__ __forceinline__ float unrank(uint32_t key) {
+  return __builtin_bit_cast(float, key & 0x80000000u ? key ^ 0x80000000u : ~key);
+}
+// Elements in falling order, equal logits by rising index, are rising codes.
+__device__ __forceinline__ uint64_t code_of(uint32_t key, int i) { return (uint64_t)~key << 32 | (uint32_t)i; }
+
+// Calls f(logit, index) for lo <= index < hi, a block's threads together: 16-byte loads between
+// the first and the last aligned place.
+template <class Z, int N, class F>
+__device__ __forceinline__ void for_each(const void *row, int lo, int hi, F f) {
+  constexpr int kVec = 16 / sizeof(Z);
+  typedef Z zv __attribute__((ext_vector_type(kVec)));
+  const Z *z = (const Z *)row;
+  const int skip = (int)(-(uintptr_t)(z + lo) / sizeof(Z) % kVec);
+  const int body = min(hi, lo + skip), vecs = (hi - body) / kVec, tail = body + vecs * kVec;
+  if ((int)threadIdx.x < body - lo) f((float)z[lo + threadIdx.x] + 0.f, lo + (int)threadIdx.x);
+#pragma unroll 2
+  for (int v = threadIdx.x; v < vecs; v += N) {
+    const zv e = *(const zv *)(z + body + v * kVec);
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) f((float)e[j] + 0.f, body + v * kVec + j);
+  }
+  if ((int)threadIdx.x < hi - tail) f((float)z[tail + threadIdx.x] + 0.f, tail + (int)threadIdx.x);
+}
+
+__device__ __forceinline__ uint64_t wave_sum(uint64_t v) {
+  for (int o = 32; o; o >>= 1) v += __shfl_xor((unsigned long long)v, o);
+  return v;
+}
+__device__ __forceinline__ uint64_t wave_max(uint64_t v) {
+  for (int o = 32; o; o >>= 1) v = max(v, (uint64_t)__shfl_xor((unsigned long long)v, o));
+  return v;
 }
 
 struct Weigh {
@@ -44,173 +94,483 @@ struct Weigh {
   __device__ __forceinline__ uint64_t parts(double w) const { return (uint64_t)rint(w * unit); }
 };
 
-// Elements kept by rank: key above `key`, or equal to it at an index up to `last`.
-struct Cut {
-  uint32_t key;
-  int last;
-  __device__ __forceinline__ bool keeps(uint32_t k, int i) const { return k > key || (k == key && i <= last); }
+// A row's settings, and its largest logit.
+struct Row {
+  float top, T, p, least;
+  int first, k;
+  bool none, greedy;  // nothing but -inf and NaN; the first largest is the answer
+  __device__ Row(const SampleArgs &a, int row, uint64_t best) {
+    first = (int)~(uint32_t)best;
+    top = unrank((uint32_t)(best >> 32));
+    T = a.temperature ? a.temperature[row] : 1.f;
+    p = a.top_p ? a.top_p[row] : 1.f;
+    k = a.top_k ? a.top_k[row] : 0;
+    if (k <= 0 || k >= a.vocab) k = 0;
+    least = a.min_p ? a.min_p[row] : 0.f;
+    if (least > 1.f) least = 1.f;
+    none = !(top > -__builtin_inff());
+    greedy = !(T > 0.f);
+  }
+  __device__ __forceinline__ bool ranked() const { return k || p < 1.f; }
+  __device__ __forceinline__ Weigh weigh(int shift) const {
+    return Weigh{top, 1.0 / (double)T, (double)(1ull << shift)};
+  }
 };
 
-template <class T>
-__device__ __forceinline__ T block_sum(T v, T *scratch) {
-  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-  if (threadIdx.x % 64 == 0) scratch[threadIdx.x / 64] = v;
-  __syncthreads();
-  T sum = 0;
-  for (int w = 0; w < kWaves; ++w) sum += scratch[w];
-  __syncthreads();
-  return sum;
+// Bins of (top - z) / T, rising with falling logits; weights beyond the last are below half of 2^-s.
+struct Binning {
+  float top, scale, limit, per;
+  __device__ Binning(const Row &r, int shift) : top(r.top), scale(2.f / r.T) {
+    limit = (float)(shift + 1) * 0.69314718f + 0.01f;
+    per = kBins / limit;
+  }
+  // (of halves: two logits may be further apart than the largest float)
+  __device__ __forceinline__ float depth(float z) const { return z == top ? 0.f : (0.5f * top - 0.5f * z) * scale; }
+  __device__ __forceinline__ int bin(float x) const { return x < limit ? min(kBins - 1, (int)(x * per)) : kBins; }
+};
+
+// The largest of the slices' bests; every wave of the block for itself.
+__device__ __forceinline__ uint64_t row_best(const RowWork &w, int slices) {
+  const int lane = threadIdx.x % 64;
+  return wave_max(lane < slices ? w.best[lane] : 0);
 }
 
-// One row per block: the row is read once per step of the selection.
+// Pass 1, a block per slice of a row: its largest logit; the row's bins are cleared on the way.
 template <class Z>
-__global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs a, int shift) {
-  __shared__ uint64_t hist[256];
-  __shared__ uint64_t scratch[kWaves];
-  __shared__ uint64_t found[2];
-  const int row = blockIdx.x, V = a.vocab, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  const void *z = (const Z *)a.logits + (int64_t)row * a.stride;
-
-  // the largest logit and its first index
+__global__ __launch_bounds__(kSliceThreads) void largest_kernel(SampleArgs a, int slices, int len) {
+  RowWork &w = ((RowWork *)a.work)[blockIdx.y];
+  const void *z = (const Z *)a.logits + (int64_t)blockIdx.y * a.stride;
+  const int slice = blockIdx.x, lo = min(a.vocab, slice * len), hi = min(a.vocab, lo + len);
+  for (int i = slice * kSliceThreads + threadIdx.x; i < kBins; i += slices * kSliceThreads) w.mass[i] = 0, w.count[i] = 0;
+  if (slice == 0 && threadIdx.x == 0) w.n_list = 0;
   uint64_t best = 0;
-  for (int i = threadIdx.x; i < V; i += kThreads)
-    best = max(best, (uint64_t)rank_key(logit<Z>(z, i)) << 32 | (uint32_t)~i);
-  for (int o = 32; o; o >>= 1) best = max(best, (uint64_t)__shfl_xor((unsigned long long)best, o));
-  if (lane == 0) scratch[wave] = best;
+  for_each<Z, kSliceThreads>(z, lo, hi, [&](float x, int i) {
+    best = max(best, (uint64_t)rank_key(x) << 32 | (uint32_t)~i);
+  });
+  __shared__ uint64_t scratch[kSliceThreads / 64];
+  best = wave_max(best);
+  if (threadIdx.x % 64 == 0) scratch[threadIdx.x / 64] = best;
   __syncthreads();
-  for (int w = 0; w < kWaves; ++w) best = max(best, scratch[w]);
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < kSliceThreads / 64; ++i) best = max(best, scratch[i]);
+    w.best[slice] = best;
+  }
+}
+
+// Pass 2, for rows with a filter by rank: elements (for top-k) and mass (for top-p) by bin.  The
+// masses here are of 32-bit exponentials, rounded to 2^-31: they only choose which bins need
+// ranking, with their errors allowed for (least_of, most_of).
+template <class Z>
+__global__ __launch_bounds__(kSliceThreads) void bins_kernel(SampleArgs a, int slices, int len, int shift) {
+  RowWork &w = ((RowWork *)a.work)[blockIdx.y];
+  const Row r(a, blockIdx.y, row_best(w, slices));
+  if (r.none || r.greedy || !r.ranked()) return;
+  __shared__ uint64_t mass[kBins];
+  __shared__ uint32_t count[kBins];
+  for (int i = threadIdx.x; i < kBins; i += kSliceThreads) mass[i] = 0, count[i] = 0;
   __syncthreads();
-  const int first = (int)~(uint32_t)best;
-  const float top = logit<Z>(z, first), T = a.temperature ? a.temperature[row] : 1.f;
-  const bool none = !(top > -__builtin_inff());  // nothing but -inf and NaN
-  if (none || !(T > 0.f)) {
+  const void *z = (const Z *)a.logits + (int64_t)blockIdx.y * a.stride;
+  const int lo = min(a.vocab, (int)blockIdx.x * len), hi = min(a.vocab, lo + len);
+  const Binning bin(r, shift);
+  const bool by_mass = r.p < 1.f, by_count = r.k != 0;
+  for_each<Z, kSliceThreads>(z, lo, hi, [&](float v, int) {
+    const float x = bin.depth(v);
+    const int b = bin.bin(x);
+    if (b >= kBins) return;
+    if (by_mass) atomicAdd((unsigned long long *)&mass[b], (unsigned long long)(uint32_t)rintf(__builtin_amdgcn_exp2f(x * -1.44269504f) * 0x1p31f));
+    if (by_count) atomicAdd(&count[b], 1u);
+  });
+  __syncthreads();
+  for (int i = threadIdx.x; i < kBins; i += kSliceThreads) {
+    if (mass[i]) atomicAdd((unsigned long long *)&w.mass[i], (unsigned long long)mass[i]);
+    if (count[i]) atomicAdd(&w.count[i], count[i]);
+  }
+}
+
+// Bounds on the exact mass, in 2^-31, of elements whose binned masses sum to m: half a unit for each of at most
+// V elements, and the exponentials' own error (their arguments, up to 44, are off by a few
+// parts in 2^24: the results by less than 2^-15).
+__device__ __forceinline__ double least_of(uint64_t m, int V) { return (double)m * (1.0 - 0x1p-15) - 0.5 * V; }
+__device__ __forceinline__ double most_of(uint64_t m, int V) { return (double)m * (1.0 + 0x1p-15) + 0.5 * V; }
+
+// Pass 3: which bins may hold a cut (every block of a row finds them for itself), the elements of
+// those bins into the row's list, and each slice's exact masses of
+//   0: elements in bins before the list's
+//   1: those of them that min_p keeps
+//   2: elements in bins between the top-p cut's and the top-k cut's
+template <class Z>
+__global__ __launch_bounds__(kSliceThreads) void collect_kernel(SampleArgs a, int slices, int len, int shift) {
+  RowWork &w = ((RowWork *)a.work)[blockIdx.y];
+  const Row r(a, blockIdx.y, row_best(w, slices));
+  if (r.none || r.greedy) return;
+  __shared__ uint64_t mine[kCandidates], scratch[3][kSliceThreads / 64];
+  __shared__ uint32_t counts[kSliceThreads / 64];
+  __shared__ int cuts[3], n_mine, place;
+  __shared__ double reach[2];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, V = a.vocab;
+  // bins low .. high and rank_bin go into the list; bins past `last` hold nothing that is kept
+  int low = kBins, high = kBins, rank_bin = kBins;
+  if (threadIdx.x == 0) n_mine = 0;
+  if (r.ranked()) {
+    constexpr int kPer = kBins / kSliceThreads;
+    uint64_t mass[kPer], up = 0;
+    uint32_t count[kPer], up_n = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      up += mass[i] = w.mass[threadIdx.x * kPer + i];
+      up_n += count[i] = w.count[threadIdx.x * kPer + i];
+    }
+    uint64_t before = up;
+    uint32_t before_n = up_n;
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint64_t m = __shfl_up((unsigned long long)up, o);
+      const uint32_t n = __shfl_up(up_n, o);
+      if (lane >= o) up += m, up_n += n;
+    }
+    if (lane == 63) scratch[0][wave] = up, counts[wave] = up_n;
+    if (threadIdx.x == 0) cuts[0] = 0, cuts[1] = kBins - 1, cuts[2] = kBins;
+    __syncthreads();
+    before = up - before;
+    before_n = up_n - before_n;
+    uint64_t all = 0;
+    uint32_t all_n = 0;
+    for (int i = 0; i < kSliceThreads / 64; ++i) {
+      if (i < wave) before += scratch[0][i], before_n += counts[i];
+      all += scratch[0][i];
+      all_n += counts[i];
+    }
+    const bool cut_k = r.k && (uint32_t)r.k < all_n;  // else top-k cuts nothing but weights of 0
+    if (threadIdx.x == 0 && !cut_k) reach[0] = least_of(all, V), reach[1] = most_of(all, V);
+    if (cut_k) {
+      uint64_t at = before;
+      uint32_t n = before_n;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        if (n < (uint32_t)r.k && n + count[i] >= (uint32_t)r.k) {  // in one thread's one bin
+          cuts[2] = threadIdx.x * kPer + i;
+          reach[0] = least_of(at, V), reach[1] = most_of(at + mass[i], V);
+          if (blockIdx.x == 0) w.before_rank = n;
+        }
+        at += mass[i];
+        n += count[i];
+      }
+    }
+    __syncthreads();
+    low = high = rank_bin = cuts[2];
+    if (r.p < 1.f) {
+      // what top-p reaches for lies between these
+      const double least = (double)r.p * reach[0], most = (double)r.p * reach[1] + 1.0;
+      uint64_t at = before;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int b = threadIdx.x * kPer + i;
+        // the last bin that begins before it for certain, the first that ends past it for certain
+        if (most_of(at, V) < least) atomicMax(&cuts[0], b);
+        at += mass[i];
+        if (least_of(at, V) >= most) atomicMin(&cuts[1], b);
+      }
+      __syncthreads();
+      high = min(cuts[1], rank_bin);
+      low = min(cuts[0], high);
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) w.high = high, w.rank_bin = rank_bin;
+  }
+  __syncthreads();
+
+  const void *z = (const Z *)a.logits + (int64_t)blockIdx.y * a.stride;
+  const int lo = min(V, (int)blockIdx.x * len), hi = min(V, lo + len);
+  const Binning bin(r, shift);
+  const Weigh wt = r.weigh(shift);
+  const double least = r.least;
+  const int last = min(rank_bin, kBins - 1);
+  uint64_t sums[3] = {0, 0, 0};
+  for_each<Z, kSliceThreads>(z, lo, hi, [&](float v, int i) {
+    const int b = bin.bin(bin.depth(v));
+    if (b > last) return;
+    if ((b >= low && b <= high) || b == rank_bin) {
+      const int at = atomicAdd(&n_mine, 1);
+      if (at < kCandidates) mine[at] = code_of(rank_key(v), i);
+      return;
+    }
+    const double x = wt.weight(v);
+    const uint64_t n = wt.parts(x);
+    if (b < low) {
+      sums[0] += n;
+      if (!(x < least)) sums[1] += n;
+    } else {
+      sums[2] += n;
+    }
+  });
+#pragma unroll
+  for (int j = 0; j < 3; ++j) {
+    const uint64_t s = wave_sum(sums[j]);
+    if (lane == 0) scratch[j][wave] = s;
+  }
+  __syncthreads();
+  if (threadIdx.x < 3) {
+    uint64_t s = 0;
+    for (int i = 0; i < kSliceThreads / 64; ++i) s += scratch[threadIdx.x][i];
+    w.sums[blockIdx.x][threadIdx.x] = s;
+  }
+  if (threadIdx.x == 0 && n_mine) place = atomicAdd(&w.n_list, n_mine);
+  __syncthreads();
+  for (int i = threadIdx.x; i < min(n_mine, kCandidates); i += kSliceThreads)
+    if (place + i < kCandidates) w.list[place + i] = mine[i];
+}
+
+// The cut as a code, found by going over the whole row: for rows with more elements in the bins
+// that hold a cut than the list takes (few distinct logits).  A total in falling order (of ones,
+// or of weights), over elements up to the code `in`, first reaches `want` at the code returned; want is at least 1
+// and at most the total.
+template <class Z>
+__device__ uint64_t select_row(const void *z, int V, const Weigh &wt, uint64_t want, bool weighted, uint64_t in,
+                               uint64_t *hist, uint64_t *scratch, uint64_t *found) {
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  uint32_t key = 0;
+  uint64_t above = 0;  // total over keys above the prefix's range
+  for (int bits = 24; bits >= 0; bits -= 8) {
+    for (int i = threadIdx.x; i < 256; i += kThreads) hist[i] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < V; i += kThreads) {
+      const float x = logit<Z>(z, i);
+      const uint32_t k = rank_key(x);
+      if (code_of(k, i) > in || (bits < 24 && k >> (bits + 8) != key >> (bits + 8))) continue;
+      const uint64_t n = weighted ? wt.parts(wt.weight(x)) : 1;
+      if (n) atomicAdd((unsigned long long *)&hist[k >> bits & 255], (unsigned long long)n);
+    }
+    __syncthreads();
     if (threadIdx.x == 0) {
-      a.token[row] = none ? -1 : first;
-      if (a.prob) a.prob[row] = none ? 0.f : 1.f;
+      uint64_t sum = above;
+      int d = 255;
+      while (d > 0 && sum + hist[d] < want) sum += hist[d--];
+      found[0] = d;
+      found[1] = sum;
+    }
+    __syncthreads();
+    key |= (uint32_t)found[0] << bits;
+    above = found[1];
+    __syncthreads();
+  }
+  // equal logits: the first `ties` of them by index
+  const uint64_t one = weighted ? wt.parts(wt.weight(unrank(key))) : 1;
+  const uint64_t ties = one ? (want - above + one - 1) / one : 1;
+  uint64_t seen = 0;
+  for (int base = 0; base < V; base += kThreads) {
+    const int i = base + threadIdx.x;
+    const bool tie = i < V && rank_key(logit<Z>(z, i)) == key && code_of(key, i) <= in;
+    const uint64_t mask = __ballot(tie);
+    if (lane == 0) scratch[wave] = __popcll(mask);
+    __syncthreads();
+    uint64_t before = seen;
+    for (int w = 0; w < kWaves; ++w) {
+      if (w < wave) before += scratch[w];
+      seen += scratch[w];
+    }
+    before += __popcll(mask & ((1ull << lane) - 1));
+    if (tie && before + 1 == ties) found[0] = i;
+    __syncthreads();
+    if (seen >= ties) break;
+  }
+  const uint64_t cut = code_of(key, seen >= ties ? (int)found[0] : V);
+  __syncthreads();
+  return cut;
+}
+
+// What top-p reaches for, of a mass: at least 1, so that the first element stays.
+__device__ __forceinline__ uint64_t reach_of(float p, uint64_t mass) {
+  const double part = ceil((double)p * (double)mass);
+  return part < 1.0 ? 1 : min(mass, (uint64_t)part);
+}
+
+// Pass 4, a block per row: ranks the listed elements, which gives the cut, then finds the slice in
+// which the draw falls, and the element in it.
+template <class Z>
+__global__ __launch_bounds__(kThreads) void draw_kernel(SampleArgs a, int slices, int len, int shift) {
+  __shared__ uint64_t codes[kCandidates], parts[kCandidates];
+  __shared__ uint64_t hist[256], scratch[kWaves], found[2], in_slice[kMaxSlices];
+  __shared__ int n_early;
+  const int row = blockIdx.x, V = a.vocab, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const RowWork &w = ((const RowWork *)a.work)[row];
+  const void *z = (const Z *)a.logits + (int64_t)row * a.stride;
+  const Row r(a, row, row_best(w, slices));
+  if (r.none || r.greedy) {
+    if (threadIdx.x == 0) {
+      a.token[row] = r.none ? -1 : r.first;
+      if (a.prob) a.prob[row] = r.none ? 0.f : 1.f;
     }
     return;
   }
-  const Weigh wt{top, 1.0 / (double)T, (double)(1ull << shift)};
-
-  // the cut after the element at which a running total in falling order (of ones, or of
-  // weights) first reaches `want`; want is at least 1 and at most the total over `in`
-  auto select = [&](uint64_t want, bool weighted, Cut in) -> Cut {
-    uint32_t key = 0;
-    uint64_t above = 0;  // total over keys above the prefix's range
-    for (int bits = 24; bits >= 0; bits -= 8) {
-      for (int i = threadIdx.x; i < 256; i += kThreads) hist[i] = 0;
+  const Weigh wt = r.weigh(shift);
+  const double least = r.least;
+  auto kept = [&](float v, int i, uint64_t cut) -> uint64_t {
+    if (code_of(rank_key(v), i) > cut) return 0;
+    const double x = wt.weight(v);
+    return x < least ? 0 : wt.parts(x);
+  };
+  uint64_t cut = ~0ull;  // code of the last element that the filters by rank keep
+  const int n = r.ranked() ? w.n_list : 0;
+  if (n <= kCandidates) {
+    if ((int)threadIdx.x < kMaxSlices) {
+      const bool real = (int)threadIdx.x < slices;
+      in_slice[threadIdx.x] = real ? w.sums[threadIdx.x][1] : 0;
+      const uint64_t ahead = wave_sum(real ? w.sums[threadIdx.x][0] : (uint64_t)0);
+      const uint64_t between = wave_sum(real ? w.sums[threadIdx.x][2] : (uint64_t)0);
+      if (threadIdx.x == 0) scratch[0] = ahead, scratch[1] = between, found[0] = found[1] = 0, n_early = 0;
+    }
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+      codes[i] = w.list[i];
+      parts[i] = wt.parts(wt.weight(unrank(~(uint32_t)(codes[i] >> 32))));
+    }
+    __syncthreads();
+    if (n) {
+      const uint64_t ahead = scratch[0], between = scratch[1];
+      const int high = w.high, rank_bin = w.rank_bin;
+      const Binning bin(r, shift);
+      constexpr int kEach = kCandidates / kThreads;
+      uint64_t code[kEach], before[kEach];  // own elements, the listed mass before them
+      int rank[kEach], at[kEach];
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        const int i = e * kThreads + threadIdx.x;
+        code[e] = i < n ? codes[i] : ~0ull;
+        const float v = unrank(~(uint32_t)(code[e] >> 32));
+        at[e] = i < n ? bin.bin(bin.depth(v)) : kBins;
+        before[e] = 0;
+        rank[e] = 0;
+        if (i < n && at[e] < rank_bin) atomicAdd(&n_early, 1);
+      }
+      for (int j = 0; j < n; ++j) {
+        const uint64_t other = codes[j], m = parts[j];
+#pragma unroll
+        for (int e = 0; e < kEach; ++e)
+          if (e * kThreads < n && other < code[e]) before[e] += m, ++rank[e];
+      }
       __syncthreads();
+      // the top-k cut, and the listed mass up to it (all, without one)
+      const bool cut_k = r.k && rank_bin < kBins;
+      const int want = cut_k ? n_early + r.k - (int)w.before_rank - 1 : n - 1;
+#pragma unroll
+      for (int e = 0; e < kEach; ++e)
+        if (e * kThreads + (int)threadIdx.x < n && rank[e] == want)
+          found[0] = code[e], found[1] = before[e] + parts[e * kThreads + threadIdx.x];
+      __syncthreads();
+      cut = found[0];
+      if (r.p < 1.f) {
+        const uint64_t reach = reach_of(r.p, ahead + between + found[1]);
+        __syncthreads();
+        if (threadIdx.x == 0) found[0] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < kEach; ++e)
+          if (e * kThreads + (int)threadIdx.x < n && code[e] <= cut &&
+              ahead + (at[e] > high ? between : 0) + before[e] < reach)
+            atomicMax((unsigned long long *)&found[0], (unsigned long long)code[e]);
+        __syncthreads();
+        cut = found[0];
+      }
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        const int i = e * kThreads + threadIdx.x;
+        if (i >= n) break;
+        const uint64_t m = kept(unrank(~(uint32_t)(code[e] >> 32)), (int)(uint32_t)code[e], cut);
+        if (m) atomicAdd((unsigned long long *)&in_slice[(uint32_t)code[e] / len], (unsigned long long)m);
+      }
+    }
+  } else {
+    if (r.k) cut = select_row<Z>(z, V, wt, (uint64_t)r.k, false, cut, hist, scratch, found);
+    if (r.p < 1.f) {
+      uint64_t mass = 0;
       for (int i = threadIdx.x; i < V; i += kThreads) {
         const float x = logit<Z>(z, i);
-        const uint32_t k = rank_key(x);
-        if (!in.keeps(k, i) || (bits < 24 && k >> (bits + 8) != key >> (bits + 8))) continue;
-        const uint64_t n = weighted ? wt.parts(wt.weight(x)) : 1;
-        if (n) atomicAdd((unsigned long long *)&hist[k >> bits & 255], (unsigned long long)n);
+        if (code_of(rank_key(x), i) <= cut) mass += wt.parts(wt.weight(x));
       }
+      mass = wave_sum(mass);
+      if (lane == 0) scratch[wave] = mass;
       __syncthreads();
-      if (threadIdx.x == 0) {
-        uint64_t sum = above;
-        int d = 255;
-        while (d > 0 && sum + hist[d] < want) sum += hist[d--];
-        found[0] = d;
-        found[1] = sum;
-      }
+      mass = 0;
+      for (int i = 0; i < kWaves; ++i) mass += scratch[i];
       __syncthreads();
-      key |= (uint32_t)found[0] << bits;
-      above = found[1];
-      __syncthreads();
+      cut = select_row<Z>(z, V, wt, reach_of(r.p, mass), true, cut, hist, scratch, found);
     }
-    // equal logits: the first `ties` of them by index
-    const uint64_t one = weighted ? wt.parts(wt.weight(__builtin_bit_cast(float, key & 0x80000000u ? key ^ 0x80000000u : ~key))) : 1;
-    const uint64_t ties = one ? (want - above + one - 1) / one : 1;
-    uint64_t seen = 0;
-    for (int base = 0; base < V; base += kThreads) {
-      const int i = base + threadIdx.x;
-      const bool tie = i < V && rank_key(logit<Z>(z, i)) == key && in.keeps(key, i);
-      const uint64_t mask = __ballot(tie);
-      if (lane == 0) scratch[wave] = __popcll(mask);
-      __syncthreads();
-      uint64_t before = seen;
-      for (int w = 0; w < kWaves; ++w) {
-        if (w < wave) before += scratch[w];
-        seen += scratch[w];
-      }
-      before += __popcll(mask & ((1ull << lane) - 1));
-      if (tie && before + 1 == ties) found[0] = i;
-      __syncthreads();
-      if (seen >= ties) break;
+    for (int s = wave; s < kMaxSlices; s += kWaves) {
+      const int lo = min(V, s * len), hi = s < slices ? min(V, lo + len) : lo;
+      uint64_t mass = 0;
+      for (int i = lo + lane; i < hi; i += 64) mass += kept(logit<Z>(z, i), i, cut);
+      mass = wave_sum(mass);
+      if (lane == 0) in_slice[s] = mass;
     }
-    const Cut cut{key, seen >= ties ? (int)found[0] : V};
-    __syncthreads();
-    return cut;
-  };
-
-  Cut cut{0u, V};
-  const int k = a.top_k ? a.top_k[row] : 0;
-  if (k > 0 && k < V) cut = select((uint64_t)k, false, cut);
-  const float p = a.top_p ? a.top_p[row] : 1.f;
-  if (p < 1.f) {
-    uint64_t mass = 0;
-    for (int i = threadIdx.x; i < V; i += kThreads) {
-      const float x = logit<Z>(z, i);
-      if (cut.keeps(rank_key(x), i)) mass += wt.parts(wt.weight(x));
-    }
-    mass = block_sum(mass, scratch);
-    const double part = ceil((double)p * (double)mass);
-    const uint64_t want = part < 1.0 ? 1 : min(mass, (uint64_t)part);
-    cut = select(want, true, cut);
   }
-  const float least = a.min_p ? a.min_p[row] : 0.f;
-  const double floor = least > 1.f ? 1.0 : (double)least;
-
-  auto kept = [&](int i) -> uint64_t {
-    const float x = logit<Z>(z, i);
-    if (!cut.keeps(rank_key(x), i)) return 0;
-    const double w = wt.weight(x);
-    return w < floor ? 0 : wt.parts(w);
-  };
-  // every wave sums a run of the row; the draw falls into one of them
-  const int seg = (V + kWaves - 1) / kWaves, lo = min(V, wave * seg), hi = min(V, lo + seg);
-  uint64_t mine = 0;
-  for (int i = lo + lane; i < hi; i += 64) mine += kept(i);
-  for (int o = 32; o; o >>= 1) mine += __shfl_xor((unsigned long long)mine, o);
-  if (lane == 0) scratch[wave] = mine;
   __syncthreads();
-  uint64_t before = 0, mass = 0;
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) before += scratch[w];
-    mass += scratch[w];
+
+  // the draw, the slice it falls into, the wave's run of the slice, the element
+  uint64_t up = in_slice[lane];
+  const uint64_t own = up;
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint64_t v = __shfl_up((unsigned long long)up, o);
+    if (lane >= o) up += v;
   }
+  const uint64_t mass = __shfl((unsigned long long)up, 63);
   const float u = a.u[row];
   const double want = (double)u * (double)mass;
   const uint64_t target = !(want > 0.0) ? 0 : want >= (double)mass ? mass - 1 : min(mass - 1, (uint64_t)want);
+  const int slice = max(0, __ffsll((unsigned long long)__ballot(target < up)) - 1);
+  uint64_t before = __shfl((unsigned long long)(up - own), slice);
+  const int begin = min(V, slice * len), end = min(V, begin + len);
+  const int run = (end - begin + kWaves - 1) / kWaves, lo = min(end, begin + wave * run), hi = min(end, lo + run);
+  uint64_t mine = 0;
+  for (int i = lo + lane; i < hi; i += 64) mine += kept(logit<Z>(z, i), i, cut);
+  mine = wave_sum(mine);
+  __syncthreads();
+  if (lane == 0) scratch[wave] = mine;
+  __syncthreads();
+  for (int i = 0; i < wave; ++i) before += scratch[i];
   if (target < before || target >= before + mine) return;
   for (int base = lo; base < hi; base += 64) {
     const int i = base + lane;
-    const uint64_t w = i < hi ? kept(i) : 0;
-    uint64_t up = w;
+    const uint64_t m = i < hi ? kept(logit<Z>(z, i), i, cut) : 0;
+    uint64_t sum = m;
     for (int o = 1; o < 64; o <<= 1) {
-      const uint64_t v = __shfl_up((unsigned long long)up, o);
-      if (lane >= o) up += v;
+      const uint64_t v = __shfl_up((unsigned long long)sum, o);
+      if (lane >= o) sum += v;
     }
-    if (w && target >= before + up - w && target < before + up) {
+    if (m && target >= before + sum - m && target < before + sum) {
       a.token[row] = i;
-      if (a.prob) a.prob[row] = (float)((double)w / (double)mass);
+      if (a.prob) a.prob[row] = (float)((double)m / (double)mass);
     }
-    before += __shfl((unsigned long long)up, 63);
+    before += __shfl((unsigned long long)sum, 63);
     if (target < before) return;
   }
 }
 
+// Slices of a row: about 1024 blocks over all rows, each with at least 1024 elements.
+void slices_of(int rows, int vocab, int *slices, int *len) {
+  int s = (1024 + rows - 1) / rows;
+  s = s > kMaxSlices ? kMaxSlices : s;
+  const int most = (vocab + 1023) / 1024;
+  s = s > most ? most : s;
+  *len = (vocab + s - 1) / s;
+  *slices = (vocab + *len - 1) / *len;
+}
+
 template <class Z>
 hipError_t launch(const SampleArgs &a, hipStream_t s) {
-  int shift = 62;
+  int shift = 62, slices, len;
   while ((int64_t)1 << (62 - shift) < a.vocab) --shift;
-  void *args[] = {const_cast<SampleArgs *>(&a), &shift};
-  return hipLaunchKernel((const void *)sample_row_kernel<Z>, dim3(a.rows), dim3(kThreads), args, 0, s);
+  slices_of(a.rows, a.vocab, &slices, &len);
+  void *args[] = {const_cast<SampleArgs *>(&a), &slices, &len, &shift};
+  const dim3 grid(slices, a.rows);
+  hipError_t e = hipLaunchKernel((const void *)largest_kernel<Z>, grid, dim3(kSliceThreads), args, 0, s);
+  if (e == hipSuccess && (a.top_k || a.top_p))
+    e = hipLaunchKernel((const void *)bins_kernel<Z>, grid, dim3(kSliceThreads), args, 0, s);
+  if (e == hipSuccess) e = hipLaunchKernel((const void *)collect_kernel<Z>, grid, dim3(kSliceThreads), args, 0, s);
+  if (e == hipSuccess)
+    e = hipLaunchKernel((const void *)draw_kernel<Z>, dim3(a.rows), dim3(kThreads), args, 0, s);
+  return e;
 }
 
 }  // namespace
+
+size_t sample_work_bytes(int rows) { return (size_t)rows * sizeof(RowWork); }
 
 hipError_t launch_sample(const SampleArgs &a, int type, hipStream_t s) {
   return type == 0 ? launch<float>(a, s) : type == 1 ? launch<__bf16>(a, s) : launch<_Float16>(a, s);

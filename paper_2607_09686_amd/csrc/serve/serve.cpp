@@ -54,6 +54,7 @@ bool aligned(const void *p) { return (uintptr_t)p % 16 == 0; }
 
 // A grid holds less than 2^32 threads: at most 2^24 blocks of 256 per call.
 constexpr int64_t kMaxRows = 1 << 27, kMaxTokens = 1 << 24, kMaxSeqHeads = 1 << 22;
+constexpr int kMaxSampleRows = 65535;  // rows are a grid's second dimension
 // The grid of an attention call aims at this many units; partial results are kept for twice as many.
 constexpr int kFewTarget = 1024, kFewMinKeys = 256;
 constexpr int kManyTarget = 512, kManyMinKeys = 512;
@@ -188,18 +189,31 @@ int moe_kv_attend(const moe_kv_batch *b, int32_t window, float scale, const void
   return e == hipSuccess ? MOE_OK : hip_fail("moe_kv_attend", e);
 }
 
-int moe_sample(const moe_sample_batch *b, int32_t *token, float *prob) {
+int moe_sample_workspace(const moe_sample_batch *b, uint64_t *bytes) {
+  if (!b || !bytes) return fail(MOE_EINVAL, "moe_sample_workspace: the batch or bytes is NULL");
+  if (b->n_rows < 0 || b->n_rows > kMaxSampleRows)
+    return fail(MOE_EINVAL, "moe_sample_workspace: n_rows must be in [0, 65535]");
+  *bytes = sample_work_bytes(b->n_rows);
+  return MOE_OK;
+}
+
+int moe_sample(const moe_sample_batch *b, int32_t *token, float *prob, void *workspace, uint64_t workspace_bytes) {
   if (!b) return fail(MOE_EINVAL, "moe_sample: the batch is NULL");
   if (b->dtype != MOE_F32 && b->dtype != MOE_BF16 && b->dtype != MOE_F16)
     return fail(MOE_EINVAL, "moe_sample: dtype must be MOE_F32, MOE_BF16 or MOE_F16");
   if (b->vocab < 1 || b->vocab > 1 << 20) return fail(MOE_EINVAL, "moe_sample: vocab must be in [1, 2^20]");
-  if (b->n_rows < 0 || b->n_rows > 1 << 20) return fail(MOE_EINVAL, "moe_sample: n_rows must be in [0, 2^20]");
+  if (b->n_rows < 0 || b->n_rows > kMaxSampleRows) return fail(MOE_EINVAL, "moe_sample: n_rows must be in [0, 65535]");
   if (b->n_rows == 0) return MOE_OK;
   if (!b->logits || !b->u || !token) return fail(MOE_EINVAL, "moe_sample: logits, u and token must not be NULL");
   if (b->row_stride < b->vocab || b->row_stride > (int64_t)1 << 32)
     return fail(MOE_EINVAL, "moe_sample: row_stride must be at least vocab");
+  if (!workspace || !aligned(workspace) || workspace_bytes < sample_work_bytes(b->n_rows))
+    return fail(MOE_EINVAL, "moe_sample: the workspace must be 16-byte aligned and of at least %llu bytes",
+                (unsigned long long)sample_work_bytes(b->n_rows));
+  const uintptr_t size = b->dtype == MOE_F32 ? 4 : 2;
+  if ((uintptr_t)b->logits % size) return fail(MOE_EINVAL, "moe_sample: logits are not aligned to their elements");
   const SampleArgs a{b->logits, b->row_stride, b->n_rows, b->vocab, b->temperature, b->top_p, b->min_p,
-                     b->top_k,  b->u,          token,     prob};
+                     b->top_k,  b->u,          token,     prob,     workspace};
   const hipStream_t s = (hipStream_t)b->hip_stream;
   DeviceScope scope;
   hipError_t e = scope.enter(s);

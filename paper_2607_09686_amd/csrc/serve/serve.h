@@ -63,7 +63,9 @@ struct SampleArgs {
   const float *u;                            // [rows]
   int32_t *token;                            // [rows]
   float *prob;                               // [rows], nullable
+  void *work;                                // sample_work_bytes(rows)
 };
+size_t sample_work_bytes(int rows);
 // type of the logits: 0 fp32, 1 bf16, 2 fp16
 hipError_t launch_sample(const SampleArgs &a, int type, hipStream_t s);
 

@@ -174,7 +174,8 @@ def lib():
         "moe_kv_append": ([P(KvBatch), P(KvRope), i32, vp, i64, vp, i64, vp, i64, vp, i64], ctypes.c_int),
         "moe_kv_attend": ([P(KvBatch), i32, ctypes.c_float, vp, i64, vp, i64, vp, u64], ctypes.c_int),
         "moe_kv_attend_workspace": ([P(KvBatch), P(u64)], ctypes.c_int),
-        "moe_sample": ([P(SampleBatch), vp, vp], ctypes.c_int),
+        "moe_sample": ([P(SampleBatch), vp, vp, vp, u64], ctypes.c_int),
+        "moe_sample_workspace": ([P(SampleBatch), P(u64)], ctypes.c_int),
         "moe_pack_gguf": ([ctypes.c_char_p] * 4 + [P(PackInfo)], ctypes.c_int),
     }
     for name, (args, res) in sig.items():

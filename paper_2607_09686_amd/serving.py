@@ -193,6 +193,9 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None):
     b = SampleBatch(_types()[logits.dtype], n, vocab, 0, logits.data_ptr(),
                     logits.stride(0) if n > 1 else vocab, *row, _vector(u, "u", torch.float32, n, dev),
                     torch.cuda.current_stream(dev).cuda_stream)
+    size = ctypes.c_uint64()
+    _check(lib().moe_sample_workspace(ctypes.byref(b), ctypes.byref(size)))
+    work = torch.empty(size.value, dtype=torch.uint8, device=dev)
     with torch.cuda.device(dev):
-        _check(lib().moe_sample(ctypes.byref(b), tokens.data_ptr(), probs.data_ptr()))
+        _check(lib().moe_sample(ctypes.byref(b), tokens.data_ptr(), probs.data_ptr(), work.data_ptr(), size.value))
     return tokens, probs
