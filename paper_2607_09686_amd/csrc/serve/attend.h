@@ -21,8 +21,8 @@
 // block derives the cut from them itself: with W = sum over tiles of the keys they span, a unit
 // takes C = max(min_keys, ceil(W * kv_heads / target)) keys, which bounds the number of units by
 // target / kv_heads + tiles whatever the lengths are (the grid), and evens out ragged
-// batches.  A tile of several units leaves partial (m, l, o) rows in the workspace, joined by a
-// second launch.
+// batches.  A tile of several units leaves partial (m, l, o) rows in the workspace, and a note of
+// itself for a second launch, which joins them.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -59,11 +59,6 @@ constexpr int kThreads = 256, kWaves = kThreads / kLanes;
 constexpr int kIds = 1024;  // page ids of a unit held in LDS at a time
 constexpr float kNegInf = -__builtin_inff();
 
-__device__ __forceinline__ int64_t wave_sum(int64_t v) {
-  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-  return v;
-}
-
 // One sequence's share of the batch, read defensively: whatever starts and lengths hold, rows
 // stay within [0, n_tokens) and keys within the table.
 struct Seq {
@@ -89,60 +84,65 @@ __device__ __forceinline__ int span_of(const AttendArgs &a, const Seq &q) {
   const int64_t reach = (int64_t)a.window + (M - 1) / a.kv.group + 1 + 64;
   return (int)min((int64_t)q.length, reach);
 }
-__device__ __forceinline__ int units_of(int span, int C) { return max(1, (span + C - 1) / C); }
+// Units of a tile that spans `span` keys: the nearest whole number of C's (a tile of few more keys
+// than C is better left whole than split and joined), which it shares out evenly.
+__device__ __forceinline__ int units_of(int span, int C) { return max(1, (int)(((int64_t)span + C / 2) / C)); }
+__device__ __forceinline__ int share_of(int keys, int units) { return ((keys + units - 1) / units + 63) & ~63; }
 
-// Keys of a unit, from the whole batch.  All lanes of a wave get the same value.
+// Keys of a unit, from the whole batch.  `mine` is sequence threadIdx.x % 64 where there is one.
+// All lanes of a wave get the same value.
 template <int M>
-__device__ __forceinline__ int plan_keys(const AttendArgs &a, int *widest) {
-  int64_t work = 0;
-  int wide = 0;
-  for (int s = threadIdx.x % kLanes; s < a.kv.n_seqs; s += kLanes) {
+__device__ __forceinline__ int plan_keys(const AttendArgs &a, const Seq &mine) {
+  int64_t work = (int64_t)tiles_of<M>(a, mine) * span_of<M>(a, mine);
+  for (int s = threadIdx.x % kLanes + kLanes; s < a.kv.n_seqs; s += kLanes) {
     const Seq q = seq_of(a.kv, s);
-    const int t = tiles_of<M>(a, q), span = span_of<M>(a, q);
-    work += (int64_t)t * span;
-    if (t) wide = max(wide, span);
+    work += (int64_t)tiles_of<M>(a, q) * span_of<M>(a, q);
   }
-  work = wave_sum(work);
-  for (int o = 32; o; o >>= 1) wide = max(wide, __shfl_xor(wide, o));
-  *widest = wide;
+  for (int o = 1; o < min(kLanes, a.kv.n_seqs); o <<= 1) work += __shfl_xor(work, o);
+  work = __shfl(work, 0);  // lanes past the sequences have their own sums of nothing
   const int64_t c = (work * a.kv.kv_heads + a.target - 1) / a.target;
   return (int)min((int64_t)1 << 30, max((int64_t)a.min_keys, (c + 63) & ~(int64_t)63));
 }
 
-// Where a unit (or a sequence's first one) stands.
+// Where a unit stands: its sequence and its number among the sequence's units; the split tiles and
+// the units of split tiles in the sequences before.
 struct Place {
-  int seq, index;   // index: the unit's number within its sequence
-  int64_t slot;     // first partial-result slot of the sequence
+  int seq, index;
+  int64_t tiles, slots;
   Seq q;
 };
-// The sequence holding unit `want` (by_seq: the sequence `want` itself).  False past the last one.
 template <int M>
-__device__ __forceinline__ bool plan_find(const AttendArgs &a, int C, int want, bool by_seq, Place *out) {
-  int64_t units = 0, slots = 0;
+__device__ __forceinline__ bool plan_find(const AttendArgs &a, const Seq &mine, int C, int want, Place *out) {
+  int64_t units = 0, tiles = 0, slots = 0;
   const int lane = threadIdx.x % kLanes;
   for (int s0 = 0; s0 < a.kv.n_seqs; s0 += kLanes) {
-    Seq q{0, 0, 0, false};
-    if (s0 + lane < a.kv.n_seqs) q = seq_of(a.kv, s0 + lane);
+    Seq q = mine;
+    if (s0) q = s0 + lane < a.kv.n_seqs ? seq_of(a.kv, s0 + lane) : Seq{0, 0, 0, false};
     const int per = units_of(span_of<M>(a, q), C);
-    const int64_t n = (int64_t)tiles_of<M>(a, q) * per, m = per > 1 ? n : 0;
-    int64_t nu = n, ns = m;  // inclusive prefix sums over the lanes
-    for (int o = 1; o < kLanes; o <<= 1) {
-      const int64_t u = __shfl_up(nu, o), v = __shfl_up(ns, o);
-      if (lane >= o) nu += u, ns += v;
+    // (no batch has 2^24 units: only starts out of order could add up to more)
+    const int n = (int)min((int64_t)1 << 24, (int64_t)tiles_of<M>(a, q) * per), m = per > 1 ? n : 0;
+    const int t = per > 1 ? n / per : 0;
+    int nu = n, ns = m, nt = t;  // inclusive prefix sums over the lanes
+    const int lanes = min(kLanes, a.kv.n_seqs - s0);
+    for (int o = 1; o < lanes; o <<= 1) {
+      const int u = __shfl_up(nu, o), v = __shfl_up(ns, o), w = __shfl_up(nt, o);
+      if (lane >= o) nu += u, ns += v, nt += w;
     }
-    const bool hit = by_seq ? s0 + lane == want : want < units + nu;
-    const uint64_t any = __ballot(hit);
+    const uint64_t any = __ballot(lane < lanes && want < units + nu);
     if (any) {
       const int at = __ffsll((unsigned long long)any) - 1;
       out->seq = s0 + at;
       out->index = (int)(want - (units + __shfl(nu - n, at)));
-      out->slot = slots + __shfl(ns - m, at);
+      out->slots = slots + __shfl(ns - m, at);
+      out->tiles = tiles + __shfl(nt - t, at);
       out->q = Seq{__shfl(q.first, at), __shfl(q.count, at), __shfl(q.length, at), (bool)__shfl((int)q.bad, at)};
       return true;
     }
-    units += __shfl(nu, kLanes - 1);
-    slots += __shfl(ns, kLanes - 1);
+    units += __shfl(nu, lanes - 1);
+    slots += __shfl(ns, lanes - 1);
+    tiles += __shfl(nt, lanes - 1);
   }
+  out->tiles = tiles;
   return false;
 }
 
@@ -329,14 +329,28 @@ __device__ __forceinline__ void store_out(const AttendArgs &a, const Seq &q, int
   *(typename Vec<E>::x4 *)((E *)a.out + (int64_t)tok * a.out_stride + (int64_t)head * D + d) = e;
 }
 
-// Partial results: o rows of slot (slot, kvh), then (m, l) pairs of all slots.
+// The workspace: how many tiles were split (written by the last block), a note of each, then the
+// o rows of slot (slot, kvh), then (m, l) pairs of all slots.
+struct SplitTile {
+  int32_t slot, units;        // its first partial result, and their number
+  int32_t first, row0, rows;  // its sequence's first token row, the tile's first row in the sequence, its rows
+  int32_t pad[3];
+};
+struct SplitTiles {
+  int32_t count, pad[7];
+  SplitTile tile[];
+};
+__device__ __forceinline__ SplitTiles *split_tiles(const AttendArgs &a) { return (SplitTiles *)a.work; }
+__device__ __forceinline__ float *part_base(const AttendArgs &a) {
+  return (float *)((uint8_t *)a.work + sizeof(SplitTiles) + a.max_tiles * sizeof(SplitTile));
+}
 template <int D, int M>
 __device__ __forceinline__ float *part_o(const AttendArgs &a, int64_t slot, int kvh, int row) {
-  return a.part + ((slot * a.kv.kv_heads + kvh) * M + row) * D;
+  return part_base(a) + ((slot * a.kv.kv_heads + kvh) * M + row) * D;
 }
 template <int D, int M>
 __device__ __forceinline__ float *part_ml(const AttendArgs &a, int64_t slot, int kvh, int row) {
-  return a.part + (int64_t)a.max_slots * a.kv.kv_heads * M * D + ((slot * a.kv.kv_heads + kvh) * M + row) * 2;
+  return part_base(a) + (int64_t)a.max_slots * a.kv.kv_heads * M * D + ((slot * a.kv.kv_heads + kvh) * M + row) * 2;
 }
 
 // The ids of the unit's pages pg0 .. , at most kIds of them, into LDS; an id outside the pool is
@@ -363,11 +377,24 @@ struct Unit {
 };
 template <int M>
 __device__ __forceinline__ bool unit_of(const AttendArgs &a, Unit *u) {
-  int widest;
-  const int C = plan_keys<M>(a, &widest);
+  const int lane = threadIdx.x % kLanes;
+  Seq mine{0, 0, 0, false};
+  if (lane < a.kv.n_seqs) mine = seq_of(a.kv, lane);
+  const int C = plan_keys<M>(a, mine);
   Place pl;
   u->kvh = blockIdx.x % a.kv.kv_heads;
-  if (!plan_find<M>(a, C, blockIdx.x / a.kv.kv_heads, false, &pl)) return false;
+  const int unit = blockIdx.x / a.kv.kv_heads;
+  const bool found = plan_find<M>(a, mine, C, unit, &pl);
+  if (unit == a.max_units - 1 && u->kvh == 0 && threadIdx.x == 0) {
+    // the grid's last unit lies past the batch's last one, or is it
+    int64_t count = pl.tiles;
+    if (found) {
+      const int per = units_of(span_of<M>(a, pl.q), C);
+      if (per > 1) count += tiles_of<M>(a, pl.q);
+    }
+    split_tiles(a)->count = (int)min((int64_t)a.max_tiles, count);
+  }
+  if (!found) return false;
   const int per = units_of(span_of<M>(a, pl.q), C);
   // the tiles with the most keys first
   const int order = pl.index / per, split = pl.index % per;
@@ -375,13 +402,20 @@ __device__ __forceinline__ bool unit_of(const AttendArgs &a, Unit *u) {
   u->q = pl.q;
   u->tile = tiles_of<M>(a, pl.q) - 1 - order;
   const Range r = range_of<M>(a, pl.q, u->tile);
-  const int real = units_of(r.hi - r.lo, C);  // the tile's units that have keys
-  if (split >= real) return false;
-  u->k0 = r.lo + split * C;
-  u->k1 = min(r.hi, u->k0 + C);
-  u->slot = real > 1 ? pl.slot + pl.index : -1;
-  if (u->slot >= a.max_slots) return false;  // starts out of order can ask for more than there are
-  return true;
+  const int share = share_of(r.hi - r.lo, per);
+  const int real = max(1, (r.hi - r.lo + share - 1) / max(1, share));  // the tile's units that have keys
+  u->k0 = r.lo + split * share;
+  u->k1 = min(r.hi, u->k0 + share);
+  u->slot = real > 1 ? pl.slots + pl.index : -1;
+  if (per > 1) {
+    // starts out of order can ask for more than there are
+    if (pl.slots + pl.index + per > a.max_slots || pl.tiles + order >= a.max_tiles) return false;
+    if (split == 0 && u->kvh == 0 && threadIdx.x == 0)
+      split_tiles(a)->tile[pl.tiles + order] =
+          SplitTile{(int)(pl.slots + pl.index), real, pl.q.first, u->tile * M,
+                    min(M, pl.q.count * a.kv.group - u->tile * M), {0, 0, 0}};
+  }
+  return split < real;
 }
 
 // Rows of a sequence that cannot be served become NaN.
@@ -645,74 +679,73 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_many_kernel(
 }
 
 // ---------------------------------------------------------------------------------------------
-// Joins the units of split tiles: one row (new token, query head) per block and round, the row's
-// units spread over the block's groups of D / 4 lanes.
+// Joins the units of split tiles: a block per tile, KV head and eighth of the tile's rows (every
+// eighth row, so that the few rows of a decode step get a block each).  The block's groups of D / 4
+// lanes share out a row's units, or several rows' where there are fewer units than groups.
 // ---------------------------------------------------------------------------------------------
-constexpr int kJoinThreads = 512;
+constexpr int kJoinRows = 8;
 
 template <class E, int D, int M>
-__global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a) {
-  constexpr int kPer = D / 4, kGroups = kJoinThreads / kPer;
+__global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
+  constexpr int kPer = D / 4, kGroups = kThreads / kPer;
   __shared__ __align__(16) float sum[kGroups][D];
-  __shared__ float sums_l[kGroups];
-  int widest;
-  const int C = plan_keys<M>(a, &widest);
-  if (widest <= C) return;  // no tile was split
-  const KvView &kv = a.kv;
-  const int g = threadIdx.x / kPer, d = threadIdx.x % kPer * 4, lane = threadIdx.x % kLanes;
-  for (int64_t item = blockIdx.x; item < (int64_t)kv.n_tokens * kv.heads; item += gridDim.x) {
-    const int tok = (int)(item / kv.heads), head = (int)(item % kv.heads), kvh = head / kv.group;
-    // the sequence of this token: the last one starting at or before it
-    int seq = -1;
-    for (int s0 = 0; s0 < kv.n_seqs; s0 += kLanes) {
-      bool in = false;
-      if (s0 + lane < kv.n_seqs) {
-        const Seq q = seq_of(kv, s0 + lane);
-        in = tok >= q.first && tok < q.first + q.count;
-      }
-      const uint64_t any = __ballot(in);
-      if (any) {
-        seq = s0 + __ffsll((unsigned long long)any) - 1;
-        break;
-      }
-    }
-    if (seq < 0) continue;
-    Place pl;
-    if (!plan_find<M>(a, C, seq, true, &pl) || pl.q.bad) continue;
-    const int row = (tok - pl.q.first) * kv.group + head % kv.group, tile = row / M;
-    const Range r = range_of<M>(a, pl.q, tile);
-    const int real = units_of(r.hi - r.lo, C), per = units_of(span_of<M>(a, pl.q), C);
-    if (real <= 1) continue;
-    const int64_t slot = pl.slot + (int64_t)(tiles_of<M>(a, pl.q) - 1 - tile) * per;
-    if (slot + real > a.max_slots) continue;
-    float top = kNegInf;
-    for (int i = lane; i < real; i += kLanes) top = fmaxf(top, part_ml<D, M>(a, slot + i, kvh, row % M)[0]);
-    for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-    const float base = top == kNegInf ? 0.f : top;
+  __shared__ float stat[kGroups][2];
+  const int item = blockIdx.x / a.kv.kv_heads, kvh = blockIdx.x % a.kv.kv_heads;
+  const SplitTile t = split_tiles(a)->tile[item];
+  if (item >= split_tiles(a)->count) return;
+  // starts out of order can leave a note unwritten: nothing is taken from one that makes no sense
+  if (t.units < 2 || t.slot < 0 || t.slot > a.max_slots - t.units || t.rows < 1 || t.rows > M || t.first < 0 ||
+      t.row0 < 0 || t.row0 > (1 << 28) || t.first > a.kv.n_tokens - 1 - (t.row0 + t.rows - 1) / a.kv.group)
+    return;
+  const int g = threadIdx.x / kPer, d = threadIdx.x % kPer * 4;
+  // groups to a row: a power of two, so that a tile of few units has several rows joined at once
+  int per = 1;
+  while (per < kGroups && per < t.units) per *= 2;
+  const int own = g / per, at_once = kGroups / per;
+  const int64_t step = (int64_t)a.kv.kv_heads * M;  // rows from unit to unit
+  for (int r0 = 0; blockIdx.y + kJoinRows * r0 < t.rows; r0 += at_once) {
+    const int row = blockIdx.y + kJoinRows * (r0 + own);
+    float m = kNegInf, l = 0.f;
     f32x4 o{};
-    float l = 0.f;
+    if (row < t.rows) {
+      const float *ml = part_ml<D, M>(a, t.slot, kvh, row), *part = part_o<D, M>(a, t.slot, kvh, row) + d;
 #pragma unroll 4
-    for (int i = g; i < real; i += kGroups) {
-      const float *ml = part_ml<D, M>(a, slot + i, kvh, row % M);
-      const float w = __builtin_amdgcn_exp2f(ml[0] - base);
-      l += w * ml[1];
-      o += w * *(const f32x4 *)(part_o<D, M>(a, slot + i, kvh, row % M) + d);
+      for (int i = g % per; i < t.units; i += per) {
+        const float mi = ml[i * step * 2], li = ml[i * step * 2 + 1];
+        const f32x4 oi = *(const f32x4 *)(part + i * step * D);
+        const float top = fmaxf(m, mi), base = top == kNegInf ? 0.f : top;
+        const float w = __builtin_amdgcn_exp2f(mi - base), shrink = __builtin_amdgcn_exp2f(m - base);
+        l = l * shrink + w * li;
+        o = o * shrink + w * oi;
+        m = top;
+      }
     }
     *(f32x4 *)&sum[g][d] = o;
-    if (d == 0) sums_l[g] = l;
+    if (d == 0) stat[g][0] = m, stat[g][1] = l;
     __syncthreads();
-    if (g == 0) {
+    if (g % per == 0 && row < t.rows) {
+      float top = kNegInf;
+      for (int i = 0; i < per; ++i) top = fmaxf(top, stat[g + i][0]);
+      const float base = top == kNegInf ? 0.f : top;
       o = f32x4{};
       l = 0.f;
-      for (int i = 0; i < kGroups; ++i) {
-        o += *(const f32x4 *)&sum[i][d];
-        l += sums_l[i];
+      for (int i = 0; i < per; ++i) {
+        const float w = __builtin_amdgcn_exp2f(stat[g + i][0] - base);
+        o += w * *(const f32x4 *)&sum[g + i][d];
+        l += w * stat[g + i][1];
       }
-      store_out<E, D>(a, pl.q, kvh, row, d, o * finish(l));
+      store_out<E, D>(a, Seq{t.first, 0, 0, false}, kvh, t.row0 + row, d, o * finish(l));
     }
     __syncthreads();
   }
 }
+
+}  // namespace
+static inline uint64_t attend_work_size(const AttendArgs &a, int rows, int dim) {
+  return sizeof(SplitTiles) + a.max_tiles * sizeof(SplitTile) +
+         (uint64_t)a.max_slots * a.kv.kv_heads * rows * (dim + 2) * sizeof(float);
+}
+namespace {
 
 template <class E, int D, int M>
 hipError_t launch_kernels(const AttendArgs &a, hipStream_t s) {
@@ -721,9 +754,8 @@ hipError_t launch_kernels(const AttendArgs &a, hipStream_t s) {
   const void *fn = M == kFewRows ? (const void *)attend_few_kernel<E, D> : (const void *)attend_many_kernel<E, D>;
   hipError_t e = hipLaunchKernel(fn, grid, dim3(kThreads), args, 0, s);
   if (e != hipSuccess) return e;
-  const int64_t rows = (int64_t)a.kv.n_tokens * a.kv.heads;
-  return hipLaunchKernel((const void *)attend_join_kernel<E, D, M>, dim3((unsigned)(rows < 2048 ? rows : 2048)),
-                         dim3(kJoinThreads), args, 0, s);
+  return hipLaunchKernel((const void *)attend_join_kernel<E, D, M>, dim3(a.max_tiles * a.kv.kv_heads, kJoinRows),
+                         dim3(kThreads), args, 0, s);
 }
 
 }  // namespace

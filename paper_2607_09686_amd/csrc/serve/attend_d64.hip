@@ -2,5 +2,6 @@
 #include "attend.h"
 
 namespace moecache {
+uint64_t attend_work_bytes(const AttendArgs &a, int rows, int dim) { return attend_work_size(a, rows, dim); }
 template hipError_t launch_attend<64>(const AttendArgs &, bool, bool, hipStream_t);
 }  // namespace moecache

@@ -97,7 +97,8 @@ bool rows_ok(const void *p, int64_t stride, int heads, int dim, int size) {
 // its waves share the tile's steps: with few rows most of them have nothing to multiply.
 bool many_rows(const KvView &kv) { return (int64_t)kv.n_tokens * kv.group > (int64_t)64 * kv.n_seqs; }
 
-void plan(const KvView &kv, AttendArgs *a, bool *many, uint64_t *bytes, int dim) {
+void plan(AttendArgs *a, bool *many, uint64_t *bytes, int dim) {
+  const KvView &kv = a->kv;
   *many = many_rows(kv);
   const int rows = *many ? kManyRows : kFewRows;
   a->target = *many ? kManyTarget : kFewTarget;
@@ -108,7 +109,8 @@ void plan(const KvView &kv, AttendArgs *a, bool *many, uint64_t *bytes, int dim)
   const int64_t share = a->target / kv.kv_heads + 1;
   a->max_units = (int)(share + tiles);
   a->max_slots = (int)(2 * share);  // a split tile's ceil(x) units, x > 1, are fewer than 2 x
-  *bytes = (uint64_t)a->max_slots * kv.kv_heads * rows * (dim + 2) * sizeof(float);
+  a->max_tiles = (int)share;        // and at least two
+  *bytes = attend_work_bytes(*a, rows, dim);
 }
 
 }  // namespace
@@ -154,7 +156,7 @@ int moe_kv_attend_workspace(const moe_kv_batch *b, uint64_t *bytes) {
   const int rc = check_kv(b, "moe_kv_attend_workspace", &a.kv);
   if (rc) return rc;
   bool many;
-  plan(a.kv, &a, &many, bytes, b->head_dim);
+  plan(&a, &many, bytes, b->head_dim);
   return MOE_OK;
 }
 
@@ -170,14 +172,14 @@ int moe_kv_attend(const moe_kv_batch *b, int32_t window, float scale, const void
     return fail(MOE_EINVAL, "moe_kv_attend: q and out must be 16-byte aligned rows of n_heads * head_dim elements");
   bool many;
   uint64_t bytes;
-  plan(a.kv, &a, &many, &bytes, b->head_dim);
+  plan(&a, &many, &bytes, b->head_dim);
   if (!workspace || !aligned(workspace) || workspace_bytes < bytes)
     return fail(MOE_EINVAL, "moe_kv_attend: the workspace must be 16-byte aligned and of at least %llu bytes",
                 (unsigned long long)bytes);
   a.q = q, a.out = out, a.q_stride = q_stride, a.out_stride = out_stride;
   a.window = window;
   a.scale_log2 = scale * 1.44269504088896340736f;
-  a.part = (float *)workspace;
+  a.work = workspace;
   const hipStream_t s = (hipStream_t)b->hip_stream;
   DeviceScope scope;
   hipError_t e = scope.enter(s);

@@ -42,7 +42,8 @@ struct AttendArgs {
   int min_keys;        // fewest keys of a unit, a multiple of 64
   int max_units;       // grid units per KV head
   int max_slots;       // partial-result slots per KV head
-  float *part;         // [max_slots][kv_heads][tile rows][dim] then [max_slots][kv_heads][rows][2]
+  int max_tiles;       // split tiles
+  void *work;          // attend_work_bytes
 };
 
 // in_f32: q, k, v hold fp32 instead of the cache's type; half: the cache's type is fp16
@@ -51,6 +52,7 @@ hipError_t launch_append(const AppendArgs &a, bool half, bool in_f32, hipStream_
 // Rows of a tile of the two attention kernels: few rows per sequence (a block's waves share
 // the rows and split the keys) or many (they share the keys and split the rows).
 constexpr int kFewRows = 32, kManyRows = 128;
+uint64_t attend_work_bytes(const AttendArgs &a, int rows, int dim);
 template <int D>
 hipError_t launch_attend(const AttendArgs &a, bool half, bool many, hipStream_t s);
 
