@@ -9,8 +9,9 @@
 //
 // Whether an element is in and where the draw falls are decisions on sums of up to 2^20 weights, so
 // the weights are taken in 64 bits and then held as integers of 2^-s, s = 62 - log2 of the row's
-// length: sums of integers do not depend on their order, so every split of a row over threads gives
-// the same token, and two tokens' border is off by at most 2^(20 - s) of the largest weight.
+// length (at most 50): sums of integers do not depend on their order, so every split of a row over
+// threads gives the same token, and two tokens' border is off by at most 2^(20 - s) of the
+// largest weight.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -22,13 +23,16 @@ namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;  // of the draw, a block per row
 constexpr int kSliceThreads = 256;                      // of the passes over slices of a row
-constexpr int kMaxSlices = 64;
+constexpr int kSliceWaves = kSliceThreads / 64;
+constexpr int kMaxBlocks = 64;                          // of a row's passes; its slices are their waves
+constexpr int kMaxSlices = kMaxBlocks * kSliceWaves;
 constexpr int kBins = 2048;
 constexpr int kCandidates = 4096;
+constexpr int kOwn = 512;  // of them, a block's, before it hands them over one by one
 
 // Per row in the workspace.
 struct RowWork {
-  uint64_t best[kMaxSlices];     // slices' largest logit: rank key, then the smallest index
+  uint64_t best[kMaxBlocks];     // blocks' largest logit: rank key, then the smallest index
   uint64_t sums[kMaxSlices][3];  // slices' masses, see collect_kernel
   uint64_t mass[kBins];          // binned, in 2^-31
   uint32_t count[kBins];
@@ -54,23 +58,35 @@ __device__ __forceinline__ float unrank(uint32_t key) {
 // Elements in falling order, equal logits by rising index, are rising codes.
 __device__ __forceinline__ uint64_t code_of(uint32_t key, int i) { return (uint64_t)~key << 32 | (uint32_t)i; }
 
-// Calls f(logit, index) for lo <= index < hi, a block's threads together: 16-byte loads between
-// the first and the last aligned place.
-template <class Z, int N, class F>
-__device__ __forceinline__ void for_each(const void *row, int lo, int hi, F f) {
-  constexpr int kVec = 16 / sizeof(Z);
+// Calls f(logit, index) for lo <= index < hi, by one wave: 16-byte loads between the first and the
+// last aligned place, four in flight.  Every lane takes part in every call, with a NaN where it has no element;
+// g() is called after every few.
+template <class Z, class F, class G>
+__device__ __forceinline__ void for_each(const void *row, int lo, int hi, F f, G g) {
+  constexpr int kVec = 16 / sizeof(Z), kAhead = 4;
   typedef Z zv __attribute__((ext_vector_type(kVec)));
   const Z *z = (const Z *)row;
+  const float nan = __builtin_nanf("");
+  const int lane = threadIdx.x % 64;
   const int skip = (int)(-(uintptr_t)(z + lo) / sizeof(Z) % kVec);
   const int body = min(hi, lo + skip), vecs = (hi - body) / kVec, tail = body + vecs * kVec;
-  if ((int)threadIdx.x < body - lo) f((float)z[lo + threadIdx.x] + 0.f, lo + (int)threadIdx.x);
-#pragma unroll 2
-  for (int v = threadIdx.x; v < vecs; v += N) {
-    const zv e = *(const zv *)(z + body + v * kVec);
+  if (body > lo) f(lane < body - lo ? (float)z[lo + lane] + 0.f : nan, lo + lane);
+  if (hi > tail) f(lane < hi - tail ? (float)z[tail + lane] + 0.f : nan, tail + lane);
+  g();
+  for (int v0 = lane; v0 - lane < vecs; v0 += 64 * kAhead) {
+    zv e[kAhead];
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) f((float)e[j] + 0.f, body + v * kVec + j);
+    for (int u = 0; u < kAhead; ++u)
+      if (v0 + 64 * u < vecs) e[u] = *(const zv *)(z + body + (v0 + 64 * u) * kVec);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int v = v0 + 64 * u;
+      if (v - lane >= vecs) break;
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) f(v < vecs ? (float)e[u][j] + 0.f : nan, body + v * kVec + j);
+      g();
+    }
   }
-  if ((int)threadIdx.x < hi - tail) f((float)z[tail + threadIdx.x] + 0.f, tail + (int)threadIdx.x);
 }
 
 __device__ __forceinline__ uint64_t wave_sum(uint64_t v) {
@@ -82,16 +98,44 @@ __device__ __forceinline__ uint64_t wave_max(uint64_t v) {
   return v;
 }
 
+// exp((z - top) / T), and its whole number of 2^-shift's.
 struct Weigh {
-  float top;  // the row's largest logit
-  double scale, unit;  // 1 / T, 2^s
-  // exp((z - top) / T), 0 for NaN and -inf
-  __device__ __forceinline__ double weight(float z) const {
-    if (z == top) return 1.0;
+  float top;     // the row's largest logit
+  double scale;  // 1 / T
+  int shift;     // at most 50
+  struct Weight {
+    double w;
+    uint64_t parts;
+  };
+  // With x = n ln 2 + g, |g| <= ln 2 / 2: e^x = 2^n e^g, e^g by its series to g^12 / 12! (what is left
+  // is below 2^-52), the whole parts from the bits of e^g's mantissa.  0 for NaN and -inf.
+  __device__ __forceinline__ Weight operator()(float z) const {
+    if (z == top) return {1.0, 1ull << shift};
     const double x = ((double)z - (double)top) * scale;
-    return x > -64.0 ? exp(x) : 0.0;  // 2^-s > e^-64: nothing is lost, and NaN goes to 0
+    if (!(x > -64.0)) return {0.0, 0};  // e^-64 is below a half of every unit
+    const double n = rint(x * 1.4426950408889634);
+    const double g = fma(n, -1.9082149292705877e-10, fma(n, -0.6931471803691238, x));  // ln 2 in two parts
+    // odd and even powers apart: two chains of half the length
+    const double g2 = g * g;
+    double even = 1.0 / 479001600, odd = 1.0 / 39916800;
+    even = fma(even, g2, 1.0 / 3628800);
+    odd = fma(odd, g2, 1.0 / 362880);
+    even = fma(even, g2, 1.0 / 40320);
+    odd = fma(odd, g2, 1.0 / 5040);
+    even = fma(even, g2, 1.0 / 720);
+    odd = fma(odd, g2, 1.0 / 120);
+    even = fma(even, g2, 1.0 / 24);
+    odd = fma(odd, g2, 1.0 / 6);
+    even = fma(even, g2, 0.5);
+    odd = fma(odd, g2, 1.0);
+    const double e = fma(odd, g, fma(even, g2, 1.0));
+    const uint64_t bits = __builtin_bit_cast(uint64_t, e);
+    const int up = (int)n;
+    const uint64_t mantissa = (bits & ((1ull << 52) - 1)) | 1ull << 52;
+    const int k = 52 - ((int)(bits >> 52) - 1023) - up - shift;  // >= 2: x <= 0, shift <= 50
+    const uint64_t parts = k > 54 ? 0 : (mantissa + (1ull << (k - 1))) >> k;
+    return {__builtin_bit_cast(double, bits + ((uint64_t)(int64_t)up << 52)), parts};
   }
-  __device__ __forceinline__ uint64_t parts(double w) const { return (uint64_t)rint(w * unit); }
 };
 
 // A row's settings, and its largest logit.
@@ -113,7 +157,7 @@ struct Row {
   }
   __device__ __forceinline__ bool ranked() const { return k || p < 1.f; }
   __device__ __forceinline__ Weigh weigh(int shift) const {
-    return Weigh{top, 1.0 / (double)T, (double)(1ull << shift)};
+    return Weigh{top, 1.0 / (double)T, shift};
   }
 };
 
@@ -129,31 +173,32 @@ struct Binning {
   __device__ __forceinline__ int bin(float x) const { return x < limit ? min(kBins - 1, (int)(x * per)) : kBins; }
 };
 
-// The largest of the slices' bests; every wave of the block for itself.
-__device__ __forceinline__ uint64_t row_best(const RowWork &w, int slices) {
+// The largest of the blocks' bests; every wave of the block for itself.
+__device__ __forceinline__ uint64_t row_best(const RowWork &w, int blocks) {
   const int lane = threadIdx.x % 64;
-  return wave_max(lane < slices ? w.best[lane] : 0);
+  return wave_max(lane < blocks ? w.best[lane] : 0);
 }
 
-// Pass 1, a block per slice of a row: its largest logit; the row's bins are cleared on the way.
+// Pass 1, a wave per slice of a row: its largest logit; the row's bins are cleared on the way.
 template <class Z>
-__global__ __launch_bounds__(kSliceThreads) void largest_kernel(SampleArgs a, int slices, int len) {
+__global__ __launch_bounds__(kSliceThreads) void largest_kernel(SampleArgs a, int len) {
   RowWork &w = ((RowWork *)a.work)[blockIdx.y];
   const void *z = (const Z *)a.logits + (int64_t)blockIdx.y * a.stride;
-  const int slice = blockIdx.x, lo = min(a.vocab, slice * len), hi = min(a.vocab, lo + len);
-  for (int i = slice * kSliceThreads + threadIdx.x; i < kBins; i += slices * kSliceThreads) w.mass[i] = 0, w.count[i] = 0;
-  if (slice == 0 && threadIdx.x == 0) w.n_list = 0;
+  const int slice = blockIdx.x * kSliceWaves + threadIdx.x / 64, lo = min(a.vocab, slice * len);
+  for (int i = blockIdx.x * kSliceThreads + threadIdx.x; i < kBins; i += gridDim.x * kSliceThreads)
+    w.mass[i] = 0, w.count[i] = 0;
+  if (blockIdx.x == 0 && threadIdx.x == 0) w.n_list = 0;
   uint64_t best = 0;
-  for_each<Z, kSliceThreads>(z, lo, hi, [&](float x, int i) {
+  for_each<Z>(z, lo, min(a.vocab, lo + len), [&](float x, int i) __attribute__((always_inline)) {
     best = max(best, (uint64_t)rank_key(x) << 32 | (uint32_t)~i);
-  });
-  __shared__ uint64_t scratch[kSliceThreads / 64];
+  }, [] {});
+  __shared__ uint64_t scratch[kSliceWaves];
   best = wave_max(best);
   if (threadIdx.x % 64 == 0) scratch[threadIdx.x / 64] = best;
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int i = 1; i < kSliceThreads / 64; ++i) best = max(best, scratch[i]);
-    w.best[slice] = best;
+    for (int i = 1; i < kSliceWaves; ++i) best = max(best, scratch[i]);
+    w.best[blockIdx.x] = best;
   }
 }
 
@@ -161,25 +206,28 @@ __global__ __launch_bounds__(kSliceThreads) void largest_kernel(SampleArgs a, in
 // masses here are of 32-bit exponentials, rounded to 2^-31: they only choose which bins need
 // ranking, with their errors allowed for (least_of, most_of).
 template <class Z>
-__global__ __launch_bounds__(kSliceThreads) void bins_kernel(SampleArgs a, int slices, int len, int shift) {
+__global__ __launch_bounds__(kSliceThreads) void bins_kernel(SampleArgs a, int len, int shift) {
   RowWork &w = ((RowWork *)a.work)[blockIdx.y];
-  const Row r(a, blockIdx.y, row_best(w, slices));
+  const Row r(a, blockIdx.y, row_best(w, gridDim.x));
   if (r.none || r.greedy || !r.ranked()) return;
   __shared__ uint64_t mass[kBins];
   __shared__ uint32_t count[kBins];
   for (int i = threadIdx.x; i < kBins; i += kSliceThreads) mass[i] = 0, count[i] = 0;
   __syncthreads();
   const void *z = (const Z *)a.logits + (int64_t)blockIdx.y * a.stride;
-  const int lo = min(a.vocab, (int)blockIdx.x * len), hi = min(a.vocab, lo + len);
+  const int lo = min(a.vocab, (int)(blockIdx.x * kSliceWaves + threadIdx.x / 64) * len);
   const Binning bin(r, shift);
   const bool by_mass = r.p < 1.f, by_count = r.k != 0;
-  for_each<Z, kSliceThreads>(z, lo, hi, [&](float v, int) {
+  for_each<Z>(z, lo, min(a.vocab, lo + len), [&](float v, int) __attribute__((always_inline)) {
     const float x = bin.depth(v);
     const int b = bin.bin(x);
     if (b >= kBins) return;
-    if (by_mass) atomicAdd((unsigned long long *)&mass[b], (unsigned long long)(uint32_t)rintf(__builtin_amdgcn_exp2f(x * -1.44269504f) * 0x1p31f));
+    if (by_mass) {
+      const uint32_t m = (uint32_t)rintf(__builtin_amdgcn_exp2f(x * -1.44269504f) * 0x1p31f);
+      atomicAdd((unsigned long long *)&mass[b], (unsigned long long)m);
+    }
     if (by_count) atomicAdd(&count[b], 1u);
-  });
+  }, [] {});
   __syncthreads();
   for (int i = threadIdx.x; i < kBins; i += kSliceThreads) {
     if (mass[i]) atomicAdd((unsigned long long *)&w.mass[i], (unsigned long long)mass[i]);
@@ -199,12 +247,22 @@ __device__ __forceinline__ double most_of(uint64_t m, int V) { return (double)m 
 //   1: those of them that min_p keeps
 //   2: elements in bins between the top-p cut's and the top-k cut's
 template <class Z>
-__global__ __launch_bounds__(kSliceThreads) void collect_kernel(SampleArgs a, int slices, int len, int shift) {
+__global__ __launch_bounds__(kSliceThreads) void collect_kernel(SampleArgs a, int len, int shift) {
   RowWork &w = ((RowWork *)a.work)[blockIdx.y];
-  const Row r(a, blockIdx.y, row_best(w, slices));
+  constexpr int kPer = kBins / kSliceThreads;
+  uint64_t mass[kPer];  // asked for together with the row's settings
+  uint32_t count[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    mass[i] = w.mass[threadIdx.x * kPer + i];
+    count[i] = w.count[threadIdx.x * kPer + i];
+  }
+  const Row r(a, blockIdx.y, row_best(w, gridDim.x));
   if (r.none || r.greedy) return;
-  __shared__ uint64_t mine[kCandidates], scratch[3][kSliceThreads / 64];
-  __shared__ uint32_t counts[kSliceThreads / 64];
+  constexpr int kQueue = 64 * (16 / sizeof(Z)) + 128;
+  __shared__ uint64_t mine[kOwn], scratch[kSliceWaves];
+  __shared__ float queues[kSliceWaves][kQueue];
+  __shared__ uint32_t counts[kSliceWaves];
   __shared__ int cuts[3], n_mine, place;
   __shared__ double reach[2];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, V = a.vocab;
@@ -212,14 +270,10 @@ __global__ __launch_bounds__(kSliceThreads) void collect_kernel(SampleArgs a, in
   int low = kBins, high = kBins, rank_bin = kBins;
   if (threadIdx.x == 0) n_mine = 0;
   if (r.ranked()) {
-    constexpr int kPer = kBins / kSliceThreads;
-    uint64_t mass[kPer], up = 0;
-    uint32_t count[kPer], up_n = 0;
+    uint64_t up = 0;
+    uint32_t up_n = 0;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      up += mass[i] = w.mass[threadIdx.x * kPer + i];
-      up_n += count[i] = w.count[threadIdx.x * kPer + i];
-    }
+    for (int i = 0; i < kPer; ++i) up += mass[i], up_n += count[i];
     uint64_t before = up;
     uint32_t before_n = up_n;
     for (int o = 1; o < 64; o <<= 1) {
@@ -227,16 +281,16 @@ __global__ __launch_bounds__(kSliceThreads) void collect_kernel(SampleArgs a, in
       const uint32_t n = __shfl_up(up_n, o);
       if (lane >= o) up += m, up_n += n;
     }
-    if (lane == 63) scratch[0][wave] = up, counts[wave] = up_n;
+    if (lane == 63) scratch[wave] = up, counts[wave] = up_n;
     if (threadIdx.x == 0) cuts[0] = 0, cuts[1] = kBins - 1, cuts[2] = kBins;
     __syncthreads();
     before = up - before;
     before_n = up_n - before_n;
     uint64_t all = 0;
     uint32_t all_n = 0;
-    for (int i = 0; i < kSliceThreads / 64; ++i) {
-      if (i < wave) before += scratch[0][i], before_n += counts[i];
-      all += scratch[0][i];
+    for (int i = 0; i < kSliceWaves; ++i) {
+      if (i < wave) before += scratch[i], before_n += counts[i];
+      all += scratch[i];
       all_n += counts[i];
     }
     const bool cut_k = r.k && (uint32_t)r.k < all_n;  // else top-k cuts nothing but weights of 0
@@ -261,14 +315,17 @@ __global__ __launch_bounds__(kSliceThreads) void collect_kernel(SampleArgs a, in
       // what top-p reaches for lies between these
       const double least = (double)r.p * reach[0], most = (double)r.p * reach[1] + 1.0;
       uint64_t at = before;
+      int begun = 0, ended = kBins - 1;
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
         const int b = threadIdx.x * kPer + i;
         // the last bin that begins before it for certain, the first that ends past it for certain
-        if (most_of(at, V) < least) atomicMax(&cuts[0], b);
+        if (most_of(at, V) < least) begun = b;
         at += mass[i];
-        if (least_of(at, V) >= most) atomicMin(&cuts[1], b);
+        if (least_of(at, V) >= most) ended = min(ended, b);
       }
+      for (int o = 32; o; o >>= 1) begun = max(begun, __shfl_xor(begun, o)), ended = min(ended, __shfl_xor(ended, o));
+      if (lane == 0) atomicMax(&cuts[0], begun), atomicMin(&cuts[1], ended);
       __syncthreads();
       high = min(cuts[1], rank_bin);
       low = min(cuts[0], high);
@@ -278,43 +335,57 @@ __global__ __launch_bounds__(kSliceThreads) void collect_kernel(SampleArgs a, in
   __syncthreads();
 
   const void *z = (const Z *)a.logits + (int64_t)blockIdx.y * a.stride;
-  const int lo = min(V, (int)blockIdx.x * len), hi = min(V, lo + len);
+  const int slice = blockIdx.x * kSliceWaves + wave, lo = min(V, slice * len);
   const Binning bin(r, shift);
-  const Weigh wt = r.weigh(shift);
+  const Weigh weigh = r.weigh(shift);
   const double least = r.least;
   const int last = min(rank_bin, kBins - 1);
-  uint64_t sums[3] = {0, 0, 0};
-  for_each<Z, kSliceThreads>(z, lo, hi, [&](float v, int i) {
+  uint64_t before_low = 0, kept_low = 0, between = 0;
+  // few elements of a row with a cut lie before it: they are queued, so that the 64-bit
+  // exponentials are taken by full waves
+  float *queue = queues[wave];
+  int queued = 0;
+  auto weigh_one = [&](float v) __attribute__((always_inline)) {
+    const Weigh::Weight x = weigh(v);
+    const bool early = bin.bin(bin.depth(v)) < low;
+    before_low += early ? x.parts : 0;
+    kept_low += early && !(x.w < least) ? x.parts : 0;
+    between += early ? 0 : x.parts;
+  };
+  for_each<Z>(z, lo, min(V, lo + len), [&](float v, int i) __attribute__((always_inline)) {
     const int b = bin.bin(bin.depth(v));
-    if (b > last) return;
-    if ((b >= low && b <= high) || b == rank_bin) {
+    const bool listed = (b >= low && b <= high) || b == rank_bin;
+    if (listed && b < kBins) {
       const int at = atomicAdd(&n_mine, 1);
-      if (at < kCandidates) mine[at] = code_of(rank_key(v), i);
-      return;
+      if (at < kOwn) {
+        mine[at] = code_of(rank_key(v), i);
+      } else {
+        const int far = atomicAdd(&w.n_list, 1);
+        if (far < kCandidates) w.list[far] = code_of(rank_key(v), i);
+      }
     }
-    const double x = wt.weight(v);
-    const uint64_t n = wt.parts(x);
-    if (b < low) {
-      sums[0] += n;
-      if (!(x < least)) sums[1] += n;
-    } else {
-      sums[2] += n;
+    const bool in = b <= last && !listed;
+    const uint64_t mask = __ballot(in);
+    if (in) queue[queued + __popcll(mask & ((1ull << lane) - 1))] = v;
+    queued += __popcll(mask);
+  }, [&]() __attribute__((always_inline)) {
+    __builtin_amdgcn_wave_barrier();
+    while (queued >= 128) {  // two at a time: one's arithmetic fills the other's waits
+      queued -= 128;
+      const float v0 = queue[queued + lane], v1 = queue[queued + 64 + lane];
+      weigh_one(v0);
+      weigh_one(v1);
     }
+    __builtin_amdgcn_wave_barrier();
   });
-#pragma unroll
-  for (int j = 0; j < 3; ++j) {
-    const uint64_t s = wave_sum(sums[j]);
-    if (lane == 0) scratch[j][wave] = s;
-  }
+  if (lane < queued) weigh_one(queue[lane]);
+  if (lane + 64 < queued) weigh_one(queue[lane + 64]);
+  before_low = wave_sum(before_low), kept_low = wave_sum(kept_low), between = wave_sum(between);
+  if (lane < 3) w.sums[slice][lane] = lane == 0 ? before_low : lane == 1 ? kept_low : between;
   __syncthreads();
-  if (threadIdx.x < 3) {
-    uint64_t s = 0;
-    for (int i = 0; i < kSliceThreads / 64; ++i) s += scratch[threadIdx.x][i];
-    w.sums[blockIdx.x][threadIdx.x] = s;
-  }
-  if (threadIdx.x == 0 && n_mine) place = atomicAdd(&w.n_list, n_mine);
+  if (threadIdx.x == 0 && n_mine) place = atomicAdd(&w.n_list, min(n_mine, kOwn));
   __syncthreads();
-  for (int i = threadIdx.x; i < min(n_mine, kCandidates); i += kSliceThreads)
+  for (int i = threadIdx.x; i < min(n_mine, kOwn); i += kSliceThreads)
     if (place + i < kCandidates) w.list[place + i] = mine[i];
 }
 
@@ -323,7 +394,7 @@ __global__ __launch_bounds__(kSliceThreads) void collect_kernel(SampleArgs a, in
 // or of weights), over elements up to the code `in`, first reaches `want` at the code returned; want is at least 1
 // and at most the total.
 template <class Z>
-__device__ uint64_t select_row(const void *z, int V, const Weigh &wt, uint64_t want, bool weighted, uint64_t in,
+__device__ uint64_t select_row(const void *z, int V, const Weigh &weigh, uint64_t want, bool weighted, uint64_t in,
                                uint64_t *hist, uint64_t *scratch, uint64_t *found) {
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   uint32_t key = 0;
@@ -335,7 +406,7 @@ __device__ uint64_t select_row(const void *z, int V, const Weigh &wt, uint64_t w
       const float x = logit<Z>(z, i);
       const uint32_t k = rank_key(x);
       if (code_of(k, i) > in || (bits < 24 && k >> (bits + 8) != key >> (bits + 8))) continue;
-      const uint64_t n = weighted ? wt.parts(wt.weight(x)) : 1;
+      const uint64_t n = weighted ? weigh(x).parts : 1;
       if (n) atomicAdd((unsigned long long *)&hist[k >> bits & 255], (unsigned long long)n);
     }
     __syncthreads();
@@ -352,7 +423,7 @@ __device__ uint64_t select_row(const void *z, int V, const Weigh &wt, uint64_t w
     __syncthreads();
   }
   // equal logits: the first `ties` of them by index
-  const uint64_t one = weighted ? wt.parts(wt.weight(unrank(key))) : 1;
+  const uint64_t one = weighted ? weigh(unrank(key)).parts : 1;
   const uint64_t ties = one ? (want - above + one - 1) / one : 1;
   uint64_t seen = 0;
   for (int base = 0; base < V; base += kThreads) {
@@ -385,14 +456,15 @@ __device__ __forceinline__ uint64_t reach_of(float p, uint64_t mass) {
 // Pass 4, a block per row: ranks the listed elements, which gives the cut, then finds the slice in
 // which the draw falls, and the element in it.
 template <class Z>
-__global__ __launch_bounds__(kThreads) void draw_kernel(SampleArgs a, int slices, int len, int shift) {
+__global__ __launch_bounds__(kThreads) void draw_kernel(SampleArgs a, int blocks, int len, int shift) {
   __shared__ uint64_t codes[kCandidates], parts[kCandidates];
   __shared__ uint64_t hist[256], scratch[kWaves], found[2], in_slice[kMaxSlices];
   __shared__ int n_early;
   const int row = blockIdx.x, V = a.vocab, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int slices = blocks * kSliceWaves;
   const RowWork &w = ((const RowWork *)a.work)[row];
   const void *z = (const Z *)a.logits + (int64_t)row * a.stride;
-  const Row r(a, row, row_best(w, slices));
+  const Row r(a, row, row_best(w, blocks));
   if (r.none || r.greedy) {
     if (threadIdx.x == 0) {
       a.token[row] = r.none ? -1 : r.first;
@@ -400,12 +472,12 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleArgs a, int slices
     }
     return;
   }
-  const Weigh wt = r.weigh(shift);
+  const Weigh weigh = r.weigh(shift);
   const double least = r.least;
   auto kept = [&](float v, int i, uint64_t cut) -> uint64_t {
     if (code_of(rank_key(v), i) > cut) return 0;
-    const double x = wt.weight(v);
-    return x < least ? 0 : wt.parts(x);
+    const Weigh::Weight x = weigh(v);
+    return x.w < least ? 0 : x.parts;
   };
   uint64_t cut = ~0ull;  // code of the last element that the filters by rank keep
   const int n = r.ranked() ? w.n_list : 0;
@@ -415,15 +487,18 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleArgs a, int slices
       in_slice[threadIdx.x] = real ? w.sums[threadIdx.x][1] : 0;
       const uint64_t ahead = wave_sum(real ? w.sums[threadIdx.x][0] : (uint64_t)0);
       const uint64_t between = wave_sum(real ? w.sums[threadIdx.x][2] : (uint64_t)0);
-      if (threadIdx.x == 0) scratch[0] = ahead, scratch[1] = between, found[0] = found[1] = 0, n_early = 0;
+      if (lane == 0) scratch[wave] = ahead, scratch[kMaxSlices / 64 + wave] = between;
+      if (threadIdx.x == 0) found[0] = found[1] = 0, n_early = 0;
     }
     for (int i = threadIdx.x; i < n; i += kThreads) {
       codes[i] = w.list[i];
-      parts[i] = wt.parts(wt.weight(unrank(~(uint32_t)(codes[i] >> 32))));
+      parts[i] = weigh(unrank(~(uint32_t)(codes[i] >> 32))).parts;
     }
     __syncthreads();
     if (n) {
-      const uint64_t ahead = scratch[0], between = scratch[1];
+      uint64_t ahead = 0, between = 0;
+#pragma unroll
+      for (int i = 0; i < kMaxSlices / 64; ++i) ahead += scratch[i], between += scratch[kMaxSlices / 64 + i];
       const int high = w.high, rank_bin = w.rank_bin;
       const Binning bin(r, shift);
       constexpr int kEach = kCandidates / kThreads;
@@ -477,12 +552,12 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleArgs a, int slices
       }
     }
   } else {
-    if (r.k) cut = select_row<Z>(z, V, wt, (uint64_t)r.k, false, cut, hist, scratch, found);
+    if (r.k) cut = select_row<Z>(z, V, weigh, (uint64_t)r.k, false, cut, hist, scratch, found);
     if (r.p < 1.f) {
       uint64_t mass = 0;
       for (int i = threadIdx.x; i < V; i += kThreads) {
         const float x = logit<Z>(z, i);
-        if (code_of(rank_key(x), i) <= cut) mass += wt.parts(wt.weight(x));
+        if (code_of(rank_key(x), i) <= cut) mass += weigh(x).parts;
       }
       mass = wave_sum(mass);
       if (lane == 0) scratch[wave] = mass;
@@ -490,7 +565,7 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleArgs a, int slices
       mass = 0;
       for (int i = 0; i < kWaves; ++i) mass += scratch[i];
       __syncthreads();
-      cut = select_row<Z>(z, V, wt, reach_of(r.p, mass), true, cut, hist, scratch, found);
+      cut = select_row<Z>(z, V, weigh, reach_of(r.p, mass), true, cut, hist, scratch, found);
     }
     for (int s = wave; s < kMaxSlices; s += kWaves) {
       const int lo = min(V, s * len), hi = s < slices ? min(V, lo + len) : lo;
@@ -503,7 +578,10 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleArgs a, int slices
   __syncthreads();
 
   // the draw, the slice it falls into, the wave's run of the slice, the element
-  uint64_t up = in_slice[lane];
+  constexpr int kPer = kMaxSlices / 64;
+  uint64_t up = 0;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) up += in_slice[lane * kPer + i];
   const uint64_t own = up;
   for (int o = 1; o < 64; o <<= 1) {
     const uint64_t v = __shfl_up((unsigned long long)up, o);
@@ -513,8 +591,10 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleArgs a, int slices
   const float u = a.u[row];
   const double want = (double)u * (double)mass;
   const uint64_t target = !(want > 0.0) ? 0 : want >= (double)mass ? mass - 1 : min(mass - 1, (uint64_t)want);
-  const int slice = max(0, __ffsll((unsigned long long)__ballot(target < up)) - 1);
-  uint64_t before = __shfl((unsigned long long)(up - own), slice);
+  const int at = max(0, __ffsll((unsigned long long)__ballot(target < up)) - 1);
+  uint64_t before = __shfl((unsigned long long)(up - own), at);
+  int slice = at * kPer;
+  for (int i = 1; i < kPer && target >= before + in_slice[slice]; ++i) before += in_slice[slice++];
   const int begin = min(V, slice * len), end = min(V, begin + len);
   const int run = (end - begin + kWaves - 1) / kWaves, lo = min(end, begin + wave * run), hi = min(end, lo + run);
   uint64_t mine = 0;
@@ -542,29 +622,28 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleArgs a, int slices
   }
 }
 
-// Slices of a row: about 1024 blocks over all rows, each with at least 1024 elements.
-void slices_of(int rows, int vocab, int *slices, int *len) {
-  int s = (1024 + rows - 1) / rows;
-  s = s > kMaxSlices ? kMaxSlices : s;
-  const int most = (vocab + 1023) / 1024;
-  s = s > most ? most : s;
-  *len = (vocab + s - 1) / s;
-  *slices = (vocab + *len - 1) / *len;
+// Blocks for a row's passes: about 1024 over all rows, each wave with at least 256 elements.
+void split_row(int rows, int vocab, int *blocks, int *len) {
+  int n = (1024 + rows - 1) / rows;
+  const int most = (vocab + 256 * kSliceWaves - 1) / (256 * kSliceWaves);
+  n = n > kMaxBlocks ? kMaxBlocks : n;
+  *blocks = n > most ? most : n;
+  *len = (vocab + *blocks * kSliceWaves - 1) / (*blocks * kSliceWaves);
 }
 
 template <class Z>
 hipError_t launch(const SampleArgs &a, hipStream_t s) {
-  int shift = 62, slices, len;
+  int shift = 50, blocks, len;
   while ((int64_t)1 << (62 - shift) < a.vocab) --shift;
-  slices_of(a.rows, a.vocab, &slices, &len);
-  void *args[] = {const_cast<SampleArgs *>(&a), &slices, &len, &shift};
-  const dim3 grid(slices, a.rows);
-  hipError_t e = hipLaunchKernel((const void *)largest_kernel<Z>, grid, dim3(kSliceThreads), args, 0, s);
+  split_row(a.rows, a.vocab, &blocks, &len);
+  const dim3 grid(blocks, a.rows);
+  void *first[] = {const_cast<SampleArgs *>(&a), &len}, *then[] = {const_cast<SampleArgs *>(&a), &len, &shift};
+  void *last[] = {const_cast<SampleArgs *>(&a), &blocks, &len, &shift};
+  hipError_t e = hipLaunchKernel((const void *)largest_kernel<Z>, grid, dim3(kSliceThreads), first, 0, s);
   if (e == hipSuccess && (a.top_k || a.top_p))
-    e = hipLaunchKernel((const void *)bins_kernel<Z>, grid, dim3(kSliceThreads), args, 0, s);
-  if (e == hipSuccess) e = hipLaunchKernel((const void *)collect_kernel<Z>, grid, dim3(kSliceThreads), args, 0, s);
-  if (e == hipSuccess)
-    e = hipLaunchKernel((const void *)draw_kernel<Z>, dim3(a.rows), dim3(kThreads), args, 0, s);
+    e = hipLaunchKernel((const void *)bins_kernel<Z>, grid, dim3(kSliceThreads), then, 0, s);
+  if (e == hipSuccess) e = hipLaunchKernel((const void *)collect_kernel<Z>, grid, dim3(kSliceThreads), then, 0, s);
+  if (e == hipSuccess) e = hipLaunchKernel((const void *)draw_kernel<Z>, dim3(a.rows), dim3(kThreads), last, 0, s);
   return e;
 }
 
