@@ -58,6 +58,7 @@ constexpr int kLanes = 64;
 constexpr int kThreads = 256, kWaves = kThreads / kLanes;
 constexpr int kIds = 1024;  // page ids of a unit held in LDS at a time
 constexpr float kNegInf = -__builtin_inff();
+constexpr float kSlack = 8.f;  // log2, of a row's base below its maximum
 
 // One sequence's share of the batch, read defensively: whatever starts and lengths hold, rows
 // stay within [0, n_tokens) and keys within the table.
@@ -84,9 +85,12 @@ __device__ __forceinline__ int span_of(const AttendArgs &a, const Seq &q) {
   const int64_t reach = (int64_t)a.window + (M - 1) / a.kv.group + 1 + 64;
   return (int)min((int64_t)q.length, reach);
 }
-// Units of a tile that spans `span` keys: the nearest whole number of C's (a tile of few more keys
-// than C is better left whole than split and joined), which it shares out evenly.
-__device__ __forceinline__ int units_of(int span, int C) { return max(1, (int)(((int64_t)span + C / 2) / C)); }
+// Units of a tile that spans `span` keys, which it shares out evenly.  Where the units are to run all at
+// once, span / C rounded down: one unit more than the card holds would double the time.  Where they
+// run in rounds, to the nearest whole number, which leaves their sizes closer to each other.
+__device__ __forceinline__ int units_of(const AttendArgs &a, int span, int C) {
+  return max(1, (int)(((int64_t)span + (a.nearest ? C / 2 : 0)) / C));
+}
 __device__ __forceinline__ int share_of(int keys, int units) { return ((keys + units - 1) / units + 63) & ~63; }
 
 // Keys of a unit, from the whole batch.  `mine` is sequence threadIdx.x % 64 where there is one.
@@ -118,7 +122,7 @@ __device__ __forceinline__ bool plan_find(const AttendArgs &a, const Seq &mine, 
   for (int s0 = 0; s0 < a.kv.n_seqs; s0 += kLanes) {
     Seq q = mine;
     if (s0) q = s0 + lane < a.kv.n_seqs ? seq_of(a.kv, s0 + lane) : Seq{0, 0, 0, false};
-    const int per = units_of(span_of<M>(a, q), C);
+    const int per = units_of(a, span_of<M>(a, q), C);
     // (no batch has 2^24 units: only starts out of order could add up to more)
     const int n = (int)min((int64_t)1 << 24, (int64_t)tiles_of<M>(a, q) * per), m = per > 1 ? n : 0;
     const int t = per > 1 ? n / per : 0;
@@ -166,7 +170,7 @@ __device__ __forceinline__ Range range_of(const AttendArgs &a, const Seq &q, int
 template <int D>
 struct Rows {
   f32x16 acc[D / 32];  // o^T: d = 32 i + 8 (r / 4) + 4 half + r % 4
-  float m, l;          // running maximum (log2 units, both halves alike), this lane's share of the sum
+  float m, l;          // base of the exponentials (log2 units, both halves alike), this lane's share of the sum
 };
 
 // Key (within its 32) of accumulator r of a score product, for this lane's half.
@@ -185,8 +189,8 @@ __device__ __forceinline__ void mask_scores(f32x16 (&s)[N], int t0, int pos, int
     }
 }
 
-// Scores to probabilities over 32 * N keys: takes the new maximum, rescales the rows only where
-// some row's maximum rose, and packs the B operands of the second product.
+// Scores to probabilities over 32 * N keys: takes the new maximum, rescales the rows where some
+// row's maximum rose, and packs the B operands of the second product.
 // Probabilities are rounded to the cache's type, the type the matrix cores multiply; the sum
 // is taken in fp32 before that.
 template <class E, int D, int N>
@@ -197,10 +201,11 @@ __device__ __forceinline__ void softmax_step(f32x16 (&s)[N], Rows<D> &st, u32x4 
 #pragma unroll
     for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[n][r]);
   mx = fmaxf(mx, __shfl_xor(mx, 32));
-  const float top = fmaxf(st.m, mx * scale);
-  const float base = top == kNegInf ? 0.f : top;
-  if (__any(top > st.m)) {
-    const float shrink = __builtin_amdgcn_exp2f(st.m - base);
+  mx *= scale;
+  // the base follows the maximum only when that has risen by 2^8: until then probabilities are
+  // up to 256 instead of 1, which changes no relative rounding (and stays far from fp16's 65504)
+  if (__any(mx > st.m + kSlack)) {
+    const float top = fmaxf(st.m, mx), shrink = __builtin_amdgcn_exp2f(st.m - (top == kNegInf ? 0.f : top));
     st.l *= shrink;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
@@ -208,6 +213,7 @@ __device__ __forceinline__ void softmax_step(f32x16 (&s)[N], Rows<D> &st, u32x4 
       for (int r = 0; r < 16; ++r) st.acc[i][r] *= shrink;
     st.m = top;
   }
+  const float base = st.m == kNegInf ? 0.f : st.m;
   typedef typename Vec<E>::x8 x8;
 #pragma unroll
   for (int n = 0; n < N; ++n)
@@ -231,75 +237,48 @@ __device__ __forceinline__ u32x4 keep_first(u32x4 v, int n) {
   return v;
 }
 
-// Values that are not finite, as numbers whose sums over 16 keys tell which kinds were among
-// them: +inf 1, -inf 128, NaN 16384, 0 for a finite value; all exact in the type E.
-template <class E>
-struct Odd;
-template <>
-struct Odd<__bf16> {
-  static constexpr uint32_t exponent = 0x7f80, one = 0x3f80, inf = 0x3f80, minus = 0x4300, nan = 0x4680;
-};
-template <>
-struct Odd<_Float16> {
-  static constexpr uint32_t exponent = 0x7c00, one = 0x3c00, inf = 0x3c00, minus = 0x5800, nan = 0x7400;
-};
-template <class E>
-__device__ __forceinline__ bool any_odd(u32x4 v) {
-  constexpr uint32_t x = Odd<E>::exponent;
-  bool odd = false;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) odd |= (v[i] & x) == x || (v[i] >> 16 & x) == x;
-  return odd;
-}
-template <class E>
-__device__ __forceinline__ uint32_t odd_code(uint32_t e) {  // of one element's bits
-  constexpr uint32_t x = Odd<E>::exponent;
-  return (e & x) != x ? 0u : (e & 0x7fffu) != x ? Odd<E>::nan : e & 0x8000u ? Odd<E>::minus : Odd<E>::inf;
-}
-
-// Makes the values of 16 keys from t0 on fit for the second product in a step some of whose keys
-// some rows do not see.  Keys at or past `end` hold whatever the page held: their values are
-// cleared.  A value that is not finite must not reach rows that do not see its key (0 * inf is a
-// NaN), so such values are cleared too, and a product of their kinds with which row sees which key
-// says which rows they do reach (their weight there is positive: an infinity stays the infinity
-// it was).
+// Of a step some of whose keys some rows do not see, the values of 16 keys from t0 on.  Keys at or past
+// `end` hold whatever the page held: their values are cleared.  A value that is not finite must not
+// reach rows that do not see its key (0 * inf is a NaN): it is cleared too, and reported, for
+// add_odd to give it to the rows that do see it.
 template <class E, int D>
-__device__ __forceinline__ void clean_values(u32x4 (&v)[D / 32], Rows<D> &st, int t0, int end, int pos, int floor) {
-  const int half = threadIdx.x % kLanes / 32, t = t0 + 8 * half;
+__device__ __forceinline__ bool clean_values(u32x4 (&v)[D / 32], int t0, int end) {
+  constexpr uint32_t lo = __is_same(E, __bf16) ? 0x7f80u : 0x7c00u, hi = lo << 16;
+  const int n = min(8, max(0, end - (t0 + 8 * (int)(threadIdx.x % kLanes / 32))));
   bool odd = false;
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) {
-    v[i] = keep_first(v[i], min(8, max(0, end - t)));
-    odd |= any_odd<E>(v[i]);
-  }
-  if (__any(odd)) {
-    u32x4 sees;
+    v[i] = keep_first(v[i], n);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int t2 = t + 2 * j;
-      sees[j] = (t2 <= pos && t2 > floor ? Odd<E>::one : 0u) |
-                (t2 + 1 <= pos && t2 + 1 > floor ? Odd<E>::one << 16 : 0u);
+      const bool a = (v[i][j] & lo) == lo, b = (v[i][j] & hi) == hi;
+      odd |= a || b;
+      v[i][j] &= (a ? 0u : 0xffffu) | (b ? 0u : 0xffff0000u);
     }
+  }
+  return __any(odd);
+}
+
+// Adds the values of keys t0 .. t1 - 1 that are not finite to the rows that see them (their weight
+// there is positive: an infinity stays the infinity it was).  Rare, and slow: element by element.
+template <class E, int D>
+__device__ __forceinline__ void add_odd(Rows<D> &st, const uint16_t *values, const int *ids, int pg0, int shift,
+                                        int64_t page_elems, int t0, int t1, int pos, int floor) {
+  constexpr uint32_t exponent = __is_same(E, __bf16) ? 0x7f80u : 0x7c00u;
+  const int half = threadIdx.x % kLanes / 32;
+#pragma unroll 1
+  for (int t = t0; t < t1; ++t) {
+    const uint16_t *src =
+        values + ids[(t >> shift) - pg0] * page_elems + ((t & ((1 << shift) - 1)) >> 3) * 8 * D + (t & 7);
+    const bool sees = t <= pos && t > floor;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
-      u32x4 code;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t lo = odd_code<E>(v[i][j] & 0xffffu), hi = odd_code<E>(v[i][j] >> 16);
-        code[j] = lo | hi << 16;
-        v[i][j] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
-      }
-      const f32x16 kinds = mma(code, sees, f32x16{}, E());
-      __builtin_amdgcn_sched_barrier(0);  // one product's registers at a time
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const int k = (int)kinds[r];
-        const bool nan = k >= 16384, minus = k & 0x3f80, plus = k & 0x7f;
-        st.acc[i][r] += nan || (minus && plus) ? __builtin_nanf("")
-                        : minus                ? kNegInf
-                        : plus                 ? __builtin_inff()
-                                               : 0.f;
+        const uint16_t e = src[(32 * i + 8 * (r / 4) + 4 * half + r % 4) * 8];
+        st.acc[i][r] += sees && (e & exponent) == exponent ? (float)__builtin_bit_cast(E, e) : 0.f;
       }
+      __builtin_amdgcn_sched_barrier(0);  // 16 values' registers at a time
     }
   }
 }
@@ -389,13 +368,13 @@ __device__ __forceinline__ bool unit_of(const AttendArgs &a, Unit *u) {
     // the grid's last unit lies past the batch's last one, or is it
     int64_t count = pl.tiles;
     if (found) {
-      const int per = units_of(span_of<M>(a, pl.q), C);
+      const int per = units_of(a, span_of<M>(a, pl.q), C);
       if (per > 1) count += tiles_of<M>(a, pl.q);
     }
     split_tiles(a)->count = (int)min((int64_t)a.max_tiles, count);
   }
   if (!found) return false;
-  const int per = units_of(span_of<M>(a, pl.q), C);
+  const int per = units_of(a, span_of<M>(a, pl.q), C);
   // the tiles with the most keys first
   const int order = pl.index / per, split = pl.index % per;
   u->seq = pl.seq;
@@ -409,7 +388,7 @@ __device__ __forceinline__ bool unit_of(const AttendArgs &a, Unit *u) {
   u->slot = real > 1 ? pl.slots + pl.index : -1;
   if (per > 1) {
     // starts out of order can ask for more than there are
-    if (pl.slots + pl.index + per > a.max_slots || pl.tiles + order >= a.max_tiles) return false;
+    if (pl.slots + (int64_t)(order + 1) * per > a.max_slots || pl.tiles + order >= a.max_tiles) return false;
     if (split == 0 && u->kvh == 0 && threadIdx.x == 0)
       split_tiles(a)->tile[pl.tiles + order] =
           SplitTile{(int)(pl.slots + pl.index), real, pl.q.first, u->tile * M,
@@ -458,6 +437,12 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_few_kernel(A
   const int first = before + u.tile * M / kv.group, last = before + (min(u.tile * M + M, rows) - 1) / kv.group;
   u32x4 q[D / 16];
   load_q<D>(a, u.q, u.kvh, row, q);
+  // heads of 256: the queries stay in LDS, where the joining of the waves has its place later
+  constexpr bool kQInLds = D > 128;
+  u32x4 *q_lds = (u32x4 *)&sums[0][0][0][0];
+  if (kQInLds && wave == 0)
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) q_lds[c * kLanes + lane] = q[c];
 
   Rows<D> st;
 #pragma unroll
@@ -501,21 +486,23 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_few_kernel(A
       const int next = t0 + 32 * kWaves;
       f32x16 s[1] = {};
 #pragma unroll
-      for (int c = 0; c < D / 16; ++c) s[0] = mma(k[c], q[c], s[0], E());
+      for (int c = 0; c < D / 16; ++c) s[0] = mma(k[c], kQInLds ? q_lds[c * kLanes + lane] : q[c], s[0], E());
       if (next < end) load_k(next);
       // whether some row does not see some key of the step
       const bool edge = t0 + 31 > first || (a.window && t0 <= last - a.window);
-      if (edge) mask_scores<1>(s, t0, pos, floor);
       u32x4 p[2];
+      if (edge) mask_scores<1>(s, t0, pos, floor);
       softmax_step<E, D, 1>(s, st, p, a.scale_log2);
+      bool odd = false;
       if (edge) {
 #pragma unroll
-        for (int c = 0; c < 2; ++c) clean_values<E, D>(v[c], st, t0 + 16 * c, u.q.length, pos, floor);
+        for (int c = 0; c < 2; ++c) odd |= clean_values<E, D>(v[c], t0 + 16 * c, u.q.length);
       }
 #pragma unroll
       for (int c = 0; c < 2; ++c)
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) st.acc[i] = mma(v[c][i], p[c], st.acc[i], E());
+      if (odd) add_odd<E, D>(st, values, ids, pg0, shift, page_elems, t0, min(t0 + 32, end), pos, floor);
       if (next < end) load_v(next);
     }
   }
@@ -523,7 +510,7 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_few_kernel(A
   // join the four waves
   st.l += __shfl_xor(st.l, 32);
   if (half == 0) stat[wave][n][0] = st.m, stat[wave][n][1] = st.l;
-  __syncthreads();
+  __syncthreads();  // and the queries have been read
   float top = kNegInf;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) top = fmaxf(top, stat[w][n][0]);
@@ -641,17 +628,29 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_many_kernel(
         for (int j = 0; j < 2; ++j)
           s[j] = mma(*(const u32x4 *)(kt + j * 64 * D + c * 512 + koff), q[c], s[j], E());
       const bool edge = t0 + KT - 1 > first || (a.window && t0 <= last - a.window);
-      if (edge) mask_scores<2>(s, t0, pos, floor);
       u32x4 p[4];
-      softmax_step<E, D, 2>(s, st, p, a.scale_log2);
+      if (!edge) {
+        softmax_step<E, D, 2>(s, st, p, a.scale_log2);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        u32x4 v[D / 32];
+        for (int c = 0; c < 4; ++c)
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) v[i] = *(const u32x4 *)(vt + c * 32 * D + i * 512 + voff);
-        if (edge) clean_values<E, D>(v, st, t0 + 16 * c, u.q.length, pos, floor);
+          for (int i = 0; i < D / 32; ++i)
+            st.acc[i] = mma(*(const u32x4 *)(vt + c * 32 * D + i * 512 + voff), p[c], st.acc[i], E());
+      } else {
+        mask_scores<2>(s, t0, pos, floor);
+        softmax_step<E, D, 2>(s, st, p, a.scale_log2);
+        bool odd = false;
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) st.acc[i] = mma(v[i], p[c], st.acc[i], E());
+        for (int c = 0; c < 4; ++c) {
+          u32x4 v[D / 32];
+#pragma unroll
+          for (int i = 0; i < D / 32; ++i) v[i] = *(const u32x4 *)(vt + c * 32 * D + i * 512 + voff);
+          odd |= clean_values<E, D>(v, t0 + 16 * c, u.q.length);
+#pragma unroll
+          for (int i = 0; i < D / 32; ++i) st.acc[i] = mma(v[i], p[c], st.acc[i], E());
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (odd) add_odd<E, D>(st, values, ids, pg0, shift, page_elems, t0, min(t0 + KT, end), pos, floor);
       }
     }
   }
@@ -679,12 +678,10 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_many_kernel(
 }
 
 // ---------------------------------------------------------------------------------------------
-// Joins the units of split tiles: a block per tile, KV head and eighth of the tile's rows (every
-// eighth row, so that the few rows of a decode step get a block each).  The block's groups of D / 4
+// Joins the units of split tiles: gridDim.y blocks per tile and KV head take every gridDim.y-th of the
+// tile's rows each (so that the few rows of a decode step get a block each).  The block's groups of D / 4
 // lanes share out a row's units, or several rows' where there are fewer units than groups.
 // ---------------------------------------------------------------------------------------------
-constexpr int kJoinRows = 8;
-
 template <class E, int D, int M>
 __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
   constexpr int kPer = D / 4, kGroups = kThreads / kPer;
@@ -703,8 +700,8 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
   while (per < kGroups && per < t.units) per *= 2;
   const int own = g / per, at_once = kGroups / per;
   const int64_t step = (int64_t)a.kv.kv_heads * M;  // rows from unit to unit
-  for (int r0 = 0; blockIdx.y + kJoinRows * r0 < t.rows; r0 += at_once) {
-    const int row = blockIdx.y + kJoinRows * (r0 + own);
+  for (int r0 = 0; (int)(blockIdx.y + gridDim.y * r0) < t.rows; r0 += at_once) {
+    const int row = blockIdx.y + gridDim.y * (r0 + own);
     float m = kNegInf, l = 0.f;
     f32x4 o{};
     if (row < t.rows) {
@@ -754,8 +751,11 @@ hipError_t launch_kernels(const AttendArgs &a, hipStream_t s) {
   const void *fn = M == kFewRows ? (const void *)attend_few_kernel<E, D> : (const void *)attend_many_kernel<E, D>;
   hipError_t e = hipLaunchKernel(fn, grid, dim3(kThreads), args, 0, s);
   if (e != hipSuccess) return e;
-  return hipLaunchKernel((const void *)attend_join_kernel<E, D, M>, dim3(a.max_tiles * a.kv.kv_heads, kJoinRows),
-                         dim3(kThreads), args, 0, s);
+  // most blocks have nothing to join: about 4096 in all, 8 to M / 4 of them to a tile
+  const int tiles = a.max_tiles * a.kv.kv_heads;
+  int y = 8;
+  while (2 * y <= M / 4 && 2 * y * tiles <= 4096) y *= 2;
+  return hipLaunchKernel((const void *)attend_join_kernel<E, D, M>, dim3(tiles, y), dim3(kThreads), args, 0, s);
 }
 
 }  // namespace

@@ -1,6 +1,7 @@
 // C entries of the serving operators (include/moecache.h): argument checks, launch shapes.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -55,9 +56,11 @@ bool aligned(const void *p) { return (uintptr_t)p % 16 == 0; }
 // A grid holds less than 2^32 threads: at most 2^24 blocks of 256 per call.
 constexpr int64_t kMaxRows = 1 << 27, kMaxTokens = 1 << 24, kMaxSeqHeads = 1 << 22;
 constexpr int kMaxSampleRows = 65535;  // rows are a grid's second dimension
-// The grid of an attention call aims at this many units; partial results are kept for twice as many.
-constexpr int kFewTarget = 1024, kFewMinKeys = 256;
-constexpr int kManyTarget = 512, kManyMinKeys = 512;
+// Attention units aimed at: what the card holds at once (256 CUs of two blocks; few rows with heads of
+// 256: of one), or in decode twice that where there are that many tiles already, so that a long and a
+// short sequence's units even out.  Keys below which a tile isn't split.
+constexpr int kResident = 512;
+constexpr int kFewMinKeys = 256, kManyMinKeys = 512;
 
 int check_kv(const moe_kv_batch *b, const char *who, KvView *kv) {
   if (!b) return fail(MOE_EINVAL, "%s: the batch is NULL", who);
@@ -100,16 +103,20 @@ bool many_rows(const KvView &kv) { return (int64_t)kv.n_tokens * kv.group > (int
 void plan(AttendArgs *a, bool *many, uint64_t *bytes, int dim) {
   const KvView &kv = a->kv;
   *many = many_rows(kv);
-  const int rows = *many ? kManyRows : kFewRows;
-  a->target = *many ? kManyTarget : kFewTarget;
-  a->min_keys = *many ? kManyMinKeys : kFewMinKeys;
-  // units: target / kv_heads of full size and one remainder per tile; a sequence's tiles number
-  // ceil(rows / M), all sequences' together at most all rows / M + n_seqs
+  const int rows = *many ? kManyRows : kFewRows, resident = dim > 128 && !*many ? kResident / 2 : kResident;
+  // a sequence's tiles number ceil(rows / M), all sequences' together at most all rows / M + n_seqs
   const int64_t tiles = (int64_t)kv.n_tokens * kv.group / rows + kv.n_seqs;
+  a->target = !*many && 2 * tiles * kv.kv_heads >= resident ? 2 * resident : resident;
+  a->min_keys = *many ? kManyMinKeys : kFewMinKeys;
+  // units: a tile's keys / C, to the nearest whole number; with C >= all tiles' keys / (target /
+  // kv_heads) that is at most target / kv_heads in all, and one more per tile; nor can a tile
+  // have more than its table's keys give.  A split tile's units, x + 1/2 at x >= 3/2, are fewer than 2 x.
   const int64_t share = a->target / kv.kv_heads + 1;
-  a->max_units = (int)(share + tiles);
-  a->max_slots = (int)(2 * share);  // a split tile's ceil(x) units, x > 1, are fewer than 2 x
-  a->max_tiles = (int)share;        // and at least two
+  const int64_t most = (((int64_t)kv.max_pages << kv.page_shift) + a->min_keys / 2) / a->min_keys + 1;
+  a->max_units = (int)std::min(share + tiles, tiles * most);
+  a->max_slots = (int)std::min(2 * share, tiles * most);
+  a->max_tiles = (int)std::min(share, tiles);
+  a->nearest = a->target > resident;
   *bytes = attend_work_bytes(*a, rows, dim);
 }
 

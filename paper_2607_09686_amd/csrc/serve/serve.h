@@ -43,6 +43,7 @@ struct AttendArgs {
   int max_units;       // grid units per KV head
   int max_slots;       // partial-result slots per KV head
   int max_tiles;       // split tiles
+  bool nearest;        // how a tile's units are rounded, see units_of
   void *work;          // attend_work_bytes
 };
 
