@@ -410,16 +410,17 @@ __device__ __forceinline__ void refuse(const AttendArgs &a, const Unit &u) {
 __device__ __forceinline__ float finish(float l) { return l == 0.f ? 0.f : 1.f / l; }
 
 // ---------------------------------------------------------------------------------------------
-// Few rows per sequence: decode and verification windows.  Bound by the bytes of the cache.  The
-// four waves of a block take the unit's 32-key steps in turn, each with all 32 rows, straight
-// from memory into the operand registers (every byte is used by one wave only, so LDS would only
-// add a copy); a step's keys are requested while the step before is multiplied.
+// Few rows per sequence: decode and verification windows.  Bound by the bytes of the cache.  A
+// block's waves take 32 rows each: of a tile of 32 all four the same ones, in turns at the unit's
+// steps of 32 keys, of a tile of 64 two and two (the second pair finds the step's keys in the CU's
+// cache).  Keys go straight from memory into the operand registers (LDS would only add a copy); a
+// step's are requested while the step before is multiplied.
 // ---------------------------------------------------------------------------------------------
-template <class E, int D>
+template <class E, int D, int R>
 __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_few_kernel(AttendArgs a) {
-  constexpr int M = kFewRows;
+  constexpr int M = 32 * R, kTurns = kWaves / R;  // waves that take turns at the steps of the same rows
   __shared__ __align__(16) float sums[kWaves][D / 32 * 4][kLanes][4];
-  __shared__ float stat[kWaves][M][2];
+  __shared__ float stat[kWaves][32][2];
   __shared__ int ids[kIds];
   __shared__ int bad;
   Unit u;
@@ -431,7 +432,9 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_few_kernel(A
   const KvView &kv = a.kv;
   const int lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes, half = lane / 32, n = lane % 32;
   if (threadIdx.x == 0) bad = 0;
-  const int rows = u.q.count * kv.group, row = u.tile * M + n, before = u.q.length - u.q.count;
+  const int part = wave % R, turn = wave / R;
+  const int rows = u.q.count * kv.group, before = u.q.length - u.q.count;
+  const int trow = 32 * part + n, row = u.tile * M + trow;
   const int pos = row < rows ? before + row / kv.group : -1;
   const int floor = a.window ? pos - a.window : -1;
   const int first = before + u.tile * M / kv.group, last = before + (min(u.tile * M + M, rows) - 1) / kv.group;
@@ -439,8 +442,8 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_few_kernel(A
   load_q<D>(a, u.q, u.kvh, row, q);
   // heads of 256: the queries stay in LDS, where the joining of the waves has its place later
   constexpr bool kQInLds = D > 128;
-  u32x4 *q_lds = (u32x4 *)&sums[0][0][0][0];
-  if (kQInLds && wave == 0)
+  u32x4 *q_lds = (u32x4 *)&sums[0][0][0][0] + part * (D / 16) * kLanes;
+  if (kQInLds && turn == 0)
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) q_lds[c * kLanes + lane] = q[c];
 
@@ -480,10 +483,10 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_few_kernel(A
         for (int i = 0; i < D / 32; ++i) v[c][i] = *(const u32x4 *)(src + 32 * i * 8);
       }
     };
-    int t0 = begin + 32 * wave;
+    int t0 = begin + 32 * turn;
     if (t0 < end) load_k(t0), load_v(t0);
-    for (; t0 < end; t0 += 32 * kWaves) {
-      const int next = t0 + 32 * kWaves;
+    for (; t0 < end; t0 += 32 * kTurns) {
+      const int next = t0 + 32 * kTurns;
       f32x16 s[1] = {};
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) s[0] = mma(k[c], kQInLds ? q_lds[c * kLanes + lane] : q[c], s[0], E());
@@ -507,13 +510,13 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_few_kernel(A
     }
   }
 
-  // join the four waves
+  // join the waves that share rows
   st.l += __shfl_xor(st.l, 32);
   if (half == 0) stat[wave][n][0] = st.m, stat[wave][n][1] = st.l;
   __syncthreads();  // and the queries have been read
   float top = kNegInf;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, stat[w][n][0]);
+  for (int w = 0; w < kTurns; ++w) top = fmaxf(top, stat[w * R + part][n][0]);
   const float base = top == kNegInf ? 0.f : top, mine = __builtin_amdgcn_exp2f(st.m - base);
 #pragma unroll
   for (int i = 0; i < D / 32; ++i)
@@ -523,23 +526,22 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_few_kernel(A
                                                     st.acc[i][4 * g + 2] * mine, st.acc[i][4 * g + 3] * mine};
   float l = 0.f;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) l += stat[w][n][1] * __builtin_amdgcn_exp2f(stat[w][n][0] - base);
+  for (int w = 0; w < kTurns; ++w) l += stat[w * R + part][n][1] * __builtin_amdgcn_exp2f(stat[w * R + part][n][0] - base);
   __syncthreads();
   if (bad) l = __builtin_nanf("");
   if (row >= rows) return;
-  if (u.slot >= 0 && threadIdx.x < 32) {
-    float *ml = part_ml<D, M>(a, u.slot, u.kvh, n);
+  if (u.slot >= 0 && turn == 0 && half == 0) {
+    float *ml = part_ml<D, M>(a, u.slot, u.kvh, trow);
     ml[0] = top, ml[1] = l;
   }
   const float inv = finish(l);
-#pragma unroll
-  for (int i = wave; i < D / 8; i += kWaves) {
+  for (int i = turn; i < D / 8; i += kTurns) {
     f32x4 o{};
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) o += *(const f32x4 *)sums[w][i][lane];
+    for (int w = 0; w < kTurns; ++w) o += *(const f32x4 *)sums[w * R + part][i][lane];
     const int d = 32 * (i / 4) + 8 * (i % 4) + 4 * half;
     if (u.slot >= 0)
-      *(f32x4 *)(part_o<D, M>(a, u.slot, u.kvh, n) + d) = o;
+      *(f32x4 *)(part_o<D, M>(a, u.slot, u.kvh, trow) + d) = o;
     else
       store_out<E, D>(a, u.q, u.kvh, row, d, o * inv);
   }
@@ -555,7 +557,7 @@ typedef const __attribute__((address_space(1))) void global_void;
 
 template <class E, int D>
 __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_many_kernel(AttendArgs a) {
-  constexpr int M = kManyRows, KT = 64;
+  constexpr int M = 128, KT = 64;
   constexpr int kTileBytes = KT * D * 2;
   __shared__ __align__(16) uint8_t lds[4 * kTileBytes];  // [2][K tile, V tile], each four groups
   __shared__ int ids[kIds];
@@ -748,7 +750,11 @@ template <class E, int D, int M>
 hipError_t launch_kernels(const AttendArgs &a, hipStream_t s) {
   void *args[] = {const_cast<AttendArgs *>(&a)};
   const dim3 grid((unsigned)((int64_t)a.max_units * a.kv.kv_heads));
-  const void *fn = M == kFewRows ? (const void *)attend_few_kernel<E, D> : (const void *)attend_many_kernel<E, D>;
+  const void *fn;
+  if constexpr (M == 128)
+    fn = (const void *)attend_many_kernel<E, D>;
+  else
+    fn = (const void *)attend_few_kernel<E, D, M / 32>;
   hipError_t e = hipLaunchKernel(fn, grid, dim3(kThreads), args, 0, s);
   if (e != hipSuccess) return e;
   // most blocks have nothing to join: about 4096 in all, 8 to M / 4 of them to a tile
@@ -761,10 +767,10 @@ hipError_t launch_kernels(const AttendArgs &a, hipStream_t s) {
 }  // namespace
 
 template <int D>
-hipError_t launch_attend(const AttendArgs &a, bool half, bool many, hipStream_t s) {
-  if (half)
-    return many ? launch_kernels<_Float16, D, kManyRows>(a, s) : launch_kernels<_Float16, D, kFewRows>(a, s);
-  return many ? launch_kernels<__bf16, D, kManyRows>(a, s) : launch_kernels<__bf16, D, kFewRows>(a, s);
+hipError_t launch_attend(const AttendArgs &a, bool half, int rows, hipStream_t s) {
+  if (rows == 64) return half ? launch_kernels<_Float16, D, 64>(a, s) : launch_kernels<__bf16, D, 64>(a, s);
+  if (rows == 32) return half ? launch_kernels<_Float16, D, 32>(a, s) : launch_kernels<__bf16, D, 32>(a, s);
+  return half ? launch_kernels<_Float16, D, 128>(a, s) : launch_kernels<__bf16, D, 128>(a, s);
 }
 
 }  // namespace moecache

@@ -2,5 +2,5 @@
 #include "attend.h"
 
 namespace moecache {
-template hipError_t launch_attend<256>(const AttendArgs &, bool, bool, hipStream_t);
+template hipError_t launch_attend<256>(const AttendArgs &, bool, int, hipStream_t);
 }  // namespace moecache

@@ -57,8 +57,8 @@ bool aligned(const void *p) { return (uintptr_t)p % 16 == 0; }
 constexpr int64_t kMaxRows = 1 << 27, kMaxTokens = 1 << 24, kMaxSeqHeads = 1 << 22;
 constexpr int kMaxSampleRows = 65535;  // rows are a grid's second dimension
 // Attention units aimed at: what the card holds at once (256 CUs of two blocks; few rows with heads of
-// 256: of one), or in decode twice that where there are that many tiles already, so that a long and a
-// short sequence's units even out.  Keys below which a tile isn't split.
+// 256: of one), or with few rows twice that where half as many tiles are there already, so that a
+// long and a short sequence's units even out.  Keys below which a tile isn't split.
 constexpr int kResident = 512;
 constexpr int kFewMinKeys = 256, kManyMinKeys = 512;
 
@@ -95,19 +95,25 @@ bool rows_ok(const void *p, int64_t stride, int heads, int dim, int size) {
   return p && aligned(p) && stride >= (int64_t)heads * dim && stride * size % 16 == 0 && stride <= (int64_t)1 << 32;
 }
 
-// Which attention kernel a batch takes.  Tokens per sequence are known on the device only, so the
-// rule goes by their mean.  A tile of many rows reads the keys once for four times the rows, but
-// its waves share the tile's steps: with few rows most of them have nothing to multiply.
-bool many_rows(const KvView &kv) { return (int64_t)kv.n_tokens * kv.group > (int64_t)64 * kv.n_seqs; }
+// Rows (new tokens times the query heads of a KV head) of an attention tile.  New tokens per sequence
+// are known on the device only, so the rule goes by their mean.  Tiles of 32 and 64 rows read the
+// cache at full rate, once for every tile of a sequence.  In a tile of 128 the waves share the keys
+// through LDS and split the rows, and those without rows have nothing to do.
+int tile_rows(const KvView &kv) {
+  const int64_t rows = (int64_t)kv.n_tokens * kv.group;
+  return rows <= (int64_t)32 * kv.n_seqs ? 32 : rows <= (int64_t)64 * kv.n_seqs ? 64 : 128;
+}
 
-void plan(AttendArgs *a, bool *many, uint64_t *bytes, int dim) {
+int plan(AttendArgs *a, uint64_t *bytes, int dim) {
   const KvView &kv = a->kv;
-  *many = many_rows(kv);
-  const int rows = *many ? kManyRows : kFewRows, resident = dim > 128 && !*many ? kResident / 2 : kResident;
+  const int rows = tile_rows(kv);
+  const bool few = rows < 128;
+  const int resident = few && dim > 128 ? kResident / 2 : kResident;
   // a sequence's tiles number ceil(rows / M), all sequences' together at most all rows / M + n_seqs
   const int64_t tiles = (int64_t)kv.n_tokens * kv.group / rows + kv.n_seqs;
-  a->target = !*many && 2 * tiles * kv.kv_heads >= resident ? 2 * resident : resident;
-  a->min_keys = *many ? kManyMinKeys : kFewMinKeys;
+  a->target = few && 2 * tiles * kv.kv_heads >= resident ? 2 * resident : resident;
+  a->nearest = few && 4 * tiles * kv.kv_heads >= resident;
+  a->min_keys = few ? kFewMinKeys : kManyMinKeys;
   // units: a tile's keys / C, to the nearest whole number; with C >= all tiles' keys / (target /
   // kv_heads) that is at most target / kv_heads in all, and one more per tile; nor can a tile
   // have more than its table's keys give.  A split tile's units, x + 1/2 at x >= 3/2, are fewer than 2 x.
@@ -116,8 +122,8 @@ void plan(AttendArgs *a, bool *many, uint64_t *bytes, int dim) {
   a->max_units = (int)std::min(share + tiles, tiles * most);
   a->max_slots = (int)std::min(2 * share, tiles * most);
   a->max_tiles = (int)std::min(share, tiles);
-  a->nearest = a->target > resident;
   *bytes = attend_work_bytes(*a, rows, dim);
+  return rows;
 }
 
 }  // namespace
@@ -162,8 +168,7 @@ int moe_kv_attend_workspace(const moe_kv_batch *b, uint64_t *bytes) {
   if (!bytes) return fail(MOE_EINVAL, "moe_kv_attend_workspace: bytes is NULL");
   const int rc = check_kv(b, "moe_kv_attend_workspace", &a.kv);
   if (rc) return rc;
-  bool many;
-  plan(&a, &many, bytes, b->head_dim);
+  plan(&a, bytes, b->head_dim);
   return MOE_OK;
 }
 
@@ -177,9 +182,8 @@ int moe_kv_attend(const moe_kv_batch *b, int32_t window, float scale, const void
   if (b->n_tokens == 0 || b->n_seqs == 0) return MOE_OK;
   if (!rows_ok(q, q_stride, b->n_heads, b->head_dim, 2) || !rows_ok(out, out_stride, b->n_heads, b->head_dim, 2))
     return fail(MOE_EINVAL, "moe_kv_attend: q and out must be 16-byte aligned rows of n_heads * head_dim elements");
-  bool many;
   uint64_t bytes;
-  plan(&a, &many, &bytes, b->head_dim);
+  const int rows = plan(&a, &bytes, b->head_dim);
   if (!workspace || !aligned(workspace) || workspace_bytes < bytes)
     return fail(MOE_EINVAL, "moe_kv_attend: the workspace must be 16-byte aligned and of at least %llu bytes",
                 (unsigned long long)bytes);
@@ -192,9 +196,9 @@ int moe_kv_attend(const moe_kv_batch *b, int32_t window, float scale, const void
   hipError_t e = scope.enter(s);
   const bool half = b->dtype == MOE_F16;
   if (e == hipSuccess)
-    e = b->head_dim == 64    ? launch_attend<64>(a, half, many, s)
-        : b->head_dim == 128 ? launch_attend<128>(a, half, many, s)
-                             : launch_attend<256>(a, half, many, s);
+    e = b->head_dim == 64    ? launch_attend<64>(a, half, rows, s)
+        : b->head_dim == 128 ? launch_attend<128>(a, half, rows, s)
+                             : launch_attend<256>(a, half, rows, s);
   return e == hipSuccess ? MOE_OK : hip_fail("moe_kv_attend", e);
 }
 

@@ -50,12 +50,10 @@ struct AttendArgs {
 // in_f32: q, k, v hold fp32 instead of the cache's type; half: the cache's type is fp16
 hipError_t launch_append(const AppendArgs &a, bool half, bool in_f32, hipStream_t s);
 
-// Rows of a tile of the two attention kernels: few rows per sequence (a block's waves share
-// the rows and split the keys) or many (they share the keys and split the rows).
-constexpr int kFewRows = 32, kManyRows = 128;
+// rows: of a tile, 32, 64 or 128
 uint64_t attend_work_bytes(const AttendArgs &a, int rows, int dim);
 template <int D>
-hipError_t launch_attend(const AttendArgs &a, bool half, bool many, hipStream_t s);
+hipError_t launch_attend(const AttendArgs &a, bool half, int rows, hipStream_t s);
 
 struct SampleArgs {
   const void *logits;

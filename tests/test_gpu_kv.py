@@ -43,10 +43,11 @@ def test_chunks(dtype, dim, group, page, window):
 
 @pytest.mark.parametrize("window", [0, 1, 33, 100])
 @pytest.mark.parametrize("new", [2, 5, 8])
-def test_verification_windows(new, window):
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_verification_windows(dim, new, window):
     torch = torch_cuda()
     seqs = [(new, p) for p in (0, 1, 30, 31, 64, 250, 700)]
-    b = Batch(torch, seqs, 16, 2, 128, 16, torch.bfloat16, seed=new)
+    b = Batch(torch, seqs, 16, 2, dim, 16, torch.bfloat16, seed=new)
     b.check(b.cache(window=window, scale=0.2).attend(b.q_gpu(), b.pages, b.starts, b.lengths), window, scale=0.2)
 
 
