@@ -176,17 +176,15 @@ struct Rows {
 // Key (within its 32) of accumulator r of a score product, for this lane's half.
 __device__ __forceinline__ int key_of(int r, int half) { return 16 * (r / 8) + 8 * half + r % 8; }
 
-// Scores of keys that their row does not see become -inf.
+// Scores of keys that their row does not see become -inf: floor < t <= pos, as one comparison.
 template <int N>
 __device__ __forceinline__ void mask_scores(f32x16 (&s)[N], int t0, int pos, int floor) {
-  const int half = threadIdx.x % kLanes / 32;
+  const uint32_t first = t0 + 8 * (threadIdx.x % kLanes / 32) - floor - 1, seen = pos - floor;
 #pragma unroll
   for (int n = 0; n < N; ++n)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int t = t0 + 32 * n + key_of(r, half);
-      if (t > pos || t <= floor) s[n][r] = kNegInf;
-    }
+    for (int r = 0; r < 16; ++r)
+      if (first + (32 * n + key_of(r, 0)) >= seen) s[n][r] = kNegInf;
 }
 
 // Scores to probabilities over 32 * N keys: takes the new maximum, rescales the rows where some
@@ -244,19 +242,24 @@ __device__ __forceinline__ u32x4 keep_first(u32x4 v, int n) {
 template <class E, int D>
 __device__ __forceinline__ bool clean_values(u32x4 (&v)[D / 32], int t0, int end) {
   constexpr uint32_t lo = __is_same(E, __bf16) ? 0x7f80u : 0x7c00u, hi = lo << 16;
-  const int n = min(8, max(0, end - (t0 + 8 * (int)(threadIdx.x % kLanes / 32))));
-  bool odd = false;
+  if (t0 + 16 > end) {
+    const int n = min(8, max(0, end - (t0 + 8 * (int)(threadIdx.x % kLanes / 32))));
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i) {
-    v[i] = keep_first(v[i], n);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const bool a = (v[i][j] & lo) == lo, b = (v[i][j] & hi) == hi;
-      odd |= a || b;
-      v[i][j] &= (a ? 0u : 0xffffu) | (b ? 0u : 0xffff0000u);
-    }
+    for (int i = 0; i < D / 32; ++i) v[i] = keep_first(v[i], n);
   }
-  return __any(odd);
+  // an exponent of ones carries into the sign's place when one is added to it
+  uint32_t odd = 0;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) odd |= (v[i][j] & 0x7fff7fffu) + (0x80008000u - (lo | hi));
+  if (!__any(odd & 0x80008000u)) return false;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      v[i][j] &= ((v[i][j] & lo) == lo ? 0u : 0xffffu) | ((v[i][j] & hi) == hi ? 0u : 0xffff0000u);
+  return true;
 }
 
 // Adds the values of keys t0 .. t1 - 1 that are not finite to the rows that see them (their weight
