@@ -98,44 +98,36 @@ __device__ __forceinline__ uint64_t wave_max(uint64_t v) {
   return v;
 }
 
-// exp((z - top) / T), and its whole number of 2^-shift's.
+// exp((z - top) / T) in units of 2^-shift; a row's masses are sums of these, rounded to whole units.
 struct Weigh {
   float top;     // the row's largest logit
   double scale;  // 1 / T
   int shift;     // at most 50
-  struct Weight {
-    double w;
-    uint64_t parts;
-  };
-  // With x = n ln 2 + g, |g| <= ln 2 / 2: e^x = 2^n e^g, e^g by its series to g^12 / 12! (what is left
-  // is below 2^-52), the whole parts from the bits of e^g's mantissa.  0 for NaN and -inf.
-  __device__ __forceinline__ Weight operator()(float z) const {
-    if (z == top) return {1.0, 1ull << shift};
+  // With x = n ln 2 + g, |g| <= ln 2 / 2: e^x = 2^n e^g, e^g by its series to g^11 / 11! (what is left
+  // is below 2^-47 of it).  0 for NaN and -inf.
+  __device__ __forceinline__ double operator()(float z) const {
     const double x = ((double)z - (double)top) * scale;
-    if (!(x > -64.0)) return {0.0, 0};  // e^-64 is below a half of every unit
     const double n = rint(x * 1.4426950408889634);
     const double g = fma(n, -1.9082149292705877e-10, fma(n, -0.6931471803691238, x));  // ln 2 in two parts
     // odd and even powers apart: two chains of half the length
     const double g2 = g * g;
-    double even = 1.0 / 479001600, odd = 1.0 / 39916800;
-    even = fma(even, g2, 1.0 / 3628800);
-    odd = fma(odd, g2, 1.0 / 362880);
+    double even = 1.0 / 3628800, odd = 1.0 / 39916800;
     even = fma(even, g2, 1.0 / 40320);
-    odd = fma(odd, g2, 1.0 / 5040);
+    odd = fma(odd, g2, 1.0 / 362880);
     even = fma(even, g2, 1.0 / 720);
-    odd = fma(odd, g2, 1.0 / 120);
+    odd = fma(odd, g2, 1.0 / 5040);
     even = fma(even, g2, 1.0 / 24);
-    odd = fma(odd, g2, 1.0 / 6);
+    odd = fma(odd, g2, 1.0 / 120);
     even = fma(even, g2, 0.5);
+    odd = fma(odd, g2, 1.0 / 6);
     odd = fma(odd, g2, 1.0);
     const double e = fma(odd, g, fma(even, g2, 1.0));
-    const uint64_t bits = __builtin_bit_cast(uint64_t, e);
-    const int up = (int)n;
-    const uint64_t mantissa = (bits & ((1ull << 52) - 1)) | 1ull << 52;
-    const int k = 52 - ((int)(bits >> 52) - 1023) - up - shift;  // >= 2: x <= 0, shift <= 50
-    const uint64_t parts = k > 54 ? 0 : (mantissa + (1ull << (k - 1))) >> k;
-    return {__builtin_bit_cast(double, bits + ((uint64_t)(int64_t)up << 52)), parts};
+    const uint64_t bits = __builtin_bit_cast(uint64_t, e) + ((uint64_t)(uint32_t)((int)n + shift) << 52);
+    const double w = __builtin_bit_cast(double, bits);
+    // e^-64 is below a half of every unit; a NaN compares false
+    return z == top ? (double)(1ull << shift) : x > -64.0 ? w : 0.0;
   }
+  __device__ __forceinline__ uint64_t units(float z) const { return (uint64_t)rint((*this)(z)); }
 };
 
 // A row's settings, and its largest logit.
@@ -171,6 +163,9 @@ struct Binning {
   // (of halves: two logits may be further apart than the largest float)
   __device__ __forceinline__ float depth(float z) const { return z == top ? 0.f : (0.5f * top - 0.5f * z) * scale; }
   __device__ __forceinline__ int bin(float x) const { return x < limit ? min(kBins - 1, (int)(x * per)) : kBins; }
+  // the same as a number to compare with starts and ends of bins: bin <= b is place < end(b)
+  __device__ __forceinline__ float place(float x) const { return x < limit ? fminf(x * per, kBins - 0.5f) : __builtin_inff(); }
+  static __device__ __forceinline__ float end(int b) { return b >= kBins - 1 ? __builtin_inff() : (float)(b + 1); }
 };
 
 // The largest of the blocks' bests; every wave of the block for itself.
@@ -202,20 +197,21 @@ __global__ __launch_bounds__(kSliceThreads) void largest_kernel(SampleArgs a, in
   }
 }
 
-// Pass 2, for rows with a filter by rank: elements (for top-k) and mass (for top-p) by bin.  The
+// Pass 2, for rows with a filter by rank: elements (for top-k) and mass (for top-p) by bin, four
+// blocks' slices to a block (each block adds its bins to the row's one by one).  The
 // masses here are of 32-bit exponentials, rounded to 2^-31: they only choose which bins need
 // ranking, with their errors allowed for (least_of, most_of).
 template <class Z>
-__global__ __launch_bounds__(kSliceThreads) void bins_kernel(SampleArgs a, int len, int shift) {
+__global__ __launch_bounds__(kThreads) void bins_kernel(SampleArgs a, int blocks, int len, int shift) {
   RowWork &w = ((RowWork *)a.work)[blockIdx.y];
-  const Row r(a, blockIdx.y, row_best(w, gridDim.x));
+  const Row r(a, blockIdx.y, row_best(w, blocks));
   if (r.none || r.greedy || !r.ranked()) return;
   __shared__ uint64_t mass[kBins];
   __shared__ uint32_t count[kBins];
-  for (int i = threadIdx.x; i < kBins; i += kSliceThreads) mass[i] = 0, count[i] = 0;
+  for (int i = threadIdx.x; i < kBins; i += kThreads) mass[i] = 0, count[i] = 0;
   __syncthreads();
   const void *z = (const Z *)a.logits + (int64_t)blockIdx.y * a.stride;
-  const int lo = min(a.vocab, (int)(blockIdx.x * kSliceWaves + threadIdx.x / 64) * len);
+  const int lo = min(a.vocab, (int)(blockIdx.x * kWaves + threadIdx.x / 64) * len);
   const Binning bin(r, shift);
   const bool by_mass = r.p < 1.f, by_count = r.k != 0;
   for_each<Z>(z, lo, min(a.vocab, lo + len), [&](float v, int) __attribute__((always_inline)) {
@@ -229,7 +225,7 @@ __global__ __launch_bounds__(kSliceThreads) void bins_kernel(SampleArgs a, int l
     if (by_count) atomicAdd(&count[b], 1u);
   }, [] {});
   __syncthreads();
-  for (int i = threadIdx.x; i < kBins; i += kSliceThreads) {
+  for (int i = threadIdx.x; i < kBins; i += kThreads) {
     if (mass[i]) atomicAdd((unsigned long long *)&w.mass[i], (unsigned long long)mass[i]);
     if (count[i]) atomicAdd(&w.count[i], count[i]);
   }
@@ -338,24 +334,34 @@ __global__ __launch_bounds__(kSliceThreads) void collect_kernel(SampleArgs a, in
   const int slice = blockIdx.x * kSliceWaves + wave, lo = min(V, slice * len);
   const Binning bin(r, shift);
   const Weigh weigh = r.weigh(shift);
-  const double least = r.least;
-  const int last = min(rank_bin, kBins - 1);
+  const double least = (double)r.least * (double)(1ull << shift);
+  const float low_start = (float)low, high_end = bin.end(high), rank_start = (float)rank_bin,
+              rank_end = bin.end(rank_bin), last_end = rank_bin < kBins ? rank_end : __builtin_inff();
+  const bool parted = high < rank_bin && low < kBins;  // elements past the list's first part count apart
+  // whole units, exact in a double up to 2^53: so many sums at a time
   uint64_t before_low = 0, kept_low = 0, between = 0;
+  double before_d = 0, kept_d = 0, between_d = 0;
+  int room = 1 << (53 - shift);
   // few elements of a row with a cut lie before it: they are queued, so that the 64-bit
   // exponentials are taken by full waves
   float *queue = queues[wave];
   int queued = 0;
+  auto flush = [&]() __attribute__((always_inline)) {
+    before_low += (uint64_t)before_d, kept_low += (uint64_t)kept_d, between += (uint64_t)between_d;
+    before_d = kept_d = between_d = 0;
+    room = 1 << (53 - shift);
+  };
   auto weigh_one = [&](float v) __attribute__((always_inline)) {
-    const Weigh::Weight x = weigh(v);
-    const bool early = bin.bin(bin.depth(v)) < low;
-    before_low += early ? x.parts : 0;
-    kept_low += early && !(x.w < least) ? x.parts : 0;
-    between += early ? 0 : x.parts;
+    const double x = weigh(v), n = rint(x);
+    const bool early = !parted || bin.place(bin.depth(v)) < low_start;
+    before_d += early ? n : 0;
+    kept_d += early && !(x < least) ? n : 0;
+    between_d += early ? 0 : n;
   };
   for_each<Z>(z, lo, min(V, lo + len), [&](float v, int i) __attribute__((always_inline)) {
-    const int b = bin.bin(bin.depth(v));
-    const bool listed = (b >= low && b <= high) || b == rank_bin;
-    if (listed && b < kBins) {
+    const float f = bin.place(bin.depth(v));
+    const bool listed = (f >= low_start && f < high_end) || (f >= rank_start && f < rank_end);
+    if (listed) {
       const int at = atomicAdd(&n_mine, 1);
       if (at < kOwn) {
         mine[at] = code_of(rank_key(v), i);
@@ -364,7 +370,7 @@ __global__ __launch_bounds__(kSliceThreads) void collect_kernel(SampleArgs a, in
         if (far < kCandidates) w.list[far] = code_of(rank_key(v), i);
       }
     }
-    const bool in = b <= last && !listed;
+    const bool in = f < last_end && !listed;
     const uint64_t mask = __ballot(in);
     if (in) queue[queued + __popcll(mask & ((1ull << lane) - 1))] = v;
     queued += __popcll(mask);
@@ -375,11 +381,13 @@ __global__ __launch_bounds__(kSliceThreads) void collect_kernel(SampleArgs a, in
       const float v0 = queue[queued + lane], v1 = queue[queued + 64 + lane];
       weigh_one(v0);
       weigh_one(v1);
+      if ((room -= 2) < 2) flush();
     }
     __builtin_amdgcn_wave_barrier();
   });
   if (lane < queued) weigh_one(queue[lane]);
   if (lane + 64 < queued) weigh_one(queue[lane + 64]);
+  flush();
   before_low = wave_sum(before_low), kept_low = wave_sum(kept_low), between = wave_sum(between);
   if (lane < 3) w.sums[slice][lane] = lane == 0 ? before_low : lane == 1 ? kept_low : between;
   __syncthreads();
@@ -406,7 +414,7 @@ __device__ uint64_t select_row(const void *z, int V, const Weigh &weigh, uint64_
       const float x = logit<Z>(z, i);
       const uint32_t k = rank_key(x);
       if (code_of(k, i) > in || (bits < 24 && k >> (bits + 8) != key >> (bits + 8))) continue;
-      const uint64_t n = weighted ? weigh(x).parts : 1;
+      const uint64_t n = weighted ? weigh.units(x) : 1;
       if (n) atomicAdd((unsigned long long *)&hist[k >> bits & 255], (unsigned long long)n);
     }
     __syncthreads();
@@ -423,7 +431,7 @@ __device__ uint64_t select_row(const void *z, int V, const Weigh &weigh, uint64_
     __syncthreads();
   }
   // equal logits: the first `ties` of them by index
-  const uint64_t one = weighted ? weigh(unrank(key)).parts : 1;
+  const uint64_t one = weighted ? weigh.units(unrank(key)) : 1;
   const uint64_t ties = one ? (want - above + one - 1) / one : 1;
   uint64_t seen = 0;
   for (int base = 0; base < V; base += kThreads) {
@@ -473,11 +481,11 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleArgs a, int blocks
     return;
   }
   const Weigh weigh = r.weigh(shift);
-  const double least = r.least;
+  const double least = (double)r.least * (double)(1ull << shift);
   auto kept = [&](float v, int i, uint64_t cut) -> uint64_t {
     if (code_of(rank_key(v), i) > cut) return 0;
-    const Weigh::Weight x = weigh(v);
-    return x.w < least ? 0 : x.parts;
+    const double x = weigh(v);
+    return x < least ? 0 : (uint64_t)rint(x);
   };
   uint64_t cut = ~0ull;  // code of the last element that the filters by rank keep
   const int n = r.ranked() ? w.n_list : 0;
@@ -492,7 +500,7 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleArgs a, int blocks
     }
     for (int i = threadIdx.x; i < n; i += kThreads) {
       codes[i] = w.list[i];
-      parts[i] = weigh(unrank(~(uint32_t)(codes[i] >> 32))).parts;
+      parts[i] = weigh.units(unrank(~(uint32_t)(codes[i] >> 32)));
     }
     __syncthreads();
     if (n) {
@@ -557,7 +565,7 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleArgs a, int blocks
       uint64_t mass = 0;
       for (int i = threadIdx.x; i < V; i += kThreads) {
         const float x = logit<Z>(z, i);
-        if (code_of(rank_key(x), i) <= cut) mass += weigh(x).parts;
+        if (code_of(rank_key(x), i) <= cut) mass += weigh.units(x);
       }
       mass = wave_sum(mass);
       if (lane == 0) scratch[wave] = mass;
@@ -641,7 +649,8 @@ hipError_t launch(const SampleArgs &a, hipStream_t s) {
   void *last[] = {const_cast<SampleArgs *>(&a), &blocks, &len, &shift};
   hipError_t e = hipLaunchKernel((const void *)largest_kernel<Z>, grid, dim3(kSliceThreads), first, 0, s);
   if (e == hipSuccess && (a.top_k || a.top_p))
-    e = hipLaunchKernel((const void *)bins_kernel<Z>, grid, dim3(kSliceThreads), then, 0, s);
+    e = hipLaunchKernel((const void *)bins_kernel<Z>, dim3((blocks * kSliceWaves + kWaves - 1) / kWaves, a.rows),
+                        dim3(kThreads), last, 0, s);
   if (e == hipSuccess) e = hipLaunchKernel((const void *)collect_kernel<Z>, grid, dim3(kSliceThreads), then, 0, s);
   if (e == hipSuccess) e = hipLaunchKernel((const void *)draw_kernel<Z>, dim3(a.rows), dim3(kThreads), last, 0, s);
   return e;
