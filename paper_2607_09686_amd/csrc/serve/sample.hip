@@ -58,33 +58,40 @@ __device__ __forceinline__ float unrank(uint32_t key) {
 // Elements in falling order, equal logits by rising index, are rising codes.
 __device__ __forceinline__ uint64_t code_of(uint32_t key, int i) { return (uint64_t)~key << 32 | (uint32_t)i; }
 
-// Calls f(logit, index) for lo <= index < hi, by one wave: 16-byte loads between the first and the
-// last aligned place, four in flight.  Every lane takes part in every call, with a NaN where it has no element;
-// g() is called after every few.
-template <class Z, class F, class G>
-__device__ __forceinline__ void for_each(const void *row, int lo, int hi, F f, G g) {
-  constexpr int kVec = 16 / sizeof(Z), kAhead = 4;
-  typedef Z zv __attribute__((ext_vector_type(kVec)));
+// Calls f(logits, index of the first) for lo <= index < hi, by one wave: as many consecutive logits to a
+// lane as 16 bytes hold, NaNs where there are none, four loads in flight.  Every lane takes part in
+// every call.
+template <class Z>
+constexpr int kVec = 16 / sizeof(Z);
+template <class Z, class F>
+__device__ __forceinline__ void for_each(const void *row, int lo, int hi, F f) {
+  constexpr int kAhead = 4, V = kVec<Z>;
+  typedef Z zv __attribute__((ext_vector_type(V)));
   const Z *z = (const Z *)row;
   const float nan = __builtin_nanf("");
   const int lane = threadIdx.x % 64;
-  const int skip = (int)(-(uintptr_t)(z + lo) / sizeof(Z) % kVec);
-  const int body = min(hi, lo + skip), vecs = (hi - body) / kVec, tail = body + vecs * kVec;
-  if (body > lo) f(lane < body - lo ? (float)z[lo + lane] + 0.f : nan, lo + lane);
-  if (hi > tail) f(lane < hi - tail ? (float)z[tail + lane] + 0.f : nan, tail + lane);
-  g();
+  const int skip = (int)(-(uintptr_t)(z + lo) / sizeof(Z) % V);
+  const int body = min(hi, lo + skip), vecs = (hi - body) / V, tail = body + vecs * V;
+  // fewer than 16 bytes on either side: lanes 0 .. V - 1 and V .. 2 V - 1
+  const int at = lane < V ? lo + lane : tail + lane - V;
+  const bool edge = lane < V ? at < body : lane < 2 * V && at < hi;
+  float v[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) v[j] = nan;
+  if (edge) v[0] = (float)z[at] + 0.f;
+  if (body > lo || hi > tail) f(v, at);
   for (int v0 = lane; v0 - lane < vecs; v0 += 64 * kAhead) {
     zv e[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u)
-      if (v0 + 64 * u < vecs) e[u] = *(const zv *)(z + body + (v0 + 64 * u) * kVec);
+      if (v0 + 64 * u < vecs) e[u] = *(const zv *)(z + body + (v0 + 64 * u) * V);
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      const int v = v0 + 64 * u;
-      if (v - lane >= vecs) break;
+      const int at = v0 + 64 * u;
+      if (at - lane >= vecs) break;
 #pragma unroll
-      for (int j = 0; j < kVec; ++j) f(v < vecs ? (float)e[u][j] + 0.f : nan, body + v * kVec + j);
-      g();
+      for (int j = 0; j < V; ++j) v[j] = at < vecs ? (float)e[u][j] + 0.f : nan;
+      f(v, body + at * V);
     }
   }
 }
@@ -184,9 +191,10 @@ __global__ __launch_bounds__(kSliceThreads) void largest_kernel(SampleArgs a, in
     w.mass[i] = 0, w.count[i] = 0;
   if (blockIdx.x == 0 && threadIdx.x == 0) w.n_list = 0;
   uint64_t best = 0;
-  for_each<Z>(z, lo, min(a.vocab, lo + len), [&](float x, int i) __attribute__((always_inline)) {
-    best = max(best, (uint64_t)rank_key(x) << 32 | (uint32_t)~i);
-  }, [] {});
+  for_each<Z>(z, lo, min(a.vocab, lo + len), [&](const float (&v)[kVec<Z>], int i) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < kVec<Z>; ++j) best = max(best, (uint64_t)rank_key(v[j]) << 32 | (uint32_t)~(i + j));
+  });
   __shared__ uint64_t scratch[kSliceWaves];
   best = wave_max(best);
   if (threadIdx.x % 64 == 0) scratch[threadIdx.x / 64] = best;
@@ -214,16 +222,19 @@ __global__ __launch_bounds__(kThreads) void bins_kernel(SampleArgs a, int blocks
   const int lo = min(a.vocab, (int)(blockIdx.x * kWaves + threadIdx.x / 64) * len);
   const Binning bin(r, shift);
   const bool by_mass = r.p < 1.f, by_count = r.k != 0;
-  for_each<Z>(z, lo, min(a.vocab, lo + len), [&](float v, int) __attribute__((always_inline)) {
-    const float x = bin.depth(v);
-    const int b = bin.bin(x);
-    if (b >= kBins) return;
-    if (by_mass) {
-      const uint32_t m = (uint32_t)rintf(__builtin_amdgcn_exp2f(x * -1.44269504f) * 0x1p31f);
-      atomicAdd((unsigned long long *)&mass[b], (unsigned long long)m);
+  for_each<Z>(z, lo, min(a.vocab, lo + len), [&](const float (&v)[kVec<Z>], int) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < kVec<Z>; ++j) {
+      const float x = bin.depth(v[j]);
+      const int b = bin.bin(x);
+      if (b >= kBins) continue;
+      if (by_mass) {
+        const uint32_t m = (uint32_t)rintf(__builtin_amdgcn_exp2f(x * -1.44269504f) * 0x1p31f);
+        atomicAdd((unsigned long long *)&mass[b], (unsigned long long)m);
+      }
+      if (by_count) atomicAdd(&count[b], 1u);
     }
-    if (by_count) atomicAdd(&count[b], 1u);
-  }, [] {});
+  });
   __syncthreads();
   for (int i = threadIdx.x; i < kBins; i += kThreads) {
     if (mass[i]) atomicAdd((unsigned long long *)&w.mass[i], (unsigned long long)mass[i]);
@@ -255,9 +266,7 @@ __global__ __launch_bounds__(kSliceThreads) void collect_kernel(SampleArgs a, in
   }
   const Row r(a, blockIdx.y, row_best(w, gridDim.x));
   if (r.none || r.greedy) return;
-  constexpr int kQueue = 64 * (16 / sizeof(Z)) + 128;
   __shared__ uint64_t mine[kOwn], scratch[kSliceWaves];
-  __shared__ float queues[kSliceWaves][kQueue];
   __shared__ uint32_t counts[kSliceWaves];
   __shared__ int cuts[3], n_mine, place;
   __shared__ double reach[2];
@@ -342,51 +351,38 @@ __global__ __launch_bounds__(kSliceThreads) void collect_kernel(SampleArgs a, in
   uint64_t before_low = 0, kept_low = 0, between = 0;
   double before_d = 0, kept_d = 0, between_d = 0;
   int room = 1 << (53 - shift);
-  // few elements of a row with a cut lie before it: they are queued, so that the 64-bit
-  // exponentials are taken by full waves
-  float *queue = queues[wave];
-  int queued = 0;
   auto flush = [&]() __attribute__((always_inline)) {
     before_low += (uint64_t)before_d, kept_low += (uint64_t)kept_d, between += (uint64_t)between_d;
     before_d = kept_d = between_d = 0;
     room = 1 << (53 - shift);
   };
-  auto weigh_one = [&](float v) __attribute__((always_inline)) {
-    const double x = weigh(v), n = rint(x);
-    const bool early = !parted || bin.place(bin.depth(v)) < low_start;
-    before_d += early ? n : 0;
-    kept_d += early && !(x < least) ? n : 0;
-    between_d += early ? 0 : n;
-  };
-  for_each<Z>(z, lo, min(V, lo + len), [&](float v, int i) __attribute__((always_inline)) {
-    const float f = bin.place(bin.depth(v));
-    const bool listed = (f >= low_start && f < high_end) || (f >= rank_start && f < rank_end);
-    if (listed) {
-      const int at = atomicAdd(&n_mine, 1);
-      if (at < kOwn) {
-        mine[at] = code_of(rank_key(v), i);
-      } else {
-        const int far = atomicAdd(&w.n_list, 1);
-        if (far < kCandidates) w.list[far] = code_of(rank_key(v), i);
+  for_each<Z>(z, lo, min(V, lo + len), [&](const float (&v)[kVec<Z>], int i) __attribute__((always_inline)) {
+    // with a top-k cut few of a row's elements matter: most calls end here
+    float f[kVec<Z>], least_f = __builtin_inff();
+#pragma unroll
+    for (int j = 0; j < kVec<Z>; ++j) least_f = fminf(least_f, f[j] = bin.place(bin.depth(v[j])));
+    if (!__any(least_f < last_end)) return;
+#pragma unroll
+    for (int j = 0; j < kVec<Z>; ++j) {
+      const bool listed = (f[j] >= low_start && f[j] < high_end) || (f[j] >= rank_start && f[j] < rank_end);
+      if (listed) {
+        const uint64_t code = code_of(rank_key(v[j]), i + j);
+        const int at = atomicAdd(&n_mine, 1);
+        if (at < kOwn) {
+          mine[at] = code;
+        } else {
+          const int far = atomicAdd(&w.n_list, 1);
+          if (far < kCandidates) w.list[far] = code;
+        }
       }
+      const double x = weigh(v[j]), n = rint(x);
+      const bool in = f[j] < last_end && !listed, early = !parted || f[j] < low_start;
+      before_d += in && early ? n : 0;
+      kept_d += in && early && !(x < least) ? n : 0;
+      between_d += in && !early ? n : 0;
     }
-    const bool in = f < last_end && !listed;
-    const uint64_t mask = __ballot(in);
-    if (in) queue[queued + __popcll(mask & ((1ull << lane) - 1))] = v;
-    queued += __popcll(mask);
-  }, [&]() __attribute__((always_inline)) {
-    __builtin_amdgcn_wave_barrier();
-    while (queued >= 128) {  // two at a time: one's arithmetic fills the other's waits
-      queued -= 128;
-      const float v0 = queue[queued + lane], v1 = queue[queued + 64 + lane];
-      weigh_one(v0);
-      weigh_one(v1);
-      if ((room -= 2) < 2) flush();
-    }
-    __builtin_amdgcn_wave_barrier();
+    if ((room -= kVec<Z>) < kVec<Z>) flush();
   });
-  if (lane < queued) weigh_one(queue[lane]);
-  if (lane + 64 < queued) weigh_one(queue[lane + 64]);
   flush();
   before_low = wave_sum(before_low), kept_low = wave_sum(kept_low), between = wave_sum(between);
   if (lane < 3) w.sums[slice][lane] = lane == 0 ? before_low : lane == 1 ? kept_low : between;
