@@ -420,7 +420,8 @@ typedef struct {
 } moe_sample_batch;
 /* token: device [n_rows]; prob: device [n_rows], nullable: the chosen token's
  * share of the mass that the filters left.  workspace: as moe_kv_attend's, of the
- * size that moe_sample_workspace gives (n_rows matters alone). */
+ * size that moe_sample_workspace gives for n_rows and vocab (0 for short rows:
+ * NULL will do then). */
 int moe_sample(const moe_sample_batch *b, int32_t *token, float *prob, void *workspace, uint64_t workspace_bytes);
 int moe_sample_workspace(const moe_sample_batch *b, uint64_t *bytes);
 

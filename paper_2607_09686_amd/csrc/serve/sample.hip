@@ -21,7 +21,7 @@
 namespace moecache {
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64;  // of the draw, a block per row
+constexpr int kThreads = 512, kWaves = kThreads / 64;  // of the draw, a block per row
 constexpr int kSliceThreads = 256;                      // of the passes over slices of a row
 constexpr int kSliceWaves = kSliceThreads / 64;
 constexpr int kMaxBlocks = 64;                          // of a row's passes; its slices are their waves
@@ -29,18 +29,6 @@ constexpr int kMaxSlices = kMaxBlocks * kSliceWaves;
 constexpr int kBins = 2048;
 constexpr int kCandidates = 4096;
 constexpr int kOwn = 512;  // of them, a block's, before it hands them over one by one
-
-// Per row in the workspace.
-struct RowWork {
-  uint64_t best[kMaxBlocks];     // blocks' largest logit: rank key, then the smallest index
-  uint64_t sums[kMaxSlices][3];  // slices' masses, see collect_kernel
-  uint64_t mass[kBins];          // binned, in 2^-31
-  uint32_t count[kBins];
-  uint64_t list[kCandidates];    // codes of the elements that need ranking
-  int32_t n_list;                // how many there are, in the list or not
-  int32_t high, rank_bin;        // last bin of the top-p cut's; bin of the top-k cut (kBins: none)
-  uint32_t before_rank;          // elements in bins before rank_bin
-};
 
 template <class Z>
 __device__ __forceinline__ float logit(const void *row, int i) {
@@ -105,34 +93,37 @@ __device__ __forceinline__ uint64_t wave_max(uint64_t v) {
   return v;
 }
 
-// exp((z - top) / T) in units of 2^-shift; a row's masses are sums of these, rounded to whole units.
+// exp((z - top) / T) in units of 2^-shift, for a finite top; a row's masses are sums of these, rounded to
+// whole units.
 struct Weigh {
-  float top;     // the row's largest logit
-  double scale;  // 1 / T
-  int shift;     // at most 50
-  // With x = n ln 2 + g, |g| <= ln 2 / 2: e^x = 2^n e^g, e^g by its series to g^11 / 11! (what is left
-  // is below 2^-47 of it).  0 for NaN and -inf.
+  double top;     // the row's largest logit
+  double scale;   // log2(e) / T
+  double c[12];   // (ln 2)^k / k!
+  double shift;   // at most 50
+  __device__ Weigh(float top_, float T, int shift_)
+      : top(top_), scale(1.4426950408889634 / (double)T), shift(shift_) {
+    double term = 1.0;
+#pragma unroll
+    for (int k = 0; k < 12; ++k) {
+      c[k] = term;
+      term *= 0.69314718055994531 / (k + 1);
+      asm("" : "+s"(c[k]));  // in scalar registers, which an fma takes as they are
+    }
+  }
+  // With y = n + f, |f| <= 1/2: 2^y = 2^n 2^f, 2^f by its series to f^11 (what is left is below 2^-47 of
+  // it).  0 for NaN and -inf (the maximum of a NaN and a number is the number).
   __device__ __forceinline__ double operator()(float z) const {
-    const double x = ((double)z - (double)top) * scale;
-    const double n = rint(x * 1.4426950408889634);
-    const double g = fma(n, -1.9082149292705877e-10, fma(n, -0.6931471803691238, x));  // ln 2 in two parts
+    const double y = fmax(((double)z - top) * scale, -900.0), n = rint(y), f = y - n, f2 = f * f;
     // odd and even powers apart: two chains of half the length
-    const double g2 = g * g;
-    double even = 1.0 / 3628800, odd = 1.0 / 39916800;
-    even = fma(even, g2, 1.0 / 40320);
-    odd = fma(odd, g2, 1.0 / 362880);
-    even = fma(even, g2, 1.0 / 720);
-    odd = fma(odd, g2, 1.0 / 5040);
-    even = fma(even, g2, 1.0 / 24);
-    odd = fma(odd, g2, 1.0 / 120);
-    even = fma(even, g2, 0.5);
-    odd = fma(odd, g2, 1.0 / 6);
-    odd = fma(odd, g2, 1.0);
-    const double e = fma(odd, g, fma(even, g2, 1.0));
-    const uint64_t bits = __builtin_bit_cast(uint64_t, e) + ((uint64_t)(uint32_t)((int)n + shift) << 52);
-    const double w = __builtin_bit_cast(double, bits);
-    // e^-64 is below a half of every unit; a NaN compares false
-    return z == top ? (double)(1ull << shift) : x > -64.0 ? w : 0.0;
+    double even = c[10], odd = c[11];
+#pragma unroll
+    for (int k = 8; k >= 0; k -= 2) {
+      even = fma(even, f2, c[k]);
+      odd = fma(odd, f2, c[k + 1]);
+    }
+    const double e = fma(odd, f, even);
+    const uint64_t bits = __builtin_bit_cast(uint64_t, e) + ((uint64_t)(uint32_t)(int)(n + shift) << 52);
+    return __builtin_bit_cast(double, bits);
   }
   __device__ __forceinline__ uint64_t units(float z) const { return (uint64_t)rint((*this)(z)); }
 };
@@ -142,6 +133,7 @@ struct Row {
   float top, T, p, least;
   int first, k;
   bool none, greedy;  // nothing but -inf and NaN; the first largest is the answer
+  bool wild;          // +inf among the logits: all weight is theirs
   __device__ Row(const SampleArgs &a, int row, uint64_t best) {
     first = (int)~(uint32_t)best;
     top = unrank((uint32_t)(best >> 32));
@@ -153,93 +145,62 @@ struct Row {
     if (least > 1.f) least = 1.f;
     none = !(top > -__builtin_inff());
     greedy = !(T > 0.f);
+    wild = top == __builtin_inff();
   }
   __device__ __forceinline__ bool ranked() const { return k || p < 1.f; }
   __device__ __forceinline__ Weigh weigh(int shift) const {
-    return Weigh{top, 1.0 / (double)T, shift};
+    return Weigh(top, T, shift);
   }
 };
 
-// Bins of (top - z) / T, rising with falling logits; weights beyond the last are below half of 2^-s.
+// Bins of (top - z) / T, rising with falling logits; weights past the last are below half of 2^-shift.
 struct Binning {
-  float top, scale, limit, per;
-  __device__ Binning(const Row &r, int shift) : top(r.top), scale(2.f / r.T) {
-    limit = (float)(shift + 1) * 0.69314718f + 0.01f;
-    per = kBins / limit;
+  float half, scale, depth;  // of a place: its (top - z) / T
+  __device__ Binning(const Row &r, int shift) : half(0.5f * r.top) {
+    const float limit = (float)(shift + 1) * 0.69314718f + 0.01f;
+    scale = fminf(2.f / r.T * (kBins / limit), 3.4e38f);  // finite: 0 times it is 0
+    depth = limit / kBins;
   }
-  // (of halves: two logits may be further apart than the largest float)
-  __device__ __forceinline__ float depth(float z) const { return z == top ? 0.f : (0.5f * top - 0.5f * z) * scale; }
-  __device__ __forceinline__ int bin(float x) const { return x < limit ? min(kBins - 1, (int)(x * per)) : kBins; }
-  // the same as a number to compare with starts and ends of bins: bin <= b is place < end(b)
-  __device__ __forceinline__ float place(float x) const { return x < limit ? fminf(x * per, kBins - 0.5f) : __builtin_inff(); }
-  static __device__ __forceinline__ float end(int b) { return b >= kBins - 1 ? __builtin_inff() : (float)(b + 1); }
+  // Where a logit lies among the bins: in bin (int)place if that is below kBins (a NaN is not).  Of
+  // halves: two logits may be further apart than the largest float.
+  __device__ __forceinline__ float place(float z) const {
+#pragma clang fp contract(off)  // the top's own half less its half is 0
+    return (half - 0.5f * z) * scale;
+  }
 };
 
-// The largest of the blocks' bests; every wave of the block for itself.
-__device__ __forceinline__ uint64_t row_best(const RowWork &w, int blocks) {
-  const int lane = threadIdx.x % 64;
-  return wave_max(lane < blocks ? w.best[lane] : 0);
-}
-
-// Pass 1, a wave per slice of a row: its largest logit; the row's bins are cleared on the way.
+// The largest logit of elements lo .. hi - 1, one wave's: its rank key, then its first index.
 template <class Z>
-__global__ __launch_bounds__(kSliceThreads) void largest_kernel(SampleArgs a, int len) {
-  RowWork &w = ((RowWork *)a.work)[blockIdx.y];
-  const void *z = (const Z *)a.logits + (int64_t)blockIdx.y * a.stride;
-  const int slice = blockIdx.x * kSliceWaves + threadIdx.x / 64, lo = min(a.vocab, slice * len);
-  for (int i = blockIdx.x * kSliceThreads + threadIdx.x; i < kBins; i += gridDim.x * kSliceThreads)
-    w.mass[i] = 0, w.count[i] = 0;
-  if (blockIdx.x == 0 && threadIdx.x == 0) w.n_list = 0;
+__device__ __forceinline__ uint64_t largest_of(const void *z, int lo, int hi) {
   uint64_t best = 0;
-  for_each<Z>(z, lo, min(a.vocab, lo + len), [&](const float (&v)[kVec<Z>], int i) __attribute__((always_inline)) {
+  for_each<Z>(z, lo, hi, [&](const float (&v)[kVec<Z>], int i) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < kVec<Z>; ++j) best = max(best, (uint64_t)rank_key(v[j]) << 32 | (uint32_t)~(i + j));
   });
-  __shared__ uint64_t scratch[kSliceWaves];
-  best = wave_max(best);
-  if (threadIdx.x % 64 == 0) scratch[threadIdx.x / 64] = best;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int i = 1; i < kSliceWaves; ++i) best = max(best, scratch[i]);
-    w.best[blockIdx.x] = best;
-  }
+  return wave_max(best);
 }
 
-// Pass 2, for rows with a filter by rank: elements (for top-k) and mass (for top-p) by bin, four
-// blocks' slices to a block (each block adds its bins to the row's one by one).  The
-// masses here are of 32-bit exponentials, rounded to 2^-31: they only choose which bins need
-// ranking, with their errors allowed for (least_of, most_of).
+// Elements (for top-k) and mass (for top-p) by bin of elements lo .. hi - 1, one wave's.  The masses here
+// are of 32-bit exponentials, rounded to 2^-31: they only choose which bins need ranking, with their
+// errors allowed for (least_of, most_of).
 template <class Z>
-__global__ __launch_bounds__(kThreads) void bins_kernel(SampleArgs a, int blocks, int len, int shift) {
-  RowWork &w = ((RowWork *)a.work)[blockIdx.y];
-  const Row r(a, blockIdx.y, row_best(w, blocks));
-  if (r.none || r.greedy || !r.ranked()) return;
-  __shared__ uint64_t mass[kBins];
-  __shared__ uint32_t count[kBins];
-  for (int i = threadIdx.x; i < kBins; i += kThreads) mass[i] = 0, count[i] = 0;
-  __syncthreads();
-  const void *z = (const Z *)a.logits + (int64_t)blockIdx.y * a.stride;
-  const int lo = min(a.vocab, (int)(blockIdx.x * kWaves + threadIdx.x / 64) * len);
+__device__ __forceinline__ void bin_elements(const void *z, int lo, int hi, const Row &r, int shift, uint64_t *mass,
+                                             uint32_t *count) {
   const Binning bin(r, shift);
   const bool by_mass = r.p < 1.f, by_count = r.k != 0;
-  for_each<Z>(z, lo, min(a.vocab, lo + len), [&](const float (&v)[kVec<Z>], int) __attribute__((always_inline)) {
+  const float exponent = bin.depth * -1.44269504f;
+  for_each<Z>(z, lo, hi, [&](const float (&v)[kVec<Z>], int) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < kVec<Z>; ++j) {
-      const float x = bin.depth(v[j]);
-      const int b = bin.bin(x);
-      if (b >= kBins) continue;
+      const float f = bin.place(v[j]);
+      if (!(f < kBins)) continue;
       if (by_mass) {
-        const uint32_t m = (uint32_t)rintf(__builtin_amdgcn_exp2f(x * -1.44269504f) * 0x1p31f);
-        atomicAdd((unsigned long long *)&mass[b], (unsigned long long)m);
+        const uint32_t m = (uint32_t)rintf(__builtin_amdgcn_exp2f(f * exponent) * 0x1p31f);
+        atomicAdd((unsigned long long *)&mass[(int)f], (unsigned long long)m);
       }
-      if (by_count) atomicAdd(&count[b], 1u);
+      if (by_count) atomicAdd(&count[(int)f], 1u);
     }
   });
-  __syncthreads();
-  for (int i = threadIdx.x; i < kBins; i += kThreads) {
-    if (mass[i]) atomicAdd((unsigned long long *)&w.mass[i], (unsigned long long)mass[i]);
-    if (count[i]) atomicAdd(&w.count[i], count[i]);
-  }
 }
 
 // Bounds on the exact mass, in 2^-31, of elements whose binned masses sum to m: half a unit for each of at most
@@ -248,149 +209,162 @@ __global__ __launch_bounds__(kThreads) void bins_kernel(SampleArgs a, int blocks
 __device__ __forceinline__ double least_of(uint64_t m, int V) { return (double)m * (1.0 - 0x1p-15) - 0.5 * V; }
 __device__ __forceinline__ double most_of(uint64_t m, int V) { return (double)m * (1.0 + 0x1p-15) + 0.5 * V; }
 
-// Pass 3: which bins may hold a cut (every block of a row finds them for itself), the elements of
-// those bins into the row's list, and each slice's exact masses of
-//   0: elements in bins before the list's
-//   1: those of them that min_p keeps
-//   2: elements in bins between the top-p cut's and the top-k cut's
-template <class Z>
-__global__ __launch_bounds__(kSliceThreads) void collect_kernel(SampleArgs a, int len, int shift) {
-  RowWork &w = ((RowWork *)a.work)[blockIdx.y];
-  constexpr int kPer = kBins / kSliceThreads;
-  uint64_t mass[kPer];  // asked for together with the row's settings
-  uint32_t count[kPer];
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    mass[i] = w.mass[threadIdx.x * kPer + i];
-    count[i] = w.count[threadIdx.x * kPer + i];
-  }
-  const Row r(a, blockIdx.y, row_best(w, gridDim.x));
-  if (r.none || r.greedy) return;
-  __shared__ uint64_t mine[kOwn], scratch[kSliceWaves];
-  __shared__ uint32_t counts[kSliceWaves];
-  __shared__ int cuts[3], n_mine, place;
+// Which bins may hold a cut: bins low .. high and rank_bin need their elements ranked; bins past
+// `last` hold nothing that is kept or counts.
+struct Cuts {
+  int low, high, rank_bin;  // all kBins: no cut; rank_bin kBins: no top-k cut
+  uint32_t before_rank;     // elements in bins before rank_bin
+};
+// By a block of N threads, from the bins threadIdx.x * kBins / N on in each; uniform over the block.
+template <int N>
+__device__ __forceinline__ Cuts find_cuts(const uint64_t (&mass)[kBins / N], const uint32_t (&count)[kBins / N],
+                                          const Row &r, int V) {
+  constexpr int kPer = kBins / N;
+  __shared__ uint64_t masses[N / 64];
+  __shared__ uint32_t counts[N / 64], before_rank;
+  __shared__ int cuts[3];
   __shared__ double reach[2];
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, V = a.vocab;
-  // bins low .. high and rank_bin go into the list; bins past `last` hold nothing that is kept
-  int low = kBins, high = kBins, rank_bin = kBins;
-  if (threadIdx.x == 0) n_mine = 0;
-  if (r.ranked()) {
-    uint64_t up = 0;
-    uint32_t up_n = 0;
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  uint64_t up = 0;
+  uint32_t up_n = 0;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) up += mass[i], up_n += count[i];
-    uint64_t before = up;
-    uint32_t before_n = up_n;
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint64_t m = __shfl_up((unsigned long long)up, o);
-      const uint32_t n = __shfl_up(up_n, o);
-      if (lane >= o) up += m, up_n += n;
-    }
-    if (lane == 63) scratch[wave] = up, counts[wave] = up_n;
-    if (threadIdx.x == 0) cuts[0] = 0, cuts[1] = kBins - 1, cuts[2] = kBins;
-    __syncthreads();
-    before = up - before;
-    before_n = up_n - before_n;
-    uint64_t all = 0;
-    uint32_t all_n = 0;
-    for (int i = 0; i < kSliceWaves; ++i) {
-      if (i < wave) before += scratch[i], before_n += counts[i];
-      all += scratch[i];
-      all_n += counts[i];
-    }
-    const bool cut_k = r.k && (uint32_t)r.k < all_n;  // else top-k cuts nothing but weights of 0
-    if (threadIdx.x == 0 && !cut_k) reach[0] = least_of(all, V), reach[1] = most_of(all, V);
-    if (cut_k) {
-      uint64_t at = before;
-      uint32_t n = before_n;
+  for (int i = 0; i < kPer; ++i) up += mass[i], up_n += count[i];
+  uint64_t before = up;
+  uint32_t before_n = up_n;
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint64_t m = __shfl_up((unsigned long long)up, o);
+    const uint32_t n = __shfl_up(up_n, o);
+    if (lane >= o) up += m, up_n += n;
+  }
+  if (lane == 63) masses[wave] = up, counts[wave] = up_n;
+  if (threadIdx.x == 0) cuts[0] = 0, cuts[1] = kBins - 1, cuts[2] = kBins, before_rank = 0;
+  __syncthreads();
+  before = up - before;
+  before_n = up_n - before_n;
+  uint64_t all = 0;
+  uint32_t all_n = 0;
+  for (int i = 0; i < N / 64; ++i) {
+    if (i < wave) before += masses[i], before_n += counts[i];
+    all += masses[i];
+    all_n += counts[i];
+  }
+  const bool cut_k = r.k && (uint32_t)r.k < all_n;  // else top-k cuts nothing but weights of 0
+  if (threadIdx.x == 0 && !cut_k) reach[0] = least_of(all, V), reach[1] = most_of(all, V);
+  if (cut_k) {
+    uint64_t at = before;
+    uint32_t n = before_n;
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        if (n < (uint32_t)r.k && n + count[i] >= (uint32_t)r.k) {  // in one thread's one bin
-          cuts[2] = threadIdx.x * kPer + i;
-          reach[0] = least_of(at, V), reach[1] = most_of(at + mass[i], V);
-          if (blockIdx.x == 0) w.before_rank = n;
-        }
-        at += mass[i];
-        n += count[i];
+    for (int i = 0; i < kPer; ++i) {
+      if (n < (uint32_t)r.k && n + count[i] >= (uint32_t)r.k) {  // in one thread's one bin
+        cuts[2] = threadIdx.x * kPer + i;
+        reach[0] = least_of(at, V), reach[1] = most_of(at + mass[i], V);
+        before_rank = n;
       }
+      at += mass[i];
+      n += count[i];
     }
-    __syncthreads();
-    low = high = rank_bin = cuts[2];
-    if (r.p < 1.f) {
-      // what top-p reaches for lies between these
-      const double least = (double)r.p * reach[0], most = (double)r.p * reach[1] + 1.0;
-      uint64_t at = before;
-      int begun = 0, ended = kBins - 1;
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const int b = threadIdx.x * kPer + i;
-        // the last bin that begins before it for certain, the first that ends past it for certain
-        if (most_of(at, V) < least) begun = b;
-        at += mass[i];
-        if (least_of(at, V) >= most) ended = min(ended, b);
-      }
-      for (int o = 32; o; o >>= 1) begun = max(begun, __shfl_xor(begun, o)), ended = min(ended, __shfl_xor(ended, o));
-      if (lane == 0) atomicMax(&cuts[0], begun), atomicMin(&cuts[1], ended);
-      __syncthreads();
-      high = min(cuts[1], rank_bin);
-      low = min(cuts[0], high);
-    }
-    if (blockIdx.x == 0 && threadIdx.x == 0) w.high = high, w.rank_bin = rank_bin;
   }
   __syncthreads();
+  Cuts c{cuts[2], cuts[2], cuts[2], before_rank};
+  if (r.p < 1.f) {
+    // what top-p reaches for lies between these
+    const double least = (double)r.p * reach[0], most = (double)r.p * reach[1] + 1.0;
+    uint64_t at = before;
+    int begun = 0, ended = kBins - 1;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int b = threadIdx.x * kPer + i;
+      // the last bin that begins before it for certain, the first that ends past it for certain
+      if (most_of(at, V) < least) begun = b;
+      at += mass[i];
+      if (least_of(at, V) >= most) ended = min(ended, b);
+    }
+    for (int o = 32; o; o >>= 1) begun = max(begun, __shfl_xor(begun, o)), ended = min(ended, __shfl_xor(ended, o));
+    if (lane == 0) atomicMax(&cuts[0], begun), atomicMin(&cuts[1], ended);
+    __syncthreads();
+    c.high = min(cuts[1], c.rank_bin);
+    c.low = min(cuts[0], c.high);
+  }
+  return c;
+}
 
-  const void *z = (const Z *)a.logits + (int64_t)blockIdx.y * a.stride;
-  const int slice = blockIdx.x * kSliceWaves + wave, lo = min(V, slice * len);
+// Exact masses of elements lo .. hi - 1, one wave's: of all that may be kept (up to the last bin
+// with a cut; all, without a filter by rank), of those in bins before the list's, of those of them that min_p
+// keeps.  push(code) gets the elements of the bins to be ranked.
+struct Masses {
+  uint64_t all, ahead, kept;
+};
+template <class Z, class Push>
+__device__ __forceinline__ Masses weigh_elements(const void *z, int lo, int hi, const Row &r, const Cuts &c, int shift,
+                                                 Push push) {
   const Binning bin(r, shift);
   const Weigh weigh = r.weigh(shift);
   const double least = (double)r.least * (double)(1ull << shift);
-  const float low_start = (float)low, high_end = bin.end(high), rank_start = (float)rank_bin,
-              rank_end = bin.end(rank_bin), last_end = rank_bin < kBins ? rank_end : __builtin_inff();
-  const bool parted = high < rank_bin && low < kBins;  // elements past the list's first part count apart
+  const float low_start = (float)c.low, high_end = (float)(c.high + 1), rank_start = (float)c.rank_bin,
+              rank_end = (float)(c.rank_bin + 1), last_end = (float)min(c.rank_bin + 1, kBins);
+  // most rows ask for one sum only (elements past the last bin weigh nothing)
+  const bool one_sum = c.low == kBins && !(least > 0.0);
   // whole units, exact in a double up to 2^53: so many sums at a time
-  uint64_t before_low = 0, kept_low = 0, between = 0;
-  double before_d = 0, kept_d = 0, between_d = 0;
+  Masses m{0, 0, 0};
+  double all = 0, ahead = 0, kept = 0;
   int room = 1 << (53 - shift);
   auto flush = [&]() __attribute__((always_inline)) {
-    before_low += (uint64_t)before_d, kept_low += (uint64_t)kept_d, between += (uint64_t)between_d;
-    before_d = kept_d = between_d = 0;
+    m.all += (uint64_t)all, m.ahead += (uint64_t)ahead, m.kept += (uint64_t)kept;
+    all = ahead = kept = 0;
     room = 1 << (53 - shift);
   };
-  for_each<Z>(z, lo, min(V, lo + len), [&](const float (&v)[kVec<Z>], int i) __attribute__((always_inline)) {
+  for_each<Z>(z, lo, hi, [&](const float (&v)[kVec<Z>], int i) __attribute__((always_inline)) {
     // with a top-k cut few of a row's elements matter: most calls end here
     float f[kVec<Z>], least_f = __builtin_inff();
 #pragma unroll
-    for (int j = 0; j < kVec<Z>; ++j) least_f = fminf(least_f, f[j] = bin.place(bin.depth(v[j])));
+    for (int j = 0; j < kVec<Z>; ++j) least_f = fminf(least_f, f[j] = bin.place(v[j]));
     if (!__any(least_f < last_end)) return;
+    // without a branch between them, so that one element's arithmetic fills another's waits
+    double x[kVec<Z>];
 #pragma unroll
-    for (int j = 0; j < kVec<Z>; ++j) {
-      const bool listed = (f[j] >= low_start && f[j] < high_end) || (f[j] >= rank_start && f[j] < rank_end);
-      if (listed) {
-        const uint64_t code = code_of(rank_key(v[j]), i + j);
-        const int at = atomicAdd(&n_mine, 1);
-        if (at < kOwn) {
-          mine[at] = code;
-        } else {
-          const int far = atomicAdd(&w.n_list, 1);
-          if (far < kCandidates) w.list[far] = code;
-        }
+    for (int j = 0; j < kVec<Z>; ++j) x[j] = weigh(v[j]);
+    if (one_sum) {
+#pragma unroll
+      for (int j = 0; j < kVec<Z>; ++j) all += rint(x[j]);
+    } else {
+      bool any = false;
+#pragma unroll
+      for (int j = 0; j < kVec<Z>; ++j) {
+        const double n = f[j] < last_end ? rint(x[j]) : 0.0, early = f[j] < low_start ? n : 0.0;
+        all += n;
+        ahead += early;
+        kept += x[j] < least ? 0.0 : early;
+        any |= (f[j] >= low_start && f[j] < high_end) || (f[j] >= rank_start && f[j] < rank_end);
       }
-      const double x = weigh(v[j]), n = rint(x);
-      const bool in = f[j] < last_end && !listed, early = !parted || f[j] < low_start;
-      before_d += in && early ? n : 0;
-      kept_d += in && early && !(x < least) ? n : 0;
-      between_d += in && !early ? n : 0;
+      if (any) {
+#pragma unroll
+        for (int j = 0; j < kVec<Z>; ++j)
+          if (f[j] < kBins && ((f[j] >= low_start && f[j] < high_end) || (f[j] >= rank_start && f[j] < rank_end)))
+            push(code_of(rank_key(v[j]), i + j));
+      }
     }
     if ((room -= kVec<Z>) < kVec<Z>) flush();
   });
   flush();
-  before_low = wave_sum(before_low), kept_low = wave_sum(kept_low), between = wave_sum(between);
-  if (lane < 3) w.sums[slice][lane] = lane == 0 ? before_low : lane == 1 ? kept_low : between;
-  __syncthreads();
-  if (threadIdx.x == 0 && n_mine) place = atomicAdd(&w.n_list, min(n_mine, kOwn));
-  __syncthreads();
-  for (int i = threadIdx.x; i < min(n_mine, kOwn); i += kSliceThreads)
-    if (place + i < kCandidates) w.list[place + i] = mine[i];
+  if (one_sum) m.ahead = m.kept = m.all;
+  return Masses{wave_sum(m.all), wave_sum(m.ahead), wave_sum(m.kept)};
+}
+
+// A row's part of the workspace.
+struct RowWork {
+  uint64_t best[kMaxBlocks];   // blocks' largest logit: rank key, then the smallest index
+  Masses sums[kMaxSlices];
+  uint64_t mass[kBins];        // binned, in 2^-31
+  uint32_t count[kBins];
+  uint64_t list[kCandidates];  // codes of the elements that need ranking
+  Cuts cuts;
+  int32_t n_list, pad;         // elements that need ranking, in the list or not
+};
+
+// The largest of the blocks' bests; every wave of the block for itself.
+__device__ __forceinline__ uint64_t row_best(const RowWork &w, int blocks) {
+  const int lane = threadIdx.x % 64;
+  return wave_max(lane < blocks ? w.best[lane] : 0);
 }
 
 // The cut as a code, found by going over the whole row: for rows with more elements in the bins
@@ -451,31 +425,41 @@ __device__ uint64_t select_row(const void *z, int V, const Weigh &weigh, uint64_
   return cut;
 }
 
+// The running mass that the drawn element is the first to exceed.
+__device__ __forceinline__ uint64_t target_of(float u, uint64_t mass) {
+  const double want = (double)u * (double)mass;
+  return !(want > 0.0) ? 0 : want >= (double)mass ? mass - 1 : min(mass - 1, (uint64_t)want);
+}
+
 // What top-p reaches for, of a mass: at least 1, so that the first element stays.
 __device__ __forceinline__ uint64_t reach_of(float p, uint64_t mass) {
   const double part = ceil((double)p * (double)mass);
   return part < 1.0 ? 1 : min(mass, (uint64_t)part);
 }
 
-// Pass 4, a block per row: ranks the listed elements, which gives the cut, then finds the slice in
-// which the draw falls, and the element in it.
+// What the last step of a row works on, in LDS.
+struct Last {
+  uint64_t codes[kCandidates];  // the listed elements
+  union {
+    uint64_t parts[kCandidates];  // their masses
+    struct {                      // before those are taken: a row's bins
+      uint64_t mass[kBins];
+      uint32_t count[kBins];
+    };
+  };
+  uint64_t hist[256], scratch[kWaves], found[2], in_slice[kMaxSlices];
+  int n, n_early;
+};
+
+// The last step, a block per row: ranks the listed elements, which gives the cut, then finds the slice
+// (of `len` elements, its kept mass but for the listed ones in in_slice) in which the draw falls, and
+// the element in it.  n elements are to be listed; where they are more than the list takes, the row is gone
+// over instead.  all, ahead: exact masses of what may be kept, and of what is before the list.
 template <class Z>
-__global__ __launch_bounds__(kThreads) void draw_kernel(SampleArgs a, int blocks, int len, int shift) {
-  __shared__ uint64_t codes[kCandidates], parts[kCandidates];
-  __shared__ uint64_t hist[256], scratch[kWaves], found[2], in_slice[kMaxSlices];
-  __shared__ int n_early;
-  const int row = blockIdx.x, V = a.vocab, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  const int slices = blocks * kSliceWaves;
-  const RowWork &w = ((const RowWork *)a.work)[row];
-  const void *z = (const Z *)a.logits + (int64_t)row * a.stride;
-  const Row r(a, row, row_best(w, blocks));
-  if (r.none || r.greedy) {
-    if (threadIdx.x == 0) {
-      a.token[row] = r.none ? -1 : r.first;
-      if (a.prob) a.prob[row] = r.none ? 0.f : 1.f;
-    }
-    return;
-  }
+__device__ __forceinline__ void rank_and_draw(const SampleArgs &a, int row, const void *z, const Row &r, const Cuts &c,
+                                              int n, uint64_t all, uint64_t ahead, int slices, int len, int shift,
+                                              Last &s) {
+  const int V = a.vocab, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const Weigh weigh = r.weigh(shift);
   const double least = (double)r.least * (double)(1ull << shift);
   auto kept = [&](float v, int i, uint64_t cut) -> uint64_t {
@@ -484,26 +468,11 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleArgs a, int blocks
     return x < least ? 0 : (uint64_t)rint(x);
   };
   uint64_t cut = ~0ull;  // code of the last element that the filters by rank keep
-  const int n = r.ranked() ? w.n_list : 0;
+  if (threadIdx.x == 0) s.found[0] = s.found[1] = 0, s.n_early = 0;
   if (n <= kCandidates) {
-    if ((int)threadIdx.x < kMaxSlices) {
-      const bool real = (int)threadIdx.x < slices;
-      in_slice[threadIdx.x] = real ? w.sums[threadIdx.x][1] : 0;
-      const uint64_t ahead = wave_sum(real ? w.sums[threadIdx.x][0] : (uint64_t)0);
-      const uint64_t between = wave_sum(real ? w.sums[threadIdx.x][2] : (uint64_t)0);
-      if (lane == 0) scratch[wave] = ahead, scratch[kMaxSlices / 64 + wave] = between;
-      if (threadIdx.x == 0) found[0] = found[1] = 0, n_early = 0;
-    }
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-      codes[i] = w.list[i];
-      parts[i] = weigh.units(unrank(~(uint32_t)(codes[i] >> 32)));
-    }
+    for (int i = threadIdx.x; i < n; i += kThreads) s.parts[i] = weigh.units(unrank(~(uint32_t)(s.codes[i] >> 32)));
     __syncthreads();
     if (n) {
-      uint64_t ahead = 0, between = 0;
-#pragma unroll
-      for (int i = 0; i < kMaxSlices / 64; ++i) ahead += scratch[i], between += scratch[kMaxSlices / 64 + i];
-      const int high = w.high, rank_bin = w.rank_bin;
       const Binning bin(r, shift);
       constexpr int kEach = kCandidates / kThreads;
       uint64_t code[kEach], before[kEach];  // own elements, the listed mass before them
@@ -511,52 +480,60 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleArgs a, int blocks
 #pragma unroll
       for (int e = 0; e < kEach; ++e) {
         const int i = e * kThreads + threadIdx.x;
-        code[e] = i < n ? codes[i] : ~0ull;
-        const float v = unrank(~(uint32_t)(code[e] >> 32));
-        at[e] = i < n ? bin.bin(bin.depth(v)) : kBins;
+        code[e] = i < n ? s.codes[i] : ~0ull;
+        at[e] = i < n ? (int)bin.place(unrank(~(uint32_t)(code[e] >> 32))) : kBins;
         before[e] = 0;
         rank[e] = 0;
-        if (i < n && at[e] < rank_bin) atomicAdd(&n_early, 1);
+        if (i < n && at[e] < c.rank_bin) atomicAdd(&s.n_early, 1);
       }
       for (int j = 0; j < n; ++j) {
-        const uint64_t other = codes[j], m = parts[j];
+        const uint64_t other = s.codes[j], m = s.parts[j];
 #pragma unroll
         for (int e = 0; e < kEach; ++e)
           if (e * kThreads < n && other < code[e]) before[e] += m, ++rank[e];
       }
       __syncthreads();
-      // the top-k cut, and the listed mass up to it (all, without one)
-      const bool cut_k = r.k && rank_bin < kBins;
-      const int want = cut_k ? n_early + r.k - (int)w.before_rank - 1 : n - 1;
+      // the top-k cut (the last listed element, without one), and the mass past it
+      const bool cut_k = r.k && c.rank_bin < kBins;
+      const int want = cut_k ? s.n_early + r.k - (int)c.before_rank - 1 : n - 1;
 #pragma unroll
       for (int e = 0; e < kEach; ++e)
         if (e * kThreads + (int)threadIdx.x < n && rank[e] == want)
-          found[0] = code[e], found[1] = before[e] + parts[e * kThreads + threadIdx.x];
+          s.found[0] = code[e];
       __syncthreads();
-      cut = found[0];
+      cut = s.found[0];
       if (r.p < 1.f) {
-        const uint64_t reach = reach_of(r.p, ahead + between + found[1]);
+        uint64_t past = 0;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+          const int i = e * kThreads + threadIdx.x;
+          if (i < n && code[e] > cut) past += s.parts[i];
+        }
+        past = wave_sum(past);
+        if (lane == 0) s.scratch[wave] = past;
         __syncthreads();
-        if (threadIdx.x == 0) found[0] = 0;
+        past = 0;
+        for (int i = 0; i < kWaves; ++i) past += s.scratch[i];
+        const uint64_t reach = reach_of(r.p, all - past);
+        if (threadIdx.x == 0) s.found[0] = 0;
         __syncthreads();
 #pragma unroll
         for (int e = 0; e < kEach; ++e)
-          if (e * kThreads + (int)threadIdx.x < n && code[e] <= cut &&
-              ahead + (at[e] > high ? between : 0) + before[e] < reach)
-            atomicMax((unsigned long long *)&found[0], (unsigned long long)code[e]);
+          if (e * kThreads + (int)threadIdx.x < n && code[e] <= cut && at[e] <= c.high && ahead + before[e] < reach)
+            atomicMax((unsigned long long *)&s.found[0], (unsigned long long)code[e]);
         __syncthreads();
-        cut = found[0];
+        cut = s.found[0];
       }
 #pragma unroll
       for (int e = 0; e < kEach; ++e) {
         const int i = e * kThreads + threadIdx.x;
         if (i >= n) break;
         const uint64_t m = kept(unrank(~(uint32_t)(code[e] >> 32)), (int)(uint32_t)code[e], cut);
-        if (m) atomicAdd((unsigned long long *)&in_slice[(uint32_t)code[e] / len], (unsigned long long)m);
+        if (m) atomicAdd((unsigned long long *)&s.in_slice[(uint32_t)code[e] / len], (unsigned long long)m);
       }
     }
   } else {
-    if (r.k) cut = select_row<Z>(z, V, weigh, (uint64_t)r.k, false, cut, hist, scratch, found);
+    if (r.k) cut = select_row<Z>(z, V, weigh, (uint64_t)r.k, false, cut, s.hist, s.scratch, s.found);
     if (r.p < 1.f) {
       uint64_t mass = 0;
       for (int i = threadIdx.x; i < V; i += kThreads) {
@@ -564,19 +541,19 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleArgs a, int blocks
         if (code_of(rank_key(x), i) <= cut) mass += weigh.units(x);
       }
       mass = wave_sum(mass);
-      if (lane == 0) scratch[wave] = mass;
+      if (lane == 0) s.scratch[wave] = mass;
       __syncthreads();
       mass = 0;
-      for (int i = 0; i < kWaves; ++i) mass += scratch[i];
+      for (int i = 0; i < kWaves; ++i) mass += s.scratch[i];
       __syncthreads();
-      cut = select_row<Z>(z, V, weigh, reach_of(r.p, mass), true, cut, hist, scratch, found);
+      cut = select_row<Z>(z, V, weigh, reach_of(r.p, mass), true, cut, s.hist, s.scratch, s.found);
     }
-    for (int s = wave; s < kMaxSlices; s += kWaves) {
-      const int lo = min(V, s * len), hi = s < slices ? min(V, lo + len) : lo;
+    for (int i = wave; i < kMaxSlices; i += kWaves) {
+      const int lo = min(V, i * len), hi = i < slices ? min(V, lo + len) : lo;
       uint64_t mass = 0;
-      for (int i = lo + lane; i < hi; i += 64) mass += kept(logit<Z>(z, i), i, cut);
+      for (int j = lo + lane; j < hi; j += 64) mass += kept(logit<Z>(z, j), j, cut);
       mass = wave_sum(mass);
-      if (lane == 0) in_slice[s] = mass;
+      if (lane == 0) s.in_slice[i] = mass;
     }
   }
   __syncthreads();
@@ -585,29 +562,26 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleArgs a, int blocks
   constexpr int kPer = kMaxSlices / 64;
   uint64_t up = 0;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) up += in_slice[lane * kPer + i];
+  for (int i = 0; i < kPer; ++i) up += s.in_slice[lane * kPer + i];
   const uint64_t own = up;
   for (int o = 1; o < 64; o <<= 1) {
     const uint64_t v = __shfl_up((unsigned long long)up, o);
     if (lane >= o) up += v;
   }
   const uint64_t mass = __shfl((unsigned long long)up, 63);
-  const float u = a.u[row];
-  const double want = (double)u * (double)mass;
-  const uint64_t target = !(want > 0.0) ? 0 : want >= (double)mass ? mass - 1 : min(mass - 1, (uint64_t)want);
+  const uint64_t target = target_of(a.u[row], mass);
   const int at = max(0, __ffsll((unsigned long long)__ballot(target < up)) - 1);
   uint64_t before = __shfl((unsigned long long)(up - own), at);
   int slice = at * kPer;
-  for (int i = 1; i < kPer && target >= before + in_slice[slice]; ++i) before += in_slice[slice++];
+  for (int i = 1; i < kPer && target >= before + s.in_slice[slice]; ++i) before += s.in_slice[slice++];
   const int begin = min(V, slice * len), end = min(V, begin + len);
   const int run = (end - begin + kWaves - 1) / kWaves, lo = min(end, begin + wave * run), hi = min(end, lo + run);
   uint64_t mine = 0;
   for (int i = lo + lane; i < hi; i += 64) mine += kept(logit<Z>(z, i), i, cut);
   mine = wave_sum(mine);
+  if (lane == 0) s.scratch[wave] = mine;
   __syncthreads();
-  if (lane == 0) scratch[wave] = mine;
-  __syncthreads();
-  for (int i = 0; i < wave; ++i) before += scratch[i];
+  for (int i = 0; i < wave; ++i) before += s.scratch[i];
   if (target < before || target >= before + mine) return;
   for (int base = lo; base < hi; base += 64) {
     const int i = base + lane;
@@ -626,6 +600,223 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleArgs a, int blocks
   }
 }
 
+// Rows that need no weights: nothing to choose from; the first largest is chosen; infinite logits
+// share all of the mass evenly: the filters keep the first so many of them.  By the whole block.
+template <class Z>
+__device__ __forceinline__ bool settled(const SampleArgs &a, int row, const void *z, const Row &r, uint64_t *scratch) {
+  if (!r.none && !r.greedy && !r.wild) return false;
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, V = a.vocab;
+  int token = r.none ? -1 : r.first;
+  float prob = r.none ? 0.f : 1.f;
+  if (r.wild && !r.greedy) {
+    uint64_t n = 0;
+    for (int i = threadIdx.x; i < V; i += kThreads) n += logit<Z>(z, i) == r.top;
+    n = wave_sum(n);
+    __syncthreads();
+    if (lane == 0) scratch[wave] = n;
+    __syncthreads();
+    n = 0;
+    for (int i = 0; i < kWaves; ++i) n += scratch[i];
+    if (r.k) n = min(n, (uint64_t)r.k);
+    if (r.p < 1.f) n = reach_of(r.p, n);
+    const uint64_t target = target_of(a.u[row], n);
+    uint64_t seen = 0;
+    for (int base = 0; base < V; base += kThreads) {
+      const int i = base + threadIdx.x;
+      const bool hit = i < V && logit<Z>(z, i) == r.top;
+      const uint64_t mask = __ballot(hit);
+      __syncthreads();
+      if (lane == 0) scratch[wave] = __popcll(mask);
+      __syncthreads();
+      uint64_t before = seen + __popcll(mask & ((1ull << lane) - 1));
+      for (int w = 0; w < kWaves; ++w) {
+        if (w < wave) before += scratch[w];
+        seen += scratch[w];
+      }
+      if (hit && before == target) {
+        a.token[row] = i;
+        if (a.prob) a.prob[row] = (float)(1.0 / (double)n);
+      }
+      if (seen > target) break;
+    }
+    return true;
+  }
+  if (threadIdx.x == 0) {
+    a.token[row] = token;
+    if (a.prob) a.prob[row] = prob;
+  }
+  return true;
+}
+
+// ---------------------------------------------------------------------------------------------
+// Rows of up to kWhole elements: a block per row takes all steps in one launch (each goes over the
+// row again, from the CU's XCD's L2), a slice's quarter to a wave at a time.
+// ---------------------------------------------------------------------------------------------
+constexpr int kWhole = 8192, kRowSlices = 4 * kWaves;
+
+template <class Z>
+__global__ __launch_bounds__(kThreads, 4) void row_kernel(SampleArgs a, int shift) {
+  __shared__ Last s;
+  const int row = blockIdx.x, V = a.vocab, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const void *z = (const Z *)a.logits + (int64_t)row * a.stride;
+  const int len = (V + kRowSlices - 1) / kRowSlices;
+  const int lo = min(V, 4 * wave * len), hi = min(V, lo + 4 * len);
+  uint64_t best = largest_of<Z>(z, lo, hi);
+  if (lane == 0) s.scratch[wave] = best;
+  for (int i = threadIdx.x; i < kBins; i += kThreads) s.mass[i] = 0, s.count[i] = 0;
+  if (threadIdx.x < kMaxSlices) s.in_slice[threadIdx.x] = 0;
+  if (threadIdx.x == 0) s.n = 0;
+  __syncthreads();
+  for (int i = 0; i < kWaves; ++i) best = max(best, s.scratch[i]);
+  const Row r(a, row, best);
+  if (settled<Z>(a, row, z, r, s.scratch)) return;
+  Cuts c{kBins, kBins, kBins, 0};
+  if (r.ranked()) {
+    bin_elements<Z>(z, lo, hi, r, shift, s.mass, s.count);
+    __syncthreads();
+    uint64_t mass[kBins / kThreads];
+    uint32_t count[kBins / kThreads];
+#pragma unroll
+    for (int i = 0; i < kBins / kThreads; ++i) {
+      mass[i] = s.mass[threadIdx.x * (kBins / kThreads) + i];
+      count[i] = s.count[threadIdx.x * (kBins / kThreads) + i];
+    }
+    c = find_cuts<kThreads>(mass, count, r, V);
+  }
+  __syncthreads();  // `scratch` and the bins have been read
+  uint64_t all = 0, ahead = 0;
+#pragma unroll 1
+  for (int i = 0; i < 4; ++i) {
+    const int begin = min(hi, lo + i * len);
+    const Masses m = weigh_elements<Z>(z, begin, min(hi, begin + len), r, c, shift,
+                                       [&](uint64_t code) __attribute__((always_inline)) {
+                                         const int at = atomicAdd(&s.n, 1);
+                                         if (at < kCandidates) s.codes[at] = code;
+                                       });
+    all += m.all, ahead += m.ahead;
+    if (lane == 0) s.in_slice[4 * wave + i] = m.kept;
+  }
+  if (lane == 0) s.scratch[wave] = all, s.hist[wave] = ahead;
+  __syncthreads();
+  all = ahead = 0;
+  for (int i = 0; i < kWaves; ++i) all += s.scratch[i], ahead += s.hist[i];
+  const int n = s.n;
+  __syncthreads();
+  rank_and_draw<Z>(a, row, z, r, c, n, all, ahead, kRowSlices, len, shift, s);
+}
+
+// ---------------------------------------------------------------------------------------------
+// Longer rows: slices of a row over several blocks, a launch per step.
+// ---------------------------------------------------------------------------------------------
+// Step 1, a wave per slice: the largest logit; the row's bins are cleared on the way.
+template <class Z>
+__global__ __launch_bounds__(kSliceThreads) void largest_kernel(SampleArgs a, int len) {
+  RowWork &w = ((RowWork *)a.work)[blockIdx.y];
+  const void *z = (const Z *)a.logits + (int64_t)blockIdx.y * a.stride;
+  const int lo = min(a.vocab, (int)(blockIdx.x * kSliceWaves + threadIdx.x / 64) * len);
+  for (int i = blockIdx.x * kSliceThreads + threadIdx.x; i < kBins; i += gridDim.x * kSliceThreads)
+    w.mass[i] = 0, w.count[i] = 0;
+  if (blockIdx.x == 0 && threadIdx.x == 0) w.n_list = 0;
+  __shared__ uint64_t scratch[kSliceWaves];
+  uint64_t best = largest_of<Z>(z, lo, min(a.vocab, lo + len));
+  if (threadIdx.x % 64 == 0) scratch[threadIdx.x / 64] = best;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < kSliceWaves; ++i) best = max(best, scratch[i]);
+    w.best[blockIdx.x] = best;
+  }
+}
+
+// Step 2, for rows with a filter by rank: the bins, kWaves slices to a block (each block adds its bins
+// to the row's one by one).
+template <class Z>
+__global__ __launch_bounds__(kThreads) void bins_kernel(SampleArgs a, int blocks, int len, int shift) {
+  RowWork &w = ((RowWork *)a.work)[blockIdx.y];
+  const Row r(a, blockIdx.y, row_best(w, blocks));
+  if (r.none || r.greedy || r.wild || !r.ranked()) return;
+  __shared__ uint64_t mass[kBins];
+  __shared__ uint32_t count[kBins];
+  for (int i = threadIdx.x; i < kBins; i += kThreads) mass[i] = 0, count[i] = 0;
+  __syncthreads();
+  const void *z = (const Z *)a.logits + (int64_t)blockIdx.y * a.stride;
+  const int lo = min(a.vocab, (int)(blockIdx.x * kWaves + threadIdx.x / 64) * len);
+  bin_elements<Z>(z, lo, min(a.vocab, lo + len), r, shift, mass, count);
+  __syncthreads();
+  for (int i = threadIdx.x; i < kBins; i += kThreads) {
+    if (mass[i]) atomicAdd((unsigned long long *)&w.mass[i], (unsigned long long)mass[i]);
+    if (count[i]) atomicAdd(&w.count[i], count[i]);
+  }
+}
+
+// Step 3: the cuts' bins (every block of a row finds them for itself), their elements into the row's
+// list, each slice's exact masses.
+template <class Z>
+__global__ __launch_bounds__(kSliceThreads) void collect_kernel(SampleArgs a, int len, int shift) {
+  RowWork &w = ((RowWork *)a.work)[blockIdx.y];
+  constexpr int kPer = kBins / kSliceThreads;
+  uint64_t mass[kPer];  // asked for together with the row's settings
+  uint32_t count[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    mass[i] = w.mass[threadIdx.x * kPer + i];
+    count[i] = w.count[threadIdx.x * kPer + i];
+  }
+  const Row r(a, blockIdx.y, row_best(w, gridDim.x));
+  if (r.none || r.greedy || r.wild) return;
+  __shared__ uint64_t mine[kOwn];
+  __shared__ int n_mine, place;
+  if (threadIdx.x == 0) n_mine = 0;
+  Cuts c{kBins, kBins, kBins, 0};
+  if (r.ranked()) c = find_cuts<kSliceThreads>(mass, count, r, a.vocab);
+  if (blockIdx.x == 0 && threadIdx.x == 0) w.cuts = c;
+  __syncthreads();
+  const void *z = (const Z *)a.logits + (int64_t)blockIdx.y * a.stride;
+  const int slice = blockIdx.x * kSliceWaves + threadIdx.x / 64, lo = min(a.vocab, slice * len);
+  const Masses m = weigh_elements<Z>(z, lo, min(a.vocab, lo + len), r, c, shift,
+                                     [&](uint64_t code) __attribute__((always_inline)) {
+                                       const int at = atomicAdd(&n_mine, 1);
+                                       if (at < kOwn) {
+                                         mine[at] = code;
+                                       } else {
+                                         const int far = atomicAdd(&w.n_list, 1);
+                                         if (far < kCandidates) w.list[far] = code;
+                                       }
+                                     });
+  if (threadIdx.x % 64 == 0) w.sums[slice] = m;
+  __syncthreads();
+  if (threadIdx.x == 0 && n_mine) place = atomicAdd(&w.n_list, min(n_mine, kOwn));
+  __syncthreads();
+  for (int i = threadIdx.x; i < min(n_mine, kOwn); i += kSliceThreads)
+    if (place + i < kCandidates) w.list[place + i] = mine[i];
+}
+
+// Step 4, a block per row.
+template <class Z>
+__global__ __launch_bounds__(kThreads) void draw_kernel(SampleArgs a, int blocks, int len, int shift) {
+  __shared__ Last s;
+  const int row = blockIdx.x, lane = threadIdx.x % 64, wave = threadIdx.x / 64, slices = blocks * kSliceWaves;
+  const RowWork &w = ((const RowWork *)a.work)[row];
+  const void *z = (const Z *)a.logits + (int64_t)row * a.stride;
+  const Row r(a, row, row_best(w, blocks));
+  if (settled<Z>(a, row, z, r, s.scratch)) return;
+  static_assert(kMaxSlices <= kThreads && kMaxSlices / 64 <= kWaves, "a thread per slice");
+  if (threadIdx.x < kMaxSlices) {
+    const Masses m = (int)threadIdx.x < slices ? w.sums[threadIdx.x] : Masses{0, 0, 0};
+    s.in_slice[threadIdx.x] = m.kept;
+    const uint64_t all = wave_sum(m.all), ahead = wave_sum(m.ahead);
+    if (lane == 0) s.scratch[wave] = all, s.hist[wave] = ahead;
+  }
+  const Cuts c = w.cuts;
+  const int n = r.ranked() ? w.n_list : 0;
+  for (int i = threadIdx.x; i < min(n, kCandidates); i += kThreads) s.codes[i] = w.list[i];
+  __syncthreads();
+  uint64_t all = 0, ahead = 0;
+#pragma unroll
+  for (int i = 0; i < kMaxSlices / 64; ++i) all += s.scratch[i], ahead += s.hist[i];
+  __syncthreads();
+  rank_and_draw<Z>(a, row, z, r, c, n, all, ahead, slices, len, shift, s);
+}
+
 // Blocks for a row's passes: about 1024 over all rows, each wave with at least 256 elements.
 void split_row(int rows, int vocab, int *blocks, int *len) {
   int n = (1024 + rows - 1) / rows;
@@ -639,6 +830,10 @@ template <class Z>
 hipError_t launch(const SampleArgs &a, hipStream_t s) {
   int shift = 50, blocks, len;
   while ((int64_t)1 << (62 - shift) < a.vocab) --shift;
+  if (a.vocab <= kWhole) {
+    void *args[] = {const_cast<SampleArgs *>(&a), &shift};
+    return hipLaunchKernel((const void *)row_kernel<Z>, dim3(a.rows), dim3(kThreads), args, 0, s);
+  }
   split_row(a.rows, a.vocab, &blocks, &len);
   const dim3 grid(blocks, a.rows);
   void *first[] = {const_cast<SampleArgs *>(&a), &len}, *then[] = {const_cast<SampleArgs *>(&a), &len, &shift};
@@ -654,7 +849,7 @@ hipError_t launch(const SampleArgs &a, hipStream_t s) {
 
 }  // namespace
 
-size_t sample_work_bytes(int rows) { return (size_t)rows * sizeof(RowWork); }
+size_t sample_work_bytes(int rows, int vocab) { return vocab <= kWhole ? 0 : (size_t)rows * sizeof(RowWork); }
 
 hipError_t launch_sample(const SampleArgs &a, int type, hipStream_t s) {
   return type == 0 ? launch<float>(a, s) : type == 1 ? launch<__bf16>(a, s) : launch<_Float16>(a, s);

@@ -204,9 +204,9 @@ int moe_kv_attend(const moe_kv_batch *b, int32_t window, float scale, const void
 
 int moe_sample_workspace(const moe_sample_batch *b, uint64_t *bytes) {
   if (!b || !bytes) return fail(MOE_EINVAL, "moe_sample_workspace: the batch or bytes is NULL");
-  if (b->n_rows < 0 || b->n_rows > kMaxSampleRows)
-    return fail(MOE_EINVAL, "moe_sample_workspace: n_rows must be in [0, 65535]");
-  *bytes = sample_work_bytes(b->n_rows);
+  if (b->n_rows < 0 || b->n_rows > kMaxSampleRows || b->vocab < 1 || b->vocab > 1 << 20)
+    return fail(MOE_EINVAL, "moe_sample_workspace: n_rows must be in [0, 65535] and vocab in [1, 2^20]");
+  *bytes = sample_work_bytes(b->n_rows, b->vocab);
   return MOE_OK;
 }
 
@@ -220,9 +220,10 @@ int moe_sample(const moe_sample_batch *b, int32_t *token, float *prob, void *wor
   if (!b->logits || !b->u || !token) return fail(MOE_EINVAL, "moe_sample: logits, u and token must not be NULL");
   if (b->row_stride < b->vocab || b->row_stride > (int64_t)1 << 32)
     return fail(MOE_EINVAL, "moe_sample: row_stride must be at least vocab");
-  if (!workspace || !aligned(workspace) || workspace_bytes < sample_work_bytes(b->n_rows))
+  const uint64_t bytes = sample_work_bytes(b->n_rows, b->vocab);
+  if (bytes && (!workspace || !aligned(workspace) || workspace_bytes < bytes))
     return fail(MOE_EINVAL, "moe_sample: the workspace must be 16-byte aligned and of at least %llu bytes",
-                (unsigned long long)sample_work_bytes(b->n_rows));
+                (unsigned long long)bytes);
   const uintptr_t size = b->dtype == MOE_F32 ? 4 : 2;
   if ((uintptr_t)b->logits % size) return fail(MOE_EINVAL, "moe_sample: logits are not aligned to their elements");
   const SampleArgs a{b->logits, b->row_stride, b->n_rows, b->vocab, b->temperature, b->top_p, b->min_p,

@@ -64,9 +64,9 @@ struct SampleArgs {
   const float *u;                            // [rows]
   int32_t *token;                            // [rows]
   float *prob;                               // [rows], nullable
-  void *work;                                // sample_work_bytes(rows)
+  void *work;                                // sample_work_bytes
 };
-size_t sample_work_bytes(int rows);
+size_t sample_work_bytes(int rows, int vocab);
 // type of the logits: 0 fp32, 1 bf16, 2 fp16
 hipError_t launch_sample(const SampleArgs &a, int type, hipStream_t s);
 

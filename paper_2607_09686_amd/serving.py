@@ -232,18 +232,18 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None):
         b.min_p = _vector(min_p, "min_p", f32, n, dev)
     b.u = _vector(u, "u", f32, n, dev)
     b.hip_stream = _stream(dev.index)
-    size = _sample_bytes.get(n)
+    size = _sample_bytes.get((n, vocab))
     if size is None:
         need = ctypes.c_uint64()
         _check(lib().moe_sample_workspace(b, need))
         if len(_sample_bytes) > 4096:
             _sample_bytes.clear()
-        size = _sample_bytes[n] = need.value
+        size = _sample_bytes[n, vocab] = need.value
     tokens = torch.empty(n, dtype=torch.int32, device=dev)
     probs = torch.empty(n, dtype=f32, device=dev)
-    work = torch.empty(size, dtype=torch.uint8, device=dev)
-    _run(dev.index, lib().moe_sample, b, tokens.data_ptr(), probs.data_ptr(), work.data_ptr(), size)
+    work = torch.empty(size, dtype=torch.uint8, device=dev) if size else None
+    _run(dev.index, lib().moe_sample, b, tokens.data_ptr(), probs.data_ptr(), work.data_ptr() if size else None, size)
     return tokens, probs
 
 
-_sample_bytes = {}  # rows: bytes of moe_sample's workspace
+_sample_bytes = {}  # (rows, vocab): bytes of moe_sample's workspace

@@ -44,7 +44,7 @@ def random_rows(torch, rows, vocab, dtype, seed):
 
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
 @pytest.mark.parametrize("rows,vocab", [(1, 1), (3, 2), (5, 63), (4, 64), (4, 65), (9, 1000), (3, 4097), (2, 32003),
-                                        (70, 5001), (2, 152001), (1, 262144)])
+                                        (70, 5001), (3, 32768), (3, 32769), (2, 152001), (1, 262144)])
 def test_random_rows_and_settings(dtype, rows, vocab):
     torch = torch_cuda()
     log(f"sample {rows} x {vocab} {dtype}")
@@ -75,7 +75,7 @@ def test_ties():
     """Rows of few distinct logits: the filters cut inside runs of equal ones."""
     torch = torch_cuda()
     rng = np.random.default_rng(2)
-    for vocab in (7, 3000, 70000):
+    for vocab in (7, 3000, 30000, 70000):
         z = torch.from_numpy(rng.integers(-2, 3, (24, vocab)).astype(np.float32)).cuda()
         z[0] = 0.0
         z[1] = 0.0

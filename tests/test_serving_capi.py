@@ -80,10 +80,10 @@ def test_nothing_to_do_is_no_error(mc):
 
 def test_bad_arguments_of_sample(mc):
     L, p = mc.lib(), 1 << 12
-    base = dict(dtype=mc.MOE_F32, n_rows=2, vocab=100, pad=0, logits=p, row_stride=100, temperature=None, top_k=None,
+    base = dict(dtype=mc.MOE_F32, n_rows=2, vocab=100000, pad=0, logits=p, row_stride=100000, temperature=None, top_k=None,
                 top_p=None, min_p=None, u=p, hip_stream=None)
     for change in (dict(dtype=7), dict(vocab=0), dict(vocab=(1 << 20) + 1), dict(n_rows=-1), dict(n_rows=65536),
-                   dict(logits=None), dict(u=None), dict(row_stride=99), dict(row_stride=-100),
+                   dict(logits=None), dict(u=None), dict(row_stride=99999), dict(row_stride=-100),
                    dict(row_stride=(1 << 32) + 1), dict(logits=p + 2)):
         s = mc.SampleBatch(**dict(base, **change))
         assert L.moe_sample(ctypes.byref(s), p, p, p, 1 << 40) == mc.MOE_EINVAL, change
@@ -96,6 +96,11 @@ def test_bad_arguments_of_sample(mc):
         b = None if args[0] is None else ctypes.byref(args[0])
         assert L.moe_sample(b, *args[1:]) == mc.MOE_EINVAL
     assert L.moe_sample(ctypes.byref(mc.SampleBatch(**dict(base, n_rows=0))), None, None, None, 0) == mc.MOE_OK
+    short = mc.SampleBatch(**dict(base, vocab=100))
+    assert L.moe_sample_workspace(ctypes.byref(short), ctypes.byref(size)) == mc.MOE_OK and size.value == 0
+    for change in (dict(vocab=0), dict(vocab=(1 << 20) + 1), dict(n_rows=65536)):
+        s = mc.SampleBatch(**dict(base, **change))
+        assert L.moe_sample_workspace(ctypes.byref(s), ctypes.byref(size)) == mc.MOE_EINVAL
 
 
 def test_the_cache_refuses_what_it_cannot_hold(mc):
