@@ -93,61 +93,144 @@ __device__ __forceinline__ int units_of(const AttendArgs &a, int span, int C) {
 }
 __device__ __forceinline__ int share_of(int keys, int units) { return ((keys + units - 1) / units + 63) & ~63; }
 
-// Keys of a unit, from the whole batch.  `mine` is sequence threadIdx.x % 64 where there is one.
-// All lanes of a wave get the same value.
-template <int M>
-__device__ __forceinline__ int plan_keys(const AttendArgs &a, const Seq &mine) {
-  int64_t work = (int64_t)tiles_of<M>(a, mine) * span_of<M>(a, mine);
-  for (int s = threadIdx.x % kLanes + kLanes; s < a.kv.n_seqs; s += kLanes) {
-    const Seq q = seq_of(a.kv, s);
-    work += (int64_t)tiles_of<M>(a, q) * span_of<M>(a, q);
-  }
-  for (int o = 1; o < min(kLanes, a.kv.n_seqs); o <<= 1) work += __shfl_xor(work, o);
-  work = __shfl(work, 0);  // lanes past the sequences have their own sums of nothing
+// The workspace: how many tiles were split, with a plan_kernel the keys of a unit, a note of each split
+// tile, then the plan, then the o rows of slot (slot, kvh), then (m, l) pairs of all slots.
+struct SplitTile {
+  int32_t slot, units;        // its first partial result, and their number
+  int32_t first, row0, rows;  // its sequence's first token row, the tile's first row in the sequence, its rows
+  int32_t pad[3];
+};
+struct SplitTiles {
+  int32_t count, keys, pad[6];
+  SplitTile tile[];
+};
+constexpr int kPlanSeqs = kLanes;  // sequences up to which every block plans for itself
+__host__ __device__ inline int64_t plan_ints(const AttendArgs &a) {  // a multiple of 16 bytes
+  return a.kv.n_seqs > kPlanSeqs ? (3 * ((int64_t)a.kv.n_seqs + 1) + 3) & ~(int64_t)3 : 0;
+}
+__device__ __forceinline__ SplitTiles *split_tiles(const AttendArgs &a) { return (SplitTiles *)a.work; }
+// units, slots and split tiles before every sequence, and in all
+__device__ __forceinline__ int32_t *plan_of(const AttendArgs &a, int which) {
+  return (int32_t *)((uint8_t *)a.work + sizeof(SplitTiles) + a.max_tiles * sizeof(SplitTile)) +
+         which * (int64_t)(a.kv.n_seqs + 1);
+}
+__device__ __forceinline__ float *part_base(const AttendArgs &a) { return (float *)(plan_of(a, 0) + plan_ints(a)); }
+
+// Keys of a unit, for tiles that span `work` keys together.
+__device__ __forceinline__ int keys_of(const AttendArgs &a, int64_t work) {
   const int64_t c = (work * a.kv.kv_heads + a.target - 1) / a.target;
   return (int)min((int64_t)1 << 30, max((int64_t)a.min_keys, (c + 63) & ~(int64_t)63));
+}
+
+// What a sequence adds to the plan: units, slots (units of split tiles), split tiles.  No batch has
+// 2^24 units: only starts out of order could add up to more, and then sums stay below 2^31.
+struct Share {
+  int units, slots, tiles;
+};
+template <int M>
+__device__ __forceinline__ Share share_of_seq(const AttendArgs &a, const Seq &q, int C) {
+  const int per = units_of(a, span_of<M>(a, q), C);
+  const int n = (int)min((int64_t)1 << 24, (int64_t)tiles_of<M>(a, q) * per);
+  return per > 1 ? Share{n, n, n / per} : Share{n, 0, 0};
+}
+// Inclusive sums over the first `lanes` lanes.
+__device__ __forceinline__ Share scan(Share s, int lanes) {
+  const int lane = threadIdx.x % kLanes;
+  for (int o = 1; o < lanes; o <<= 1) {
+    const int u = __shfl_up(s.units, o), v = __shfl_up(s.slots, o), w = __shfl_up(s.tiles, o);
+    if (lane >= o) s.units += u, s.slots += v, s.tiles += w;
+  }
+  return s;
 }
 
 // Where a unit stands: its sequence and its number among the sequence's units; the split tiles and
 // the units of split tiles in the sequences before.
 struct Place {
-  int seq, index;
-  int64_t tiles, slots;
+  int seq, index, tiles, slots;
   Seq q;
 };
+
+// Up to kPlanSeqs sequences: every wave plans for itself, a sequence to a lane, which saves a launch
+// (64 sequences of 3000 keys: 70 us, with plan_kernel 76; one sequence: 14 and 18).  In rounds over more
+// sequences it would cost every block: 1024 of 400 keys took 277 us, with plan_kernel 145; 4096 of
+// 200 took 2325, now 371.
 template <int M>
-__device__ __forceinline__ bool plan_find(const AttendArgs &a, const Seq &mine, int C, int want, Place *out) {
-  int64_t units = 0, tiles = 0, slots = 0;
-  const int lane = threadIdx.x % kLanes;
-  for (int s0 = 0; s0 < a.kv.n_seqs; s0 += kLanes) {
-    Seq q = mine;
-    if (s0) q = s0 + lane < a.kv.n_seqs ? seq_of(a.kv, s0 + lane) : Seq{0, 0, 0, false};
-    const int per = units_of(a, span_of<M>(a, q), C);
-    // (no batch has 2^24 units: only starts out of order could add up to more)
-    const int n = (int)min((int64_t)1 << 24, (int64_t)tiles_of<M>(a, q) * per), m = per > 1 ? n : 0;
-    const int t = per > 1 ? n / per : 0;
-    int nu = n, ns = m, nt = t;  // inclusive prefix sums over the lanes
-    const int lanes = min(kLanes, a.kv.n_seqs - s0);
-    for (int o = 1; o < lanes; o <<= 1) {
-      const int u = __shfl_up(nu, o), v = __shfl_up(ns, o), w = __shfl_up(nt, o);
-      if (lane >= o) nu += u, ns += v, nt += w;
-    }
-    const uint64_t any = __ballot(lane < lanes && want < units + nu);
-    if (any) {
-      const int at = __ffsll((unsigned long long)any) - 1;
-      out->seq = s0 + at;
-      out->index = (int)(want - (units + __shfl(nu - n, at)));
-      out->slots = slots + __shfl(ns - m, at);
-      out->tiles = tiles + __shfl(nt - t, at);
-      out->q = Seq{__shfl(q.first, at), __shfl(q.count, at), __shfl(q.length, at), (bool)__shfl((int)q.bad, at)};
-      return true;
-    }
-    units += __shfl(nu, lanes - 1);
-    slots += __shfl(ns, lanes - 1);
-    tiles += __shfl(nt, lanes - 1);
+__device__ __forceinline__ bool plan_here(const AttendArgs &a, int unit, bool last, int *C, Place *out) {
+  const int lane = threadIdx.x % kLanes, lanes = min(kLanes, a.kv.n_seqs);
+  const Seq q = lane < lanes ? seq_of(a.kv, lane) : Seq{0, 0, 0, false};
+  int64_t work = (int64_t)tiles_of<M>(a, q) * span_of<M>(a, q);
+  for (int o = 1; o < lanes; o <<= 1) work += __shfl_xor(work, o);
+  *C = keys_of(a, __shfl(work, 0));  // lanes past the sequences have sums of nothing
+  const Share own = share_of_seq<M>(a, q, *C), sum = scan(own, lanes);
+  if (last) split_tiles(a)->count = min(a.max_tiles, __shfl(sum.tiles, lanes - 1));
+  const uint64_t any = __ballot(lane < lanes && unit < sum.units);
+  if (!any) return false;
+  const int at = __ffsll((unsigned long long)any) - 1;
+  out->seq = at;
+  out->index = unit - __shfl(sum.units - own.units, at);
+  out->slots = __shfl(sum.slots - own.slots, at);
+  out->tiles = __shfl(sum.tiles - own.tiles, at);
+  out->q = Seq{__shfl(q.first, at), __shfl(q.count, at), __shfl(q.length, at), (bool)__shfl((int)q.bad, at)};
+  return true;
+}
+
+// More sequences: one block plans for all, and a unit's sequence is searched for, 64 at a time.
+constexpr int kPlanThreads = 1024;
+template <int M>
+__global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a) {
+  constexpr int kW = kPlanThreads / kLanes;
+  __shared__ int64_t works[kW];
+  __shared__ Share sums[kW];
+  const int lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes, n = a.kv.n_seqs;
+  int64_t work = 0;
+  for (int s = threadIdx.x; s < n; s += kPlanThreads) {
+    const Seq q = seq_of(a.kv, s);
+    work += (int64_t)tiles_of<M>(a, q) * span_of<M>(a, q);
   }
-  out->tiles = tiles;
-  return false;
+  for (int o = 1; o < kLanes; o <<= 1) work += __shfl_xor(work, o);
+  if (lane == 0) works[wave] = work;
+  __syncthreads();
+  work = 0;
+  for (int i = 0; i < kW; ++i) work += works[i];
+  const int C = keys_of(a, work);
+  int32_t *units = plan_of(a, 0), *slots = plan_of(a, 1), *tiles = plan_of(a, 2);
+  constexpr int64_t kMost = 1 << 30;
+  int64_t nu = 0, ns = 0, nt = 0;
+  for (int s0 = 0; s0 < n; s0 += kPlanThreads) {
+    const int s = s0 + threadIdx.x;
+    const Share own = s < n ? share_of_seq<M>(a, seq_of(a.kv, s), C) : Share{0, 0, 0}, sum = scan(own, kLanes);
+    __syncthreads();
+    if (lane == kLanes - 1) sums[wave] = sum;
+    __syncthreads();
+    int64_t u = nu + sum.units - own.units, v = ns + sum.slots - own.slots, w = nt + sum.tiles - own.tiles;
+    for (int i = 0; i < kW; ++i) {
+      if (i < wave) u += sums[i].units, v += sums[i].slots, w += sums[i].tiles;
+      nu += sums[i].units, ns += sums[i].slots, nt += sums[i].tiles;
+    }
+    if (s < n) units[s] = (int)min(u, kMost), slots[s] = (int)min(v, kMost), tiles[s] = (int)min(w, kMost);
+  }
+  if (threadIdx.x == 0) {
+    units[n] = (int)min(nu, kMost);
+    split_tiles(a)->count = (int)min((int64_t)a.max_tiles, nt);
+    split_tiles(a)->keys = C;
+  }
+}
+template <int M>
+__device__ __forceinline__ bool plan_search(const AttendArgs &a, int unit, int *C, Place *out) {
+  const int32_t *units = plan_of(a, 0);
+  *C = split_tiles(a)->keys;
+  if (unit >= units[a.kv.n_seqs]) return false;
+  const int lane = threadIdx.x % kLanes;
+  int lo = 0, hi = a.kv.n_seqs;  // the last sequence that begins at or before the unit
+  while (hi - lo > 1) {
+    const int step = (hi - lo + kLanes - 1) / kLanes, at = lo + lane * step;
+    const uint64_t in = __ballot(at < hi && units[at] <= unit);
+    const int k = in ? kLanes - 1 - __clzll((long long)in) : 0;
+    lo += k * step;
+    hi = min(hi, lo + step);
+  }
+  *out = Place{lo, unit - units[lo], plan_of(a, 2)[lo], plan_of(a, 1)[lo], seq_of(a.kv, lo)};
+  return true;
 }
 
 // Keys lo .. hi - 1 that rows of a tile see, lo rounded down to a multiple of 64; the tile's units
@@ -311,21 +394,6 @@ __device__ __forceinline__ void store_out(const AttendArgs &a, const Seq &q, int
   *(typename Vec<E>::x4 *)((E *)a.out + (int64_t)tok * a.out_stride + (int64_t)head * D + d) = e;
 }
 
-// The workspace: how many tiles were split (written by the last block), a note of each, then the
-// o rows of slot (slot, kvh), then (m, l) pairs of all slots.
-struct SplitTile {
-  int32_t slot, units;        // its first partial result, and their number
-  int32_t first, row0, rows;  // its sequence's first token row, the tile's first row in the sequence, its rows
-  int32_t pad[3];
-};
-struct SplitTiles {
-  int32_t count, pad[7];
-  SplitTile tile[];
-};
-__device__ __forceinline__ SplitTiles *split_tiles(const AttendArgs &a) { return (SplitTiles *)a.work; }
-__device__ __forceinline__ float *part_base(const AttendArgs &a) {
-  return (float *)((uint8_t *)a.work + sizeof(SplitTiles) + a.max_tiles * sizeof(SplitTile));
-}
 template <int D, int M>
 __device__ __forceinline__ float *part_o(const AttendArgs &a, int64_t slot, int kvh, int row) {
   return part_base(a) + ((slot * a.kv.kv_heads + kvh) * M + row) * D;
@@ -359,25 +427,16 @@ struct Unit {
 };
 template <int M>
 __device__ __forceinline__ bool unit_of(const AttendArgs &a, Unit *u) {
-  const int lane = threadIdx.x % kLanes;
-  Seq mine{0, 0, 0, false};
-  if (lane < a.kv.n_seqs) mine = seq_of(a.kv, lane);
-  const int C = plan_keys<M>(a, mine);
   Place pl;
+  int C;
   u->kvh = blockIdx.x % a.kv.kv_heads;
   const int unit = blockIdx.x / a.kv.kv_heads;
-  const bool found = plan_find<M>(a, mine, C, unit, &pl);
-  if (unit == a.max_units - 1 && u->kvh == 0 && threadIdx.x == 0) {
-    // the grid's last unit lies past the batch's last one, or is it
-    int64_t count = pl.tiles;
-    if (found) {
-      const int per = units_of(a, span_of<M>(a, pl.q), C);
-      if (per > 1) count += tiles_of<M>(a, pl.q);
-    }
-    split_tiles(a)->count = (int)min((int64_t)a.max_tiles, count);
-  }
+  const bool found = a.kv.n_seqs > kPlanSeqs
+                         ? plan_search<M>(a, unit, &C, &pl)
+                         : plan_here<M>(a, unit, blockIdx.x == 0 && threadIdx.x < kLanes, &C, &pl);
   if (!found) return false;
   const int per = units_of(a, span_of<M>(a, pl.q), C);
+  if (pl.index >= (int64_t)tiles_of<M>(a, pl.q) * per) return false;  // starts out of order
   // the tiles with the most keys first
   const int order = pl.index / per, split = pl.index % per;
   u->seq = pl.seq;
@@ -391,7 +450,7 @@ __device__ __forceinline__ bool unit_of(const AttendArgs &a, Unit *u) {
   u->slot = real > 1 ? pl.slots + pl.index : -1;
   if (per > 1) {
     // starts out of order can ask for more than there are
-    if (pl.slots + (int64_t)(order + 1) * per > a.max_slots || pl.tiles + order >= a.max_tiles) return false;
+    if ((int64_t)pl.slots + (int64_t)(order + 1) * per > a.max_slots || pl.tiles + order >= a.max_tiles) return false;
     if (split == 0 && u->kvh == 0 && threadIdx.x == 0)
       split_tiles(a)->tile[pl.tiles + order] =
           SplitTile{(int)(pl.slots + pl.index), real, pl.q.first, u->tile * M,
@@ -744,7 +803,7 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
 
 }  // namespace
 static inline uint64_t attend_work_size(const AttendArgs &a, int rows, int dim) {
-  return sizeof(SplitTiles) + a.max_tiles * sizeof(SplitTile) +
+  return sizeof(SplitTiles) + a.max_tiles * sizeof(SplitTile) + plan_ints(a) * sizeof(int32_t) +
          (uint64_t)a.max_slots * a.kv.kv_heads * rows * (dim + 2) * sizeof(float);
 }
 namespace {
@@ -758,7 +817,9 @@ hipError_t launch_kernels(const AttendArgs &a, hipStream_t s) {
     fn = (const void *)attend_many_kernel<E, D>;
   else
     fn = (const void *)attend_few_kernel<E, D, M / 32>;
-  hipError_t e = hipLaunchKernel(fn, grid, dim3(kThreads), args, 0, s);
+  hipError_t e = hipSuccess;
+  if (a.kv.n_seqs > kPlanSeqs) e = hipLaunchKernel((const void *)plan_kernel<M>, dim3(1), dim3(kPlanThreads), args, 0, s);
+  if (e == hipSuccess) e = hipLaunchKernel(fn, grid, dim3(kThreads), args, 0, s);
   if (e != hipSuccess) return e;
   // most blocks have nothing to join: about 4096 in all, 8 to M / 4 of them to a tile
   const int tiles = a.max_tiles * a.kv.kv_heads;

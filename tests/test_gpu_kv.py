@@ -224,6 +224,75 @@ def test_starts_out_of_order_stay_in_bounds():
         assert (whole[:32] == 7).all() and (whole[32 + b.n:] == 7).all()
 
 
+def test_starts_out_of_order_of_many_sequences():
+    torch = torch_cuda()
+    rng = np.random.default_rng(10)
+    for trial in range(6):
+        b = Batch(torch, [(1, 40)] * 90 + [(60, 9)] * 3, 4, 2, 64, 16, torch.bfloat16, seed=trial)
+        n = len(b.seqs) + 1
+        wrong = rng.integers(-2 ** 31, 2 ** 31 - 1, n) if trial % 2 else rng.integers(-5, b.n + 5, n)
+        b.starts = torch.tensor(wrong, dtype=torch.int32, device="cuda")
+        whole = torch.full((b.n + 64, 4, 64), 7.0, dtype=b.dtype, device="cuda")
+        out = whole[32:32 + b.n]
+        cache = b.cache()
+        cache.attend(b.q_gpu(), b.pages, b.starts, b.lengths, out=out)
+        k = torch.ones(b.n, 2, 64, dtype=b.dtype, device="cuda")
+        cache.append(k, k, b.pages, b.starts, b.lengths, q=b.q_gpu(), q_out=out)
+        torch.cuda.synchronize()
+        assert (whole[:32] == 7).all() and (whole[32 + b.n:] == 7).all()
+
+
+@pytest.mark.parametrize("seqs", [[(1, 30)] * 64, [(1, 30)] * 65, [(0, 30)] * 70 + [(1, 9)] + [(0, 1)] * 70,
+                                  [(n % 3, 20 * n) for n in range(200)], [(1, n) for n in range(1100)],
+                                  [(n % 4 * 30, 7 * n) for n in range(80)], [(5, 17 * n) for n in range(70)]])
+def test_many_sequences(seqs):
+    torch = torch_cuda()
+    log(f"{len(seqs)} sequences, {sum(n for n, _ in seqs)} new tokens")
+    b = Batch(torch, seqs, 8, 1, 64, 16, torch.bfloat16, seed=len(seqs))
+    cache = b.cache(rope_dim=0)
+    b.check(cache.attend(b.q_gpu(), b.pages, b.starts, b.lengths))
+    keys, values = b.keys.clone(), b.values.clone()
+    rows = [(s, n) for s, (n, _) in enumerate(seqs) if n]
+    k = torch.from_numpy(np.concatenate([b.k[s][-n:] for s, n in rows])).to(b.dtype).cuda()
+    v = torch.from_numpy(np.concatenate([b.v[s][-n:] for s, n in rows])).to(b.dtype).cuda()
+    for s, n in rows:  # the new tokens' places, emptied, are filled again as they were
+        t = np.arange(b.total[s] - n, b.total[s])
+        pg, pl = torch.from_numpy(b.table[s, t // 16]).long().cuda(), torch.from_numpy(t % 16).cuda()
+        b.keys[0][pg, :, 0, :, pl] = 0
+        b.values[0][pg, :, 0, pl // 8, :, pl % 8] = 0
+    cache.append(k, v, b.pages, b.starts, b.lengths)
+    assert torch.equal(b.keys.view(torch.int16), keys.view(torch.int16))
+    assert torch.equal(b.values.view(torch.int16), values.view(torch.int16))
+
+
+@pytest.mark.parametrize("new,before", [(1, 70), (3, 200), (9, 33)])
+def test_more_query_heads_than_a_tile_has_rows(new, before):
+    torch = torch_cuda()
+    for window in (0, 40):
+        b = Batch(torch, [(new, before), (1, 5)], 160, 1, 64, 32, torch.float16, seed=new)
+        b.check(b.cache(window=window).attend(b.q_gpu(), b.pages, b.starts, b.lengths), window)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("new", [3, 40, 200])
+def test_what_a_window_has_passed_has_no_effect(dtype, new):
+    """An old token with values that are not finite: rows whose window has passed it are as before,
+    the others get just those elements."""
+    torch = torch_cuda()
+    window, before = 50, 120
+    b = Batch(torch, [(new, before)], 4, 2, 64, 16, types()[dtype], seed=new)
+    cache, q = b.cache(window=window), b.q_gpu()
+    clean = cache.attend(q, b.pages, b.starts, b.lengths)
+    t = before - 30  # seen by positions up to t + 49
+    b.values[0, int(b.table[0, t // 16]), 0, 0, t // 8 % 2, 7, t % 8] = float("inf")
+    b.keys[0, int(b.table[0, (t - 60) // 16]), :, 0, 3, (t - 60) % 16, 2] = float("nan")  # seen by none
+    out = cache.attend(q, b.pages, b.starts, b.lengths)
+    seen = max(0, min(new, t + window - before))
+    assert torch.isposinf(out[:seen, :2, 7]).all()
+    out[:seen, :2, 7] = clean[:seen, :2, 7]
+    assert torch.equal(out, clean)
+
+
 def test_strided_rows():
     """q, k and v as slices of one projection's output; out inside a wider row."""
     torch = torch_cuda()

@@ -44,7 +44,7 @@ def random_rows(torch, rows, vocab, dtype, seed):
 
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
 @pytest.mark.parametrize("rows,vocab", [(1, 1), (3, 2), (5, 63), (4, 64), (4, 65), (9, 1000), (3, 4097), (2, 32003),
-                                        (70, 5001), (3, 32768), (3, 32769), (2, 152001), (1, 262144)])
+                                        (70, 5001), (3, 8192), (3, 8193), (2, 152001), (1, 262144)])
 def test_random_rows_and_settings(dtype, rows, vocab):
     torch = torch_cuda()
     log(f"sample {rows} x {vocab} {dtype}")
@@ -55,6 +55,17 @@ def test_random_rows_and_settings(dtype, rows, vocab):
         compare(z, rng.random(rows), temperature=pick(0.0, 0.3, 0.7, 1.0, 1.5, 3.0),
                 top_k=pick(0, 1, 2, 50, 1000, vocab, vocab + 1, -3), top_p=pick(1.0, 0.1, 0.5, 0.9, 0.999, 2.0),
                 min_p=pick(0.0, 0.01, 0.1, 0.5, 1.0, -1.0))
+
+
+def test_the_longest_rows_and_the_most():
+    torch = torch_cuda()
+    rng = np.random.default_rng(12)
+    z = random_rows(torch, 2, 1 << 20, torch.float32, 4)
+    compare(z, rng.random(2), temperature=[1.0, 2.5], top_k=[0, 30000], top_p=[0.97, 0.8])
+    z = random_rows(torch, 2500, 8500, torch.bfloat16, 5)
+    compare(z, rng.random(2500), top_k=rng.integers(0, 300, 2500), top_p=rng.choice([1.0, 0.9], 2500))
+    z = random_rows(torch, 65535, 5, torch.float32, 6)
+    compare(z, rng.random(65535), min_p=rng.choice([0.0, 0.3], 65535))
 
 
 def test_one_filter_at_a_time():
@@ -75,7 +86,7 @@ def test_ties():
     """Rows of few distinct logits: the filters cut inside runs of equal ones."""
     torch = torch_cuda()
     rng = np.random.default_rng(2)
-    for vocab in (7, 3000, 30000, 70000):
+    for vocab in (7, 3000, 8000, 70000):
         z = torch.from_numpy(rng.integers(-2, 3, (24, vocab)).astype(np.float32)).cuda()
         z[0] = 0.0
         z[1] = 0.0

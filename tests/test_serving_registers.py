@@ -1,0 +1,12 @@
+"""The built library's kernel metadata: the attention kernels, whose loops hold their operands and
+sums in registers, spill none of them."""
+import paper_2607_09686_amd.moecache as moecache
+from test_kernel_registers import kernels
+
+
+def test_attention_kernels_use_no_scratch():
+    found = {n: k for n, k in kernels(moecache.LIB_PATH).items() if "attend_" in n}
+    # few rows (32, 64), many rows, joined (of tiles of 32, 64, 128): three head sizes, two types
+    assert len(found) == 6 * 3 * 2
+    for name, k in found.items():
+        assert (k[".vgpr_spill_count"], k[".private_segment_fixed_size"]) == (0, 0), name
