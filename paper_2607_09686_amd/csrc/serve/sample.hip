@@ -203,11 +203,12 @@ __device__ __forceinline__ void bin_elements(const void *z, int lo, int hi, cons
   });
 }
 
-// Bounds on the exact mass, in 2^-31, of elements whose binned masses sum to m: half a unit for each of at most
-// V elements, and the exponentials' own error (their arguments, up to 44, are off by a few
-// parts in 2^24: the results by less than 2^-15).
-__device__ __forceinline__ double least_of(uint64_t m, int V) { return (double)m * (1.0 - 0x1p-15) - 0.5 * V; }
-__device__ __forceinline__ double most_of(uint64_t m, int V) { return (double)m * (1.0 + 0x1p-15) + 0.5 * V; }
+// What the exact mass, in 2^-31, of elements whose binned masses sum to m lies between, as good as surely:
+// the exponentials' arguments are off by a few parts in 2^24 of up to 44 (most of the mass is at a few), the
+// roundings of 2^20 elements add up to some 500 units at random.  Where it does not, the exact sums show
+// that the cut is not in the list, and the row is gone over.
+__device__ __forceinline__ double least_of(uint64_t m) { return (double)m * (1.0 - 0x1p-18) - 4096; }
+__device__ __forceinline__ double most_of(uint64_t m) { return (double)m * (1.0 + 0x1p-18) + 4096; }
 
 // Which bins may hold a cut: bins low .. high and rank_bin need their elements ranked; bins past
 // `last` hold nothing that is kept or counts.
@@ -218,7 +219,7 @@ struct Cuts {
 // By a block of N threads, from the bins threadIdx.x * kBins / N on in each; uniform over the block.
 template <int N>
 __device__ __forceinline__ Cuts find_cuts(const uint64_t (&mass)[kBins / N], const uint32_t (&count)[kBins / N],
-                                          const Row &r, int V) {
+                                          const Row &r) {
   constexpr int kPer = kBins / N;
   __shared__ uint64_t masses[N / 64];
   __shared__ uint32_t counts[N / 64], before_rank;
@@ -249,7 +250,7 @@ __device__ __forceinline__ Cuts find_cuts(const uint64_t (&mass)[kBins / N], con
     all_n += counts[i];
   }
   const bool cut_k = r.k && (uint32_t)r.k < all_n;  // else top-k cuts nothing but weights of 0
-  if (threadIdx.x == 0 && !cut_k) reach[0] = least_of(all, V), reach[1] = most_of(all, V);
+  if (threadIdx.x == 0 && !cut_k) reach[0] = least_of(all), reach[1] = most_of(all);
   if (cut_k) {
     uint64_t at = before;
     uint32_t n = before_n;
@@ -257,7 +258,7 @@ __device__ __forceinline__ Cuts find_cuts(const uint64_t (&mass)[kBins / N], con
     for (int i = 0; i < kPer; ++i) {
       if (n < (uint32_t)r.k && n + count[i] >= (uint32_t)r.k) {  // in one thread's one bin
         cuts[2] = threadIdx.x * kPer + i;
-        reach[0] = least_of(at, V), reach[1] = most_of(at + mass[i], V);
+        reach[0] = least_of(at), reach[1] = most_of(at + mass[i]);
         before_rank = n;
       }
       at += mass[i];
@@ -274,10 +275,10 @@ __device__ __forceinline__ Cuts find_cuts(const uint64_t (&mass)[kBins / N], con
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int b = threadIdx.x * kPer + i;
-      // the last bin that begins before it for certain, the first that ends past it for certain
-      if (most_of(at, V) < least) begun = b;
+      // the last bin that begins before that, the first that ends past it
+      if (most_of(at) < least) begun = b;
       at += mass[i];
-      if (least_of(at, V) >= most) ended = min(ended, b);
+      if (least_of(at) >= most) ended = min(ended, b);
     }
     for (int o = 32; o; o >>= 1) begun = max(begun, __shfl_xor(begun, o)), ended = min(ended, __shfl_xor(ended, o));
     if (lane == 0) atomicMax(&cuts[0], begun), atomicMin(&cuts[1], ended);
@@ -368,7 +369,7 @@ __device__ __forceinline__ uint64_t row_best(const RowWork &w, int blocks) {
 }
 
 // The cut as a code, found by going over the whole row: for rows with more elements in the bins
-// that hold a cut than the list takes (few distinct logits).  A total in falling order (of ones,
+// that hold a cut than the list takes (few distinct logits; 0.4 ms for 152001).  A total in falling order (of ones,
 // or of weights), over elements up to the code `in`, first reaches `want` at the code returned; want is at least 1
 // and at most the total.
 template <class Z>
@@ -441,20 +442,33 @@ __device__ __forceinline__ uint64_t reach_of(float p, uint64_t mass) {
 struct Last {
   uint64_t codes[kCandidates];  // the listed elements
   union {
-    uint64_t parts[kCandidates];  // their masses
-    struct {                      // before those are taken: a row's bins
+    uint64_t before[kCandidates];  // sorted: the listed mass before each
+    struct {                       // until then: a row's bins
       uint64_t mass[kBins];
       uint32_t count[kBins];
     };
   };
   uint64_t hist[256], scratch[kWaves], found[2], in_slice[kMaxSlices];
-  int n, n_early;
+  int n, n_early, at;
 };
+
+// Sorts n codes, a power of two, by the whole block (a bitonic network: 78 steps for 4096).
+__device__ __forceinline__ void sort_codes(uint64_t *codes, int n) {
+  for (int k = 2; k <= n; k *= 2)
+    for (int j = k / 2; j; j /= 2) {
+      for (int i = threadIdx.x; i < n / 2; i += kThreads) {
+        const int lo = 2 * i - (i & (j - 1)), hi = lo + j;
+        const uint64_t x = codes[lo], y = codes[hi];
+        if ((x > y) == ((lo & k) == 0)) codes[lo] = y, codes[hi] = x;
+      }
+      __syncthreads();
+    }
+}
 
 // The last step, a block per row: ranks the listed elements, which gives the cut, then finds the slice
 // (of `len` elements, its kept mass but for the listed ones in in_slice) in which the draw falls, and
-// the element in it.  n elements are to be listed; where they are more than the list takes, the row is gone
-// over instead.  all, ahead: exact masses of what may be kept, and of what is before the list.
+// the element in it.  n elements are to be listed; where they are more than the list takes, or the cut turns
+// out not to be among them, the row is gone over instead.  all, ahead: exact masses of what may be kept, and of what is before the list.
 template <class Z>
 __device__ __forceinline__ void rank_and_draw(const SampleArgs &a, int row, const void *z, const Row &r, const Cuts &c,
                                               int n, uint64_t all, uint64_t ahead, int slices, int len, int shift,
@@ -468,71 +482,80 @@ __device__ __forceinline__ void rank_and_draw(const SampleArgs &a, int row, cons
     return x < least ? 0 : (uint64_t)rint(x);
   };
   uint64_t cut = ~0ull;  // code of the last element that the filters by rank keep
-  if (threadIdx.x == 0) s.found[0] = s.found[1] = 0, s.n_early = 0;
-  if (n <= kCandidates) {
-    for (int i = threadIdx.x; i < n; i += kThreads) s.parts[i] = weigh.units(unrank(~(uint32_t)(s.codes[i] >> 32)));
+  bool known = c.low == kBins;  // nothing is cut by rank
+  if (!known && n > 0 && n <= kCandidates) {
+    // the listed elements in falling order, and the listed mass before each
+    int size = 1;
+    while (size < n) size *= 2;
+    for (int i = n + threadIdx.x; i < size; i += kThreads) s.codes[i] = ~0ull;
+    if (threadIdx.x == 0) s.n_early = 0, s.at = -1;
     __syncthreads();
-    if (n) {
-      const Binning bin(r, shift);
-      constexpr int kEach = kCandidates / kThreads;
-      uint64_t code[kEach], before[kEach];  // own elements, the listed mass before them
-      int rank[kEach], at[kEach];
+    sort_codes(s.codes, size);
+    const Binning bin(r, shift);
+    constexpr int kEach = kCandidates / kThreads;
+    const int each = (size + kThreads - 1) / kThreads, from = threadIdx.x * each;
+    uint64_t mass[kEach], up = 0;
+    int early = 0;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      mass[e] = 0;
+      if (e >= each || from + e >= n) continue;
+      const float v = unrank(~(uint32_t)(s.codes[from + e] >> 32));
+      mass[e] = weigh.units(v);
+      up += mass[e];
+      early += (int)bin.place(v) < c.rank_bin;
+    }
+    if (early) atomicAdd(&s.n_early, early);
+    uint64_t at = up;
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint64_t v = __shfl_up((unsigned long long)up, o);
+      if (lane >= o) up += v;
+    }
+    if (lane == 63) s.scratch[wave] = up;
+    __syncthreads();
+    at = up - at;
+    uint64_t listed = 0;
+    for (int i = 0; i < kWaves; ++i) {
+      if (i < wave) at += s.scratch[i];
+      listed += s.scratch[i];
+    }
+#pragma unroll
+    for (int e = 0; e < kEach; ++e)
+      if (e < each && from + e < n) {
+        s.before[from + e] = at;
+        at += mass[e];
+      }
+    __syncthreads();
+    // the top-k cut (the last listed element, without one), then the top-p cut
+    const auto through = [&](int i) { return i + 1 < n ? s.before[i + 1] : listed; };
+    int last = r.k && c.rank_bin < kBins ? s.n_early + r.k - (int)c.before_rank - 1 : n - 1;
+    last = min(max(last, 0), n - 1);
+    known = true;
+    if (r.p < 1.f) {
+      const uint64_t reach = reach_of(r.p, all - (listed - through(last)));
 #pragma unroll
       for (int e = 0; e < kEach; ++e) {
-        const int i = e * kThreads + threadIdx.x;
-        code[e] = i < n ? s.codes[i] : ~0ull;
-        at[e] = i < n ? (int)bin.place(unrank(~(uint32_t)(code[e] >> 32))) : kBins;
-        before[e] = 0;
-        rank[e] = 0;
-        if (i < n && at[e] < c.rank_bin) atomicAdd(&s.n_early, 1);
-      }
-      for (int j = 0; j < n; ++j) {
-        const uint64_t other = s.codes[j], m = s.parts[j];
-#pragma unroll
-        for (int e = 0; e < kEach; ++e)
-          if (e * kThreads < n && other < code[e]) before[e] += m, ++rank[e];
+        const int i = from + e;
+        if (e < each && i <= last && ahead + s.before[i] < reach &&
+            (int)bin.place(unrank(~(uint32_t)(s.codes[i] >> 32))) <= c.high)
+          atomicMax(&s.at, i);
       }
       __syncthreads();
-      // the top-k cut (the last listed element, without one), and the mass past it
-      const bool cut_k = r.k && c.rank_bin < kBins;
-      const int want = cut_k ? s.n_early + r.k - (int)c.before_rank - 1 : n - 1;
-#pragma unroll
-      for (int e = 0; e < kEach; ++e)
-        if (e * kThreads + (int)threadIdx.x < n && rank[e] == want)
-          s.found[0] = code[e];
-      __syncthreads();
-      cut = s.found[0];
-      if (r.p < 1.f) {
-        uint64_t past = 0;
-#pragma unroll
-        for (int e = 0; e < kEach; ++e) {
-          const int i = e * kThreads + threadIdx.x;
-          if (i < n && code[e] > cut) past += s.parts[i];
-        }
-        past = wave_sum(past);
-        if (lane == 0) s.scratch[wave] = past;
-        __syncthreads();
-        past = 0;
-        for (int i = 0; i < kWaves; ++i) past += s.scratch[i];
-        const uint64_t reach = reach_of(r.p, all - past);
-        if (threadIdx.x == 0) s.found[0] = 0;
-        __syncthreads();
-#pragma unroll
-        for (int e = 0; e < kEach; ++e)
-          if (e * kThreads + (int)threadIdx.x < n && code[e] <= cut && at[e] <= c.high && ahead + before[e] < reach)
-            atomicMax((unsigned long long *)&s.found[0], (unsigned long long)code[e]);
-        __syncthreads();
-        cut = s.found[0];
-      }
+      known = s.at >= 0 && ahead + through(max(0, s.at)) >= reach;
+      last = max(0, s.at);
+    }
+    if (known) {
+      cut = s.codes[last];
 #pragma unroll
       for (int e = 0; e < kEach; ++e) {
-        const int i = e * kThreads + threadIdx.x;
-        if (i >= n) break;
-        const uint64_t m = kept(unrank(~(uint32_t)(code[e] >> 32)), (int)(uint32_t)code[e], cut);
-        if (m) atomicAdd((unsigned long long *)&s.in_slice[(uint32_t)code[e] / len], (unsigned long long)m);
+        const int i = from + e;
+        if (e >= each || i > last) continue;
+        const uint64_t code = s.codes[i], m = kept(unrank(~(uint32_t)(code >> 32)), (int)(uint32_t)code, cut);
+        if (m) atomicAdd((unsigned long long *)&s.in_slice[(uint32_t)code / len], (unsigned long long)m);
       }
     }
-  } else {
+  }
+  if (!known) {
     if (r.k) cut = select_row<Z>(z, V, weigh, (uint64_t)r.k, false, cut, s.hist, s.scratch, s.found);
     if (r.p < 1.f) {
       uint64_t mass = 0;
@@ -681,7 +704,7 @@ __global__ __launch_bounds__(kThreads, 4) void row_kernel(SampleArgs a, int shif
       mass[i] = s.mass[threadIdx.x * (kBins / kThreads) + i];
       count[i] = s.count[threadIdx.x * (kBins / kThreads) + i];
     }
-    c = find_cuts<kThreads>(mass, count, r, V);
+    c = find_cuts<kThreads>(mass, count, r);
   }
   __syncthreads();  // `scratch` and the bins have been read
   uint64_t all = 0, ahead = 0;
@@ -767,7 +790,7 @@ __global__ __launch_bounds__(kSliceThreads) void collect_kernel(SampleArgs a, in
   __shared__ int n_mine, place;
   if (threadIdx.x == 0) n_mine = 0;
   Cuts c{kBins, kBins, kBins, 0};
-  if (r.ranked()) c = find_cuts<kSliceThreads>(mass, count, r, a.vocab);
+  if (r.ranked()) c = find_cuts<kSliceThreads>(mass, count, r);
   if (blockIdx.x == 0 && threadIdx.x == 0) w.cuts = c;
   __syncthreads();
   const void *z = (const Z *)a.logits + (int64_t)blockIdx.y * a.stride;

@@ -98,6 +98,34 @@ def test_ties():
             compare(t, rng.random(24), temperature=0.0)
 
 
+def test_masses_that_the_bins_get_wrong():
+    """A quarter million weights just below a half over a whole number of 2^-31, which is where the bins that
+    choose what is ranked round to: all are rounded down, the cut lies a good part of a bin from
+    where the bins put it.  The first token carries the draw; its share shows the cut (a bin's
+    elements are 1e-4 of it, the comparison's 2^-23)."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(14)
+    for vocab in (8000, 1 << 18):
+        whole = rng.integers(10, 1000, (24, vocab)) if vocab > 10000 else rng.integers(10, 40, (24, vocab)) * 1000
+        z = np.log((whole + 0.49) / 2 ** 31)
+        z[:, 0] = 0.0
+        mass = np.exp(z.astype(np.float32).astype(np.float64)).sum(1)
+        p = 1 / mass + (1 - 1 / mass) * np.linspace(0.05, 0.95, 24)  # cuts spread over the small weights
+        tokens, _ = compare(torch.from_numpy(z).float().cuda(), 0.3, top_p=p)
+        assert (tokens == 0).all()
+
+
+def test_nearly_all_of_the_mass():
+    """Cuts far out, where thousands of elements share a bin."""
+    torch = torch_cuda()
+    z = random_rows(torch, 12, 152001, torch.float32, 21)
+    rng = np.random.default_rng(15)
+    compare(z, rng.random(12), top_p=[0.99, 0.995, 0.999, 0.9995, 0.9999, 0.99999] * 2,
+            temperature=[1.0] * 6 + [1.5] * 6)
+    compare(z.bfloat16(), rng.random(12), top_p=[0.99, 0.995, 0.999, 0.9995, 0.9999, 0.99999] * 2,
+            temperature=[1.0] * 6 + [2.0] * 6, top_k=[0, 100000] * 6)
+
+
 def test_borders_on_exact_weights():
     """Four equal logits: masses 1/4 each, and p, u on the borders between them."""
     torch = torch_cuda()
