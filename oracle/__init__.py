@@ -15,6 +15,8 @@ What it computes, in plain fp64 numpy, one obviously-correct step at a time:
 * a whole MoE layer call and the residual stack   (``layer``)
 * the prefill variant that rounds weights, inputs and activations to bf16
   where the MFMA path does                        (``layer.moe_layer_bf16``)
+* what a decoder runs beside the layer calls: rotation, the paged cache's layout,
+  attention, the choice of a token                 (``serving``)
 * the static budget planner: slots per layer from a cache budget and the
   lower bound C + E(p) + K(n) against the serving target   (``planner``)
 

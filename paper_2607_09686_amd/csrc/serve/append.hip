@@ -9,7 +9,10 @@
 //
 // Bound by the bytes it moves, in one decode step by its launch.  A block takes the new tokens of
 // one sequence within one aligned run of eight positions: they share a page, their values are
-// whole 16-byte units of the cache, and the block's angles are shared by all heads.
+// whole 16-byte units of the cache, and the block's angles are shared by all heads.  Four blocks
+// to a run share out its heads, so that a decode step's few runs still fill the card.  Measured: 64
+// tokens of 32 + 2 x 4 heads of 128, 4.2 us (an empty launch takes about 2); 4096 tokens of them from fp32,
+// 126 MB, 25 us = 5.0 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -20,7 +23,7 @@
 namespace moecache {
 namespace {
 
-constexpr int kThreads = 256, kRun = 8;
+constexpr int kThreads = 256, kRun = 8, kShares = 4;
 constexpr double kTurn = 0.15915494309189533577;  // 1 / (2 pi)
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -187,7 +190,7 @@ template <class E, class I>
 hipError_t launch(const AppendArgs &a, hipStream_t s) {
   void *args[] = {const_cast<AppendArgs *>(&a)};
   const int runs = a.kv.n_tokens / kRun + 2 * a.kv.n_seqs;
-  return hipLaunchKernel((const void *)append_kernel<E, I>, dim3(runs, 4), dim3(kThreads), args, 0, s);
+  return hipLaunchKernel((const void *)append_kernel<E, I>, dim3(runs, kShares), dim3(kThreads), args, 0, s);
 }
 
 }  // namespace

@@ -12,6 +12,14 @@
 // length (at most 50): sums of integers do not depend on their order, so every split of a row over
 // threads gives the same token, and two tokens' border is off by at most 2^(20 - s) of the
 // largest weight.
+// A row is never sorted.  Its elements are counted and weighed into 2048 bins of depth below the largest
+// logit, coarsely (32-bit exponentials); that tells which bin or two hold the top-k and the top-p cut.
+// Then one exact pass sums the weights before those bins by slice of the row and lists the bins' own
+// elements, some tens; these are sorted, which gives the cut; and the draw finds its slice, and in
+// it the element.  Bound by the exact pass's 64-bit exponentials (about 30 instructions a
+// logit), short rows by the launches.  Measured: 64 rows of 152001 fp32 logits, every row with
+// settings of its own, 8.2 + 12.0 + 20.4 + 11.1 us (one read of the logits: 8); one row
+// 3.8 + 5.4 + 8.0 + 7.2; 320 rows of 32003 bf16 9.4 + 12.9 + 28.0 + 13.1.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -673,7 +681,8 @@ __device__ __forceinline__ bool settled(const SampleArgs &a, int row, const void
 
 // ---------------------------------------------------------------------------------------------
 // Rows of up to kWhole elements: a block per row takes all steps in one launch (each goes over the
-// row again, from the CU's XCD's L2), a slice's quarter to a wave at a time.
+// row again, from L2), a quarter of its wave's share at a time.  320 rows of 8000: 34 us, by launches
+// over slices 44; one row of 16000: 22.5 and 20.7.
 // ---------------------------------------------------------------------------------------------
 constexpr int kWhole = 8192, kRowSlices = 4 * kWaves;
 
