@@ -63,6 +63,34 @@ def test_split_and_ragged_batches(seqs):
     assert torch.equal(out, again)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("seqs,window", [([(1, 20000)], 5000), ([(1, 20000), (1, 100)], 19990), ([(40, 6000)], 3000),
+                                         ([(6, 9000), (6, 30)], 7777), ([(1, 1500)] * 70, 1100), ([(90, 4000)], 64)])
+def test_split_windows(seqs, window, dtype):
+    torch = torch_cuda()
+    b = Batch(torch, seqs, 8, 2, 128, 64, types()[dtype], seed=window)
+    b.check(b.cache(window=window).attend(b.q_gpu(), b.pages, b.starts, b.lengths), window)
+
+
+@pytest.mark.parametrize("seed", range(60))
+def test_random_batches(seed):
+    torch = torch_cuda()
+    rng = np.random.default_rng(1000 + seed)
+    dim, page = int(rng.choice([64, 128, 256])), int(rng.choice([16, 32, 64, 256]))
+    kv, group = int(rng.choice([1, 2, 3])), int(rng.choice([1, 2, 5, 8, 13]))
+    most, far = int(rng.choice([1, 4, 8, 40, 150])), int(rng.choice([3, 90, 700, 2500]))
+    n = int(rng.integers(1, 9 if most > 8 else 80 if far < 100 else 20))
+    seqs = [(int(rng.integers(0 if rng.random() < 0.2 else min(1, most), most + 1)), int(rng.integers(0, far + 1)))
+            for _ in range(n)]
+    window = int(rng.choice([0, 0, 1, 17, 64, 333, 5000]))
+    dtype = [torch.bfloat16, torch.float16][seed % 2]
+    log(f"random {seed}: dim {dim} page {page} kv {kv} group {group} window {window} {n} sequences {seqs[:3]} ...")
+    b = Batch(torch, seqs, kv * group, kv, dim, page, dtype, seed=seed, pad_rows=int(rng.integers(0, 3)),
+              width=-(-(most + far) // page) + int(rng.integers(0, 40)))
+    if b.n:
+        b.check(b.cache(window=window).attend(b.q_gpu(), b.pages, b.starts, b.lengths), window)
+
+
 @pytest.mark.parametrize("seqs,new,before", [(1100, 1, 19999), (300, 70, 17000)])
 def test_small_pages_past_one_list_of_ids(seqs, new, before):
     """Units of more than 1024 pages: so many sequences (over the same pages) that none is split."""
