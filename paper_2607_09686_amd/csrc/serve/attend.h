@@ -77,21 +77,22 @@ __device__ __forceinline__ Seq seq_of(const KvView &kv, int s) {
 // 64 at or below the first row's).
 template <int M>
 __device__ __forceinline__ int tiles_of(const AttendArgs &a, const Seq &q) {
-  return (int)(((int64_t)q.count * a.kv.group + M - 1) / M);
+  return (int)((uint32_t)(q.count * a.kv.group + M - 1) / M);  // at most 2^27 rows
 }
 template <int M>
 __device__ __forceinline__ int span_of(const AttendArgs &a, const Seq &q) {
   if (!a.window) return q.length;
-  const int64_t reach = (int64_t)a.window + (M - 1) / a.kv.group + 1 + 64;
-  return (int)min((int64_t)q.length, reach);
+  return (int)min((uint32_t)q.length, (uint32_t)a.window + (M + 64));  // of at most M tokens
 }
 // Units of a tile that spans `span` keys, which it shares out evenly.  Where the units are to run all at
 // once, span / C rounded down: one unit more than the card holds would double the time.  Where they
 // run in rounds, to the nearest whole number, which leaves their sizes closer to each other.
 __device__ __forceinline__ int units_of(const AttendArgs &a, int span, int C) {
-  return max(1, (int)(((int64_t)span + (a.nearest ? C / 2 : 0)) / C));
+  return max(1, (int)((uint32_t)(span + (a.nearest ? C / 2 : 0)) / (uint32_t)C));  // both at most 2^30
 }
-__device__ __forceinline__ int share_of(int keys, int units) { return ((keys + units - 1) / units + 63) & ~63; }
+__device__ __forceinline__ int share_of(int keys, int units) {
+  return (int)(((uint32_t)(keys + units - 1) / (uint32_t)units + 63) & ~63u);
+}
 
 // The workspace: how many tiles were split, with a plan_kernel the keys of a unit, a note of each split
 // tile, then the plan, then the o rows of slot (slot, kvh), then (m, l) pairs of all slots.
@@ -118,7 +119,7 @@ __device__ __forceinline__ float *part_base(const AttendArgs &a) { return (float
 
 // Keys of a unit, for tiles that span `work` keys together.
 __device__ __forceinline__ int keys_of(const AttendArgs &a, int64_t work) {
-  const int64_t c = (work * a.kv.kv_heads + a.target - 1) / a.target;
+  const int64_t c = (work * a.kv.kv_heads + (1 << a.target_log2) - 1) >> a.target_log2;
   return (int)min((int64_t)1 << 30, max((int64_t)a.min_keys, (c + 63) & ~(int64_t)63));
 }
 

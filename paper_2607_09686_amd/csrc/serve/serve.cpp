@@ -111,13 +111,15 @@ int plan(AttendArgs *a, uint64_t *bytes, int dim) {
   const int resident = few && dim > 128 ? kResident / 2 : kResident;
   // a sequence's tiles number ceil(rows / M), all sequences' together at most all rows / M + n_seqs
   const int64_t tiles = (int64_t)kv.n_tokens * kv.group / rows + kv.n_seqs;
-  a->target = few && 2 * tiles * kv.kv_heads >= resident ? 2 * resident : resident;
+  const int target = few && 2 * tiles * kv.kv_heads >= resident ? 2 * resident : resident;
+  a->target_log2 = 0;
+  while (1 << a->target_log2 < target) ++a->target_log2;
   a->nearest = few && 4 * tiles * kv.kv_heads >= resident;
   a->min_keys = few ? kFewMinKeys : kManyMinKeys;
   // units: a tile's keys / C, to the nearest whole number; with C >= all tiles' keys / (target /
   // kv_heads) that is at most target / kv_heads in all, and one more per tile; nor can a tile
   // have more than its table's keys give.  A split tile's units, x + 1/2 at x >= 3/2, are fewer than 2 x.
-  const int64_t share = a->target / kv.kv_heads + 1;
+  const int64_t share = target / kv.kv_heads + 1;
   const int64_t most = (((int64_t)kv.max_pages << kv.page_shift) + a->min_keys / 2) / a->min_keys + 1;
   a->max_units = (int)std::min(share + tiles, tiles * most);
   a->max_slots = (int)std::min(2 * share, tiles * most);

@@ -38,7 +38,7 @@ struct AttendArgs {
   int64_t q_stride, out_stride;
   int window;          // 0: none
   float scale_log2;    // scale * log2(e)
-  int target;          // work units aimed at over all KV heads
+  int target_log2;     // of the work units aimed at over all KV heads
   int min_keys;        // fewest keys of a unit, a multiple of 64
   int max_units;       // grid units per KV head
   int max_slots;       // partial-result slots per KV head
