@@ -16,10 +16,10 @@
 // logit, coarsely (32-bit exponentials); that tells which bin or two hold the top-k and the top-p cut.
 // Then one exact pass sums the weights before those bins by slice of the row and lists the bins' own
 // elements, some tens; these are sorted, which gives the cut; and the draw finds its slice, and in
-// it the element.  Bound by the exact pass's 64-bit exponentials (about 30 instructions a
-// logit), short rows by the launches.  Measured: 64 rows of 152001 fp32 logits, every row with
-// settings of its own, 8.2 + 12.0 + 20.4 + 11.1 us (one read of the logits: 8); one row
-// 3.8 + 5.4 + 8.0 + 7.2; 320 rows of 32003 bf16 9.4 + 12.9 + 28.0 + 13.1.
+// it the element.  Bound by the exact pass's 64-bit exponentials (21 instructions a logit, those
+// behind a top-k cut or below min_p left out), short rows by the launches.  Measured: 64 rows of
+// 152001 fp32 logits, every row with settings of its own, 8.3 + 11.8 + 18.0 + 9.4 us (one read of the
+// logits: 8.3); one row 3.8 + 5.3 + 7.8 + 7.5; 320 rows of 32003 bf16 9.3 + 12.5 + 23.9 + 11.6.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -104,33 +104,37 @@ __device__ __forceinline__ uint64_t wave_max(uint64_t v) {
 // exp((z - top) / T) in units of 2^-shift, for a finite top; a row's masses are sums of these, rounded to
 // whole units.
 struct Weigh {
-  double top;     // the row's largest logit
-  double scale;   // log2(e) / T
-  double c[12];   // (ln 2)^k / k!
-  double shift;   // at most 50
-  __device__ Weigh(float top_, float T, int shift_)
-      : top(top_), scale(1.4426950408889634 / (double)T), shift(shift_) {
-    double term = 1.0;
+  double top;      // the row's largest logit
+  double scale;    // log2(e) / T
+  double deepest;  // of z - top: 2^-900
+  double magic;    // 1.5 * 2^52 + shift: a sum with it is rounded to whole numbers, and holds them below
+  double c[11];    // of 2^f
+  __device__ Weigh(float top_, float T_, int shift) : Weigh((double)top_, fmin((double)T_, 1e300), shift) {}
+  __device__ Weigh(double top_, double T, int shift)  // a finite T: z - top may not be
+      : top(top_), scale(1.4426950408889634 / T), deepest(T * (-900.0 * 0.69314718055994531)),
+        magic(0x1.8p52 + shift),
+        // the polynomial of degree 10 with the least largest relative error on |f| <= 1/2 (2^-52), by Remez' exchange
+        c{1.0, 0.6931471805599498, 0.24022650695908773, 0.05550410866445366, 0.009618129108031203,
+          0.0013333558229309474, 0.00015403529966033974, 1.5252657716476882e-05, 1.321566021119544e-06,
+          1.0208609179389605e-07, 7.037746430390509e-09} {
 #pragma unroll
-    for (int k = 0; k < 12; ++k) {
-      c[k] = term;
-      term *= 0.69314718055994531 / (k + 1);
-      asm("" : "+s"(c[k]));  // in scalar registers, which an fma takes as they are
-    }
+    for (int k = 0; k < 11; ++k) asm("" : "+s"(c[k]));  // in scalar registers, which an fma takes as they are
   }
-  // With y = n + f, |f| <= 1/2: 2^y = 2^n 2^f, 2^f by its series to f^11 (what is left is below 2^-47 of
-  // it).  0 for NaN and -inf (the maximum of a NaN and a number is the number).
+  // With y = (z - top) / T log2(e) = n + f, n whole, |f| <= 1/2: 2^y = 2^n 2^f.  0 for NaN and -inf, but for
+  // a rounding (the maximum of a NaN and a number is the number).
   __device__ __forceinline__ double operator()(float z) const {
-    const double y = fmax(((double)z - top) * scale, -900.0), n = rint(y), f = y - n, f2 = f * f;
+    const double d = fmax((double)z - top, deepest), t = fma(d, scale, magic);
+    const double f = fma(d, scale, magic - t), f2 = f * f;
     // odd and even powers apart: two chains of half the length
-    double even = c[10], odd = c[11];
+    double even = c[10], odd = c[9];
 #pragma unroll
     for (int k = 8; k >= 0; k -= 2) {
       even = fma(even, f2, c[k]);
-      odd = fma(odd, f2, c[k + 1]);
+      if (k) odd = fma(odd, f2, c[k - 1]);
     }
     const double e = fma(odd, f, even);
-    const uint64_t bits = __builtin_bit_cast(uint64_t, e) + ((uint64_t)(uint32_t)(int)(n + shift) << 52);
+    // n + shift, the low bits of t, to the exponent
+    const uint64_t bits = __builtin_bit_cast(uint64_t, e) + (__builtin_bit_cast(uint64_t, t) << 52);
     return __builtin_bit_cast(double, bits);
   }
   __device__ __forceinline__ uint64_t units(float z) const { return (uint64_t)rint((*this)(z)); }
@@ -138,7 +142,7 @@ struct Weigh {
 
 // A row's settings, and its largest logit.
 struct Row {
-  float top, T, p, least;
+  float top, T, p, least, u;
   int first, k;
   bool none, greedy;  // nothing but -inf and NaN; the first largest is the answer
   bool wild;          // +inf among the logits: all weight is theirs
@@ -150,6 +154,7 @@ struct Row {
     k = a.top_k ? a.top_k[row] : 0;
     if (k <= 0 || k >= a.vocab) k = 0;
     least = a.min_p ? a.min_p[row] : 0.f;
+    u = a.u[row];
     if (least > 1.f) least = 1.f;
     none = !(top > -__builtin_inff());
     greedy = !(T > 0.f);
@@ -310,9 +315,12 @@ __device__ __forceinline__ Masses weigh_elements(const void *z, int lo, int hi, 
   const Weigh weigh = r.weigh(shift);
   const double least = (double)r.least * (double)(1ull << shift);
   const float low_start = (float)c.low, high_end = (float)(c.high + 1), rank_start = (float)c.rank_bin,
-              rank_end = (float)(c.rank_bin + 1), last_end = (float)min(c.rank_bin + 1, kBins);
-  // most rows ask for one sum only (elements past the last bin weigh nothing)
-  const bool one_sum = c.low == kBins && !(least > 0.0);
+              rank_end = (float)(c.rank_bin + 1);
+  const bool ranked = c.low < kBins, cut_k = c.rank_bin < kBins;
+  // past this place nothing asks for a weight; where nothing is cut by rank, only the kept mass does
+  float last_end = (float)min(c.rank_bin + 1, kBins);
+  if (!ranked && r.least > 0.f) last_end = fminf(last_end, -logf(r.least) / bin.depth * 1.0001f + 1.f);
+  const bool one_sum = !ranked && !(least > 0.0);
   // whole units, exact in a double up to 2^53: so many sums at a time
   Masses m{0, 0, 0};
   double all = 0, ahead = 0, kept = 0;
@@ -322,23 +330,24 @@ __device__ __forceinline__ Masses weigh_elements(const void *z, int lo, int hi, 
     all = ahead = kept = 0;
     room = 1 << (53 - shift);
   };
-  for_each<Z>(z, lo, hi, [&](const float (&v)[kVec<Z>], int i) __attribute__((always_inline)) {
+  auto four = [&](const float *v, int i) __attribute__((always_inline)) {
+    const float first = bin.place(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])));
     // with a top-k cut few of a row's elements matter: most calls end here
-    float f[kVec<Z>], least_f = __builtin_inff();
-#pragma unroll
-    for (int j = 0; j < kVec<Z>; ++j) least_f = fminf(least_f, f[j] = bin.place(v[j]));
-    if (!__any(least_f < last_end)) return;
+    if (!__any(first < last_end)) return;
     // without a branch between them, so that one element's arithmetic fills another's waits
-    double x[kVec<Z>];
+    double x[4];
 #pragma unroll
-    for (int j = 0; j < kVec<Z>; ++j) x[j] = weigh(v[j]);
-    if (one_sum) {
+    for (int j = 0; j < 4; ++j) x[j] = weigh(v[j]);
+    if (one_sum || (!cut_k && !__any(first < high_end))) {
+      // all behind the cut, as most are under top-p alone: one sum (past the last bin all round to 0)
 #pragma unroll
-      for (int j = 0; j < kVec<Z>; ++j) all += rint(x[j]);
+      for (int j = 0; j < 4; ++j) all += rint(x[j]);
     } else {
       bool any = false;
+      float f[4];
 #pragma unroll
-      for (int j = 0; j < kVec<Z>; ++j) {
+      for (int j = 0; j < 4; ++j) {
+        f[j] = bin.place(v[j]);
         const double n = f[j] < last_end ? rint(x[j]) : 0.0, early = f[j] < low_start ? n : 0.0;
         all += n;
         ahead += early;
@@ -347,11 +356,15 @@ __device__ __forceinline__ Masses weigh_elements(const void *z, int lo, int hi, 
       }
       if (any) {
 #pragma unroll
-        for (int j = 0; j < kVec<Z>; ++j)
+        for (int j = 0; j < 4; ++j)
           if (f[j] < kBins && ((f[j] >= low_start && f[j] < high_end) || (f[j] >= rank_start && f[j] < rank_end)))
             push(code_of(rank_key(v[j]), i + j));
       }
     }
+  };
+  for_each<Z>(z, lo, hi, [&](const float (&v)[kVec<Z>], int i) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < kVec<Z>; j += 4) four(v + j, i + j);
     if ((room -= kVec<Z>) < kVec<Z>) flush();
   });
   flush();
@@ -477,7 +490,7 @@ __device__ __forceinline__ void sort_codes(uint64_t *codes, int n) {
 // (of `len` elements, its kept mass but for the listed ones in in_slice) in which the draw falls, and
 // the element in it.  n elements are to be listed; where they are more than the list takes, or the cut turns
 // out not to be among them, the row is gone over instead.  all, ahead: exact masses of what may be kept, and of what is before the list.
-template <class Z>
+template <class Z, int kHalves>
 __device__ __forceinline__ void rank_and_draw(const SampleArgs &a, int row, const void *z, const Row &r, const Cuts &c,
                                               int n, uint64_t all, uint64_t ahead, int slices, int len, int shift,
                                               Last &s) {
@@ -600,34 +613,67 @@ __device__ __forceinline__ void rank_and_draw(const SampleArgs &a, int row, cons
     if (lane >= o) up += v;
   }
   const uint64_t mass = __shfl((unsigned long long)up, 63);
-  const uint64_t target = target_of(a.u[row], mass);
+  const uint64_t target = target_of(r.u, mass);
   const int at = max(0, __ffsll((unsigned long long)__ballot(target < up)) - 1);
   uint64_t before = __shfl((unsigned long long)(up - own), at);
   int slice = at * kPer;
   for (int i = 1; i < kPer && target >= before + s.in_slice[slice]; ++i) before += s.in_slice[slice++];
   const int begin = min(V, slice * len), end = min(V, begin + len);
   const int run = (end - begin + kWaves - 1) / kWaves, lo = min(end, begin + wave * run), hi = min(end, lo + run);
-  uint64_t mine = 0;
-  for (int i = lo + lane; i < hi; i += 64) mine += kept(logit<Z>(z, i), i, cut);
+  // steps of kHalves times four neighbours to a lane, asked for together; most runs end within one
+  constexpr int kEach = 4, kHalf = 64 * kEach, kStep = kHalves * kHalf;
+  uint64_t m[kHalves][kEach] = {}, mine = 0;
+  auto take = [&](int base) __attribute__((always_inline)) {
+    float v[kHalves][kEach];
+    uint64_t sum = 0;
+#pragma unroll
+    for (int e = 0; e < kHalves * kEach; ++e)
+      v[e / kEach][e % kEach] = logit<Z>(z, min(base + e / kEach * kHalf + lane * kEach + e % kEach, hi - 1));
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) {
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) m[h][e] = 0;
+      if (base + h * kHalf < hi) {
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+          const int i = base + h * kHalf + lane * kEach + e;
+          sum += m[h][e] = i < hi ? kept(v[h][e], i, cut) : 0;
+        }
+      }
+    }
+    return sum;
+  };
+  for (int base = lo; base < hi; base += kStep) mine += take(base);
   mine = wave_sum(mine);
   if (lane == 0) s.scratch[wave] = mine;
   __syncthreads();
   for (int i = 0; i < wave; ++i) before += s.scratch[i];
   if (target < before || target >= before + mine) return;
-  for (int base = lo; base < hi; base += 64) {
-    const int i = base + lane;
-    const uint64_t m = i < hi ? kept(logit<Z>(z, i), i, cut) : 0;
-    uint64_t sum = m;
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint64_t v = __shfl_up((unsigned long long)sum, o);
-      if (lane >= o) sum += v;
+  const bool again = hi - lo > kStep;  // else m is the run's
+  for (int base = lo; base < hi; base += kStep) {
+    if (again) take(base);
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) {
+      uint64_t sum = 0;
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) sum += m[h][e];
+      const uint64_t own = sum;
+      for (int o = 1; o < 64; o <<= 1) {
+        const uint64_t v = __shfl_up((unsigned long long)sum, o);
+        if (lane >= o) sum += v;
+      }
+      uint64_t at = before + sum - own;
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        if (target >= at && target < at + m[h][e]) {
+          a.token[row] = base + h * kHalf + lane * kEach + e;
+          if (a.prob) a.prob[row] = (float)((double)m[h][e] / (double)mass);
+        }
+        at += m[h][e];
+      }
+      before += __shfl((unsigned long long)sum, 63);
+      if (target < before) return;
     }
-    if (m && target >= before + sum - m && target < before + sum) {
-      a.token[row] = i;
-      if (a.prob) a.prob[row] = (float)((double)m / (double)mass);
-    }
-    before += __shfl((unsigned long long)sum, 63);
-    if (target < before) return;
   }
 }
 
@@ -650,7 +696,7 @@ __device__ __forceinline__ bool settled(const SampleArgs &a, int row, const void
     for (int i = 0; i < kWaves; ++i) n += scratch[i];
     if (r.k) n = min(n, (uint64_t)r.k);
     if (r.p < 1.f) n = reach_of(r.p, n);
-    const uint64_t target = target_of(a.u[row], n);
+    const uint64_t target = target_of(r.u, n);
     uint64_t seen = 0;
     for (int base = 0; base < V; base += kThreads) {
       const int i = base + threadIdx.x;
@@ -734,7 +780,7 @@ __global__ __launch_bounds__(kThreads, 4) void row_kernel(SampleArgs a, int shif
   for (int i = 0; i < kWaves; ++i) all += s.scratch[i], ahead += s.hist[i];
   const int n = s.n;
   __syncthreads();
-  rank_and_draw<Z>(a, row, z, r, c, n, all, ahead, kRowSlices, len, shift, s);
+  rank_and_draw<Z, 1>(a, row, z, r, c, n, all, ahead, kRowSlices, len, shift, s);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -781,10 +827,11 @@ __global__ __launch_bounds__(kThreads) void bins_kernel(SampleArgs a, int blocks
 }
 
 // Step 3: the cuts' bins (every block of a row finds them for itself), their elements into the row's
-// list, each slice's exact masses.
+// list, each slice's exact masses.  Five waves a SIMD: 1280 blocks, as 320 rows have, run at once.
 template <class Z>
-__global__ __launch_bounds__(kSliceThreads) void collect_kernel(SampleArgs a, int len, int shift) {
+__global__ __launch_bounds__(kSliceThreads, 5) void collect_kernel(SampleArgs a, int len, int shift) {
   RowWork &w = ((RowWork *)a.work)[blockIdx.y];
+  const void *z = (const Z *)a.logits + (int64_t)blockIdx.y * a.stride;
   constexpr int kPer = kBins / kSliceThreads;
   uint64_t mass[kPer];  // asked for together with the row's settings
   uint32_t count[kPer];
@@ -802,7 +849,6 @@ __global__ __launch_bounds__(kSliceThreads) void collect_kernel(SampleArgs a, in
   if (r.ranked()) c = find_cuts<kSliceThreads>(mass, count, r);
   if (blockIdx.x == 0 && threadIdx.x == 0) w.cuts = c;
   __syncthreads();
-  const void *z = (const Z *)a.logits + (int64_t)blockIdx.y * a.stride;
   const int slice = blockIdx.x * kSliceWaves + threadIdx.x / 64, lo = min(a.vocab, slice * len);
   const Masses m = weigh_elements<Z>(z, lo, min(a.vocab, lo + len), r, c, shift,
                                      [&](uint64_t code) __attribute__((always_inline)) {
@@ -829,27 +875,31 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleArgs a, int blocks
   const int row = blockIdx.x, lane = threadIdx.x % 64, wave = threadIdx.x / 64, slices = blocks * kSliceWaves;
   const RowWork &w = ((const RowWork *)a.work)[row];
   const void *z = (const Z *)a.logits + (int64_t)row * a.stride;
+  const uint64_t head = w.list[threadIdx.x];  // asked for before its length is known
+  // and so are the rest; none of it is used where the row is settled
+  const Masses m = (int)threadIdx.x < slices ? w.sums[threadIdx.x] : Masses{0, 0, 0};
+  const Cuts c = w.cuts;
+  const int n_list = w.n_list;
   const Row r(a, row, row_best(w, blocks));
   if (settled<Z>(a, row, z, r, s.scratch)) return;
   static_assert(kMaxSlices <= kThreads && kMaxSlices / 64 <= kWaves, "a thread per slice");
   if (threadIdx.x < kMaxSlices) {
-    const Masses m = (int)threadIdx.x < slices ? w.sums[threadIdx.x] : Masses{0, 0, 0};
     s.in_slice[threadIdx.x] = m.kept;
     const uint64_t all = wave_sum(m.all), ahead = wave_sum(m.ahead);
     if (lane == 0) s.scratch[wave] = all, s.hist[wave] = ahead;
   }
-  const Cuts c = w.cuts;
-  const int n = r.ranked() ? w.n_list : 0;
-  for (int i = threadIdx.x; i < min(n, kCandidates); i += kThreads) s.codes[i] = w.list[i];
+  const int n = r.ranked() ? n_list : 0;
+  if ((int)threadIdx.x < n) s.codes[threadIdx.x] = head;
+  for (int i = threadIdx.x + kThreads; i < min(n, kCandidates); i += kThreads) s.codes[i] = w.list[i];
   __syncthreads();
   uint64_t all = 0, ahead = 0;
 #pragma unroll
   for (int i = 0; i < kMaxSlices / 64; ++i) all += s.scratch[i], ahead += s.hist[i];
   __syncthreads();
-  rank_and_draw<Z>(a, row, z, r, c, n, all, ahead, slices, len, shift, s);
+  rank_and_draw<Z, 2>(a, row, z, r, c, n, all, ahead, slices, len, shift, s);
 }
 
-// Blocks for a row's passes: about 1024 over all rows, each wave with at least 256 elements.
+// Blocks for a row's passes: 1024 or some more over all rows, each wave with at least 256 elements.
 void split_row(int rows, int vocab, int *blocks, int *len) {
   int n = (1024 + rows - 1) / rows;
   const int most = (vocab + 256 * kSliceWaves - 1) / (256 * kSliceWaves);

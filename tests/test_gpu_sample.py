@@ -82,6 +82,22 @@ def test_one_filter_at_a_time():
     compare(z, u, temperature=1e-3)
 
 
+@pytest.mark.parametrize("dtype,rows,vocab", [("float32", 12, 7001), ("bfloat16", 12, 20003), ("float32", 5, 152001)])
+def test_min_p_alone(dtype, rows, vocab):
+    torch = torch_cuda()
+    rng = np.random.default_rng(vocab)
+    z = random_rows(torch, rows, vocab, getattr(torch, dtype), vocab + 1)
+    for least in (1.0, 0.3, 1e-3, 1e-9, 1e-30, 1e-45):
+        compare(z, rng.random(rows), temperature=rng.choice([0.2, 1.0, 4.0, 1e-30, 1e30], rows), min_p=least)
+
+
+def test_slices_of_more_than_one_step():
+    torch = torch_cuda()
+    rng = np.random.default_rng(8)
+    z = random_rows(torch, 1040, 20001, torch.bfloat16, 9)  # a wave's part of a slice: 626 elements
+    compare(z, rng.random(1040), temperature=rng.choice([1.0, 5.0], 1040), top_p=rng.choice([1.0, 0.999], 1040))
+
+
 def test_ties():
     """Rows of few distinct logits: the filters cut inside runs of equal ones."""
     torch = torch_cuda()
