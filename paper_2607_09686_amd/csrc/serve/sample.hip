@@ -727,10 +727,10 @@ __device__ __forceinline__ bool settled(const SampleArgs &a, int row, const void
 
 // ---------------------------------------------------------------------------------------------
 // Rows of up to kWhole elements: a block per row takes all steps in one launch (each goes over the
-// row again, from L2), a quarter of its wave's share at a time.  320 rows of 8000: 34 us, by launches
-// over slices 44; one row of 16000: 22.5 and 20.7.
+// row again, from L2), a quarter of its wave's share at a time.  320 rows of 8000: 31.5 us, by launches
+// over slices 40.6; 320 of 16000 40.5 and 45.9, one of 16000 22.1 and 21.4.
 // ---------------------------------------------------------------------------------------------
-constexpr int kWhole = 8192, kRowSlices = 4 * kWaves;
+constexpr int kWhole = 16384, kRowSlices = 4 * kWaves;
 
 template <class Z>
 __global__ __launch_bounds__(kThreads, 4) void row_kernel(SampleArgs a, int shift) {

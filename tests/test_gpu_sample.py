@@ -44,7 +44,7 @@ def random_rows(torch, rows, vocab, dtype, seed):
 
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
 @pytest.mark.parametrize("rows,vocab", [(1, 1), (3, 2), (5, 63), (4, 64), (4, 65), (9, 1000), (3, 4097), (2, 32003),
-                                        (70, 5001), (3, 8192), (3, 8193), (2, 152001), (1, 262144)])
+                                        (70, 5001), (3, 8192), (3, 8193), (3, 16384), (3, 16385), (2, 152001), (1, 262144)])
 def test_random_rows_and_settings(dtype, rows, vocab):
     torch = torch_cuda()
     log(f"sample {rows} x {vocab} {dtype}")
