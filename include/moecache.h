@@ -326,8 +326,9 @@ int moe_probe_hbm_read(uint64_t bytes, int32_t iters, double *read_us, double *e
  * A sequence whose length is less than its new tokens or more than its table
  * holds is not served: its rows of q_out and out become NaN and nothing of it
  * is written to the cache.  A page id outside [0, n_pages): the new tokens on it
- * are not written, and the rows of out that read it become NaN (rows computed
- * together with them may too).  *status, if given, gets MOE_KV_BAD_LENGTH or
+ * are not written, and the rows of out that see its tokens become NaN (rows computed
+ * together with them may too).  The entries of pages that no new token sees, a
+ * window having passed them, may hold anything.  *status, if given, gets MOE_KV_BAD_LENGTH or
  * MOE_KV_BAD_PAGE or-ed in (the library never clears it).  No access leaves the
  * arrays' stated sizes whatever they hold. */
 #define MOE_KV_BAD_PAGE 1

@@ -405,19 +405,25 @@ __device__ __forceinline__ float *part_ml(const AttendArgs &a, int64_t slot, int
 }
 
 // The ids of the unit's pages pg0 .. , at most kIds of them, into LDS; an id outside the pool is
-// taken as page 0 and reported.  Ends with a barrier.
-__device__ __forceinline__ void load_ids(const KvView &kv, int seq, int pg0, int pg_last, int *ids, int *bad) {
+// taken as page 0, and reported if its page is at or past `seen`, the first one that a row of the tile
+// sees (a range that begins at a multiple of 64 holds up to three pages of 16 before it, whose entries may
+// be anything).  Ends with a barrier.
+__device__ __forceinline__ void load_ids(const KvView &kv, int seq, int pg0, int pg_last, int seen, int *ids, int *bad) {
   const int n = min(kIds, pg_last - pg0 + 1);
   for (int i = threadIdx.x; i < n; i += kThreads) {
     const int id = kv.pages[(int64_t)seq * kv.max_pages + pg0 + i];
     const bool ok = (unsigned)id < (unsigned)kv.n_pages;
     ids[i] = ok ? id : 0;
-    if (!ok) {
+    if (!ok && pg0 + i >= seen) {
       *bad = 1;
       if (kv.status) atomicOr(kv.status, kKvBadPage);
     }
   }
   __syncthreads();
+}
+// The first page that a row of a tile whose first row stands at `pos` sees.
+__device__ __forceinline__ int first_page(const AttendArgs &a, int pos) {
+  return a.window ? max(0, pos - a.window + 1) >> a.kv.page_shift : 0;
 }
 
 // What a block works on.
@@ -522,11 +528,11 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_few_kernel(A
   const int key = (lane & 19) | (lane & 4) << 1 | (lane & 8) >> 1;  // pi(lane): bits 2 and 3 swapped
   const int64_t head_elems = (int64_t)D << shift, page_elems = head_elems * kv.kv_heads;
   const uint16_t *keys = kv.keys + u.kvh * head_elems, *values = kv.values + u.kvh * head_elems;
-  const int pg_last = (u.k1 - 1) >> shift;
+  const int pg_last = (u.k1 - 1) >> shift, pg_seen = first_page(a, first);
 
   for (int pg0 = u.k0 >> shift; pg0 <= pg_last; pg0 += kIds) {
     __syncthreads();  // the ids of the round before have been read
-    load_ids(kv, u.seq, pg0, pg_last, ids, &bad);
+    load_ids(kv, u.seq, pg0, pg_last, pg_seen, ids, &bad);
     const int begin = max(u.k0, pg0 << shift);
     const int end = (int)min((int64_t)u.k1, ((int64_t)pg0 + kIds) << shift);
     const int id_last = min(pg_last, pg0 + kIds - 1) - pg0;
@@ -661,11 +667,11 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_many_kernel(
   const int key = (lane & 19) | (lane & 4) << 1 | (lane & 8) >> 1;  // pi(lane): bits 2 and 3 swapped
   const int64_t head_elems = (int64_t)D << shift, page_elems = head_elems * kv.kv_heads;
   const uint16_t *keys = kv.keys + u.kvh * head_elems, *values = kv.values + u.kvh * head_elems;
-  const int pg_last = (u.k1 - 1) >> shift;
+  const int pg_last = (u.k1 - 1) >> shift, pg_seen = first_page(a, before + u.tile * M / kv.group);
 
   for (int pg0 = u.k0 >> shift; pg0 <= pg_last; pg0 += kIds) {
     __syncthreads();  // ids and tiles of the round before have been read
-    load_ids(kv, u.seq, pg0, pg_last, ids, &bad);
+    load_ids(kv, u.seq, pg0, pg_last, pg_seen, ids, &bad);
     const int begin = max(u.k0, pg0 << shift);
     const int end = (int)min((int64_t)u.k1, ((int64_t)pg0 + kIds) << shift);
     // tile t0 into buffer b: four groups' keys and values as they lie in memory, one group to

@@ -75,7 +75,8 @@ class KvCache:
     [n_layers, n_pages, n_kv_heads, page_tokens / 16, 2, head_dim, 8] are allocated (uninitialised)
     unless given.  Which sequence holds which pages is the caller's: every call takes
 
-      pages    int32 [n_seqs, max_pages], page ids in token order
+      pages    int32 [n_seqs, max_pages], page ids in token order (anything for pages past the length, and
+               for those that the window has passed for every new token)
       starts   int32 [n_seqs + 1], the sequences' first rows among the new tokens; rows from
                starts[n_seqs] on (a padded batch) are left alone
       lengths  int32 [n_seqs], tokens of each sequence, the new ones counted

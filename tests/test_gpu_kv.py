@@ -505,3 +505,36 @@ def test_refusals():
         b.cache(window=-1).attend(q, *index)
     with pytest.raises(MoeError):
         b.cache(scale=0.0).attend(q, *index)
+
+
+@pytest.mark.parametrize("page_id", [-1, 2 ** 31 - 1])
+@pytest.mark.parametrize("page,window", [(16, 50), (16, 1), (32, 33), (32, 100), (16, 333), (64, 90)])
+@pytest.mark.parametrize("dim,new", [(64, 1), (128, 5), (256, 8), (128, 90), (256, 90)])
+def test_page_ids_that_a_window_has_passed_are_free(dim, new, page, window, page_id):
+    """Entries of pages that no new token sees need not be page ids (their pages may have gone to
+    others): the results are those of a table with them, and nothing is reported.  Page 0, which no
+    sequence has, holds NaN and infinities."""
+    torch = torch_cuda()
+    log(f"passed ids: dim {dim} new {new} page {page} window {window} id {page_id}")
+    seqs = [(new, p) for p in (window + 14, 199, 200, 255, 256, 700)] + [(1, 3000)]
+    b = Batch(torch, seqs, 8, 2, dim, page, torch.bfloat16, seed=window, first_page=1)
+    b.values[0, 0, :, :, :, ::2] = float("inf")
+    cache, q = b.cache(window=window), b.q_gpu()
+    want = cache.attend(q, b.pages, b.starts, b.lengths)
+    b.check(want, window)
+    passed = 0
+    for s, (_, before) in enumerate(seqs):
+        n = max(0, before - window + 1) // page
+        b.pages[s, :n] = page_id
+        passed += n
+    assert passed > 0
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out = cache.attend(q, b.pages, b.starts, b.lengths, status=status)
+    assert torch.equal(out, want) and status.item() == 0
+    # the first page that a row does see still has to be one
+    n = max(0, seqs[2][1] - window + 1) // page
+    b.pages[2, n] = page_id
+    out = cache.attend(q, b.pages, b.starts, b.lengths, status=status)
+    assert torch.isnan(out[b.rows(2).start]).all() and status.item() == 1
+    for s in (0, 1, 3, 4, 5, 6):
+        assert torch.equal(out[b.rows(s)], want[b.rows(s)])
