@@ -382,7 +382,8 @@ int moe_kv_append(const moe_kv_batch *b, const moe_kv_rope *rope, int32_t in_dty
  * it, whatever it holds.  q, out: device, token rows of [n_heads][head_dim] in
  * the batch's dtype, strides in elements, multiples of 16 bytes; out must not
  * overlap q.  Sums and softmax in fp32; probabilities are rounded to the dtype
- * for their product with the values.  Results do not depend on where a
+ * for their product with the values (in MOE_F16 those below 2^-24 of the row's largest
+ * to within 2^-35 of it).  Results do not depend on where a
  * sequence's pages lie; they may differ in rounding with what else is in the
  * batch (the work is cut by the batch's lengths), never from run to run.
  * workspace: device scratch of the size that moe_kv_attend_workspace gives for

@@ -538,3 +538,71 @@ def test_page_ids_that_a_window_has_passed_are_free(dim, new, page, window, page
     assert torch.isnan(out[b.rows(2).start]).all() and status.item() == 1
     for s in (0, 1, 3, 4, 5, 6):
         assert torch.equal(out[b.rows(s)], want[b.rows(s)])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("gap", [14.0, 16.0, 17.5, 19.0])
+@pytest.mark.parametrize("dim,new,group,seqs,before", [(64, 1, 8, 600, 4000), (128, 5, 8, 600, 4000),
+                                                       (256, 1, 4, 600, 4000), (64, 70, 4, 60, 4000),
+                                                       (128, 70, 4, 60, 4000), (256, 70, 4, 60, 4000),
+                                                       (128, 1, 8, 1, 30000), (128, 70, 4, 1, 9000)])
+def test_a_first_key_far_above_the_rest(dtype, gap, dim, new, group, seqs, before):
+    """The first key's score is `gap` above the others', its value zero in most elements: what is left
+    of the sum is the many small probabilities'.  To Batch.check's tolerance fp16 adds that of its smallest
+    numbers: a probability is off by at most half of 2^-24 where the largest is at least 2^10, so the
+    output by 2^-35 of the sum of |v|."""
+    torch = torch_cuda()
+    log(f"first key {gap} above: {dtype} dim {dim} new {new} group {group} {seqs} sequences of {before}")
+    b = Batch(torch, [(new, before)], 2 * group, 2, dim, 64, types()[dtype], seed=7)
+    b.k[0][:, :, 0], b.k[0][0] = 0.0, 0.0
+    b.k[0][0, :, 0] = b.rounded(np.array(gap * dim ** 0.5 / 8))
+    b.v[0] = b.rounded(np.abs(b.v[0]) + 0.5)
+    b.v[0][0, :, 2:] = 0.0
+    b.fill(0)
+    rng = np.random.default_rng(8)
+    q = rng.standard_normal((seqs * new, 2 * group, dim)) * 0.5
+    q[:, :, 0] = 8.0
+    q = torch.from_numpy(q).to(b.dtype)
+    starts = torch.arange(0, seqs * new + 1, new, dtype=torch.int32, device="cuda")
+    out = b.cache().attend(q.cuda(), b.pages.expand(seqs, -1).contiguous(), starts,
+                           b.lengths.expand(seqs).contiguous()).double().cpu().numpy()
+    h, scale, pos = half_step(b.dtype), dim ** -0.5, b.positions(0)
+    tiny = float(torch.finfo(b.dtype).smallest_normal) * h
+    summed = np.repeat(np.cumsum(np.abs(b.v[0]), axis=0)[pos], group, axis=1)
+    for s in sorted({0, seqs // 2, seqs - 1}):
+        rows = q[s * new:(s + 1) * new].double().numpy()
+        want, weight = ref.attend(rows, b.k[0], b.v[0], pos, scale)
+        big = np.linalg.norm(rows, axis=2).max() * np.linalg.norm(b.k[0], axis=2).max() * scale
+        ds = (dim + 8) * 2.0 ** -24 * big
+        tol = h * np.abs(want) + (h + 2 * ds + 2.0 ** -18) * (1 + h) * weight + 4 * tiny
+        if dtype == "f16":
+            tol += 2.0 ** -35 * summed
+        err = np.abs(out[s * new:(s + 1) * new] - want)
+        assert np.all(err <= tol), (s, float((err / tol).max()), float((err / weight).max()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("new", [1, 5, 90])
+def test_scores_in_the_millions(dtype, new):
+    """A row is the value of its largest key, as far as fp32 tells that from the others: finite always.
+    To two roundings: the largest key's exponential is 2 to the difference of its score and the row's base,
+    no whole number, so its rounding to the type is in the sum of products, off by h, and not in the sum of
+    probabilities; the quotient, off by h, is rounded by h again: (1 + h)^2 - 1, and 2^-18 of the sums'."""
+    torch = torch_cuda()
+    b = Batch(torch, [(new, 1000), (new, 40)], 16, 2, 128, 32, types()[dtype], seed=new, q_scale=12000.0)
+    for s in range(2):
+        b.k[s] = b.rounded(b.k[s] * 50)
+        b.fill(s)
+    out = b.cache().attend(b.q_gpu(), b.pages, b.starts, b.lengths)
+    b.check(out)
+    got, clear, step = out.double().cpu().numpy(), 0, half_step(b.dtype)
+    for s in range(2):
+        for i, p in zip(range(b.rows(s).start, b.rows(s).stop), b.positions(s)):
+            for h in range(16):
+                z = np.sort(b.k[s][:p + 1, h // 8] @ b.q[i, h]) * 128 ** -0.5
+                if z[-1] - z[-2] > 100:  # fp32 is off by a few units here
+                    t = int(np.argmax(b.k[s][:p + 1, h // 8] @ b.q[i, h]))
+                    tol = ((1 + step) ** 2 - 1 + 2.0 ** -18) * np.abs(b.v[s][t, h // 8])
+                    assert np.all(np.abs(got[i, h] - b.v[s][t, h // 8]) <= tol)
+                    clear += 1
+    assert clear > 10 * new
