@@ -128,6 +128,12 @@ class KvCache:
         if self.rope_freqs.shape != (self.rope_dim // 2,):
             raise ValueError(f"rope_freqs must hold {self.rope_dim // 2} frequencies")
         self._blank = None     # the batch struct's bytes up to the call's own fields, per layer
+        if self.keys.is_cuda:  # made here, so that the first calls of several threads find it whole
+            self._blank = [bytes(KvBatch(_codes[dtype], n_heads, n_kv_heads, head_dim, page_tokens, n_pages,
+                                         0, 0, 0, 0, k.data_ptr(), v.data_ptr()))
+                           for k, v in zip(self.keys, self.values)]
+            self._index = self.device.index
+            self._rope = KvRope(self.rope_dim, self.rope_adjacent, self.rope_freqs.data_ptr())
         self._work_bytes = {}  # a batch's counts: bytes of moe_kv_attend's workspace
 
     keys = property(lambda self: self._keys)
@@ -141,13 +147,7 @@ class KvCache:
 
     def _batch(self, layer, pages, starts, lengths, n_tokens, status):
         if self._blank is None:
-            if not self.keys.is_cuda:
-                raise ValueError("the cache must live on the GPU")
-            self._blank = [bytes(KvBatch(
-                _codes[self.dtype], self.n_heads, self.n_kv_heads, self.head_dim, self.page_tokens, self.n_pages,
-                0, 0, 0, 0, k.data_ptr(), v.data_ptr())) for k, v in zip(self.keys, self.values)]
-            self._index = self.device.index
-            self._rope = KvRope(self.rope_dim, self.rope_adjacent, self.rope_freqs.data_ptr())
+            raise ValueError("the cache must live on the GPU")
         if not 0 <= layer < self.n_layers:
             raise ValueError(f"layer {layer} outside [0, {self.n_layers})")
         i32, device = _torch.int32, self.device

@@ -606,3 +606,49 @@ def test_scores_in_the_millions(dtype, new):
                     assert np.all(np.abs(got[i, h] - b.v[s][t, h // 8]) <= tol)
                     clear += 1
     assert clear > 10 * new
+
+
+def test_first_calls_of_several_threads(monkeypatch):
+    """A cache's first call is in another thread's way nowhere: calls on several streams are independent."""
+    import threading
+    from paper_2607_09686_amd import serving
+    torch = torch_cuda()
+    b = Batch(torch, [(1, 40), (3, 90)], 4, 2, 64, 16, torch.bfloat16)
+    q, index, errors, caches = b.q_gpu(), (b.pages, b.starts, b.lengths), [], []
+    k = torch.ones(b.n, 2, 64, dtype=b.dtype, device="cuda")
+    want = b.cache().append(k, k, *index, q=q)
+    torch.cuda.synchronize()
+
+    def call(cache, ready=None):
+        try:
+            if ready:
+                ready.wait()
+            with torch.cuda.stream(torch.cuda.Stream()):
+                out = cache.append(k, k, *index, q=q)
+                torch.cuda.current_stream().synchronize()
+            assert torch.equal(out, want)
+        except BaseException as e:
+            errors.append(e)
+
+    def run(*threads):
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+
+    rope = serving.KvRope
+
+    def another_call_first(*args):  # a second thread's call while the first one's is being made ready
+        if caches:
+            run(threading.Thread(target=call, args=(caches.pop(),)))
+        return rope(*args)
+
+    monkeypatch.setattr(serving, "KvRope", another_call_first)
+    cache = b.cache()
+    caches.append(cache)
+    call(cache)
+    monkeypatch.undo()
+    for _ in range(20):
+        cache, ready = b.cache(), threading.Barrier(4)
+        run(*(threading.Thread(target=call, args=(cache, ready)) for _ in range(4)))
+    assert not errors, errors[:3]
