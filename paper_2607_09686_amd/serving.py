@@ -45,6 +45,9 @@ def _vector(t, what, dtype, n, device):
 def _rows(t, what, dtype, heads, dim, n, device):
     """(pointer, stride) of token rows [n, heads, dim]; only the first dimension may have a stride."""
     _gpu(t, what, dtype, device)
+    if t.requires_grad and _torch.is_grad_enabled():
+        raise ValueError(f"{what} requires a gradient, which the cache's calls do not give: detach it, or call "
+                         "under torch.no_grad()")
     if t.shape != (n, heads, dim):
         raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {(n, heads, dim)}")
     s0, s1, s2 = t.stride()
@@ -83,6 +86,8 @@ class KvCache:
 
     on the GPU; a captured graph sees their contents at replay.  `status`, an int32 tensor of one
     element, gets MOE_KV_BAD_* bits or-ed in when they are out of range.
+
+    No call has a backward pass: rows that require a gradient are refused where gradients are recorded.
 
     rope_dim elements of each head turn by position * rope_theta ** (-2 i / rope_dim), or by
     rope_freqs[i], as pairs (i, i + rope_dim / 2), or (2 i, 2 i + 1) with rope_adjacent; 0: none.
@@ -170,7 +175,6 @@ class KvCache:
         dtype or float32, into their pages; with q [tokens, n_heads, head_dim] of the same dtype, also
         turn q and return it in the cache's dtype (in q_out if given, which may be q)."""
         n, kind, device, heads, dim = k.shape[0], k.dtype, self.device, self.n_heads, self.head_dim
-        b = self._batch(layer, pages, starts, lengths, n, status)
         if kind != self.dtype and kind != _torch.float32:
             raise TypeError(f"k must be {self.dtype} or torch.float32, got {kind}")
         kp, ks = _rows(k, "k", kind, self.n_kv_heads, dim, n, device)
@@ -183,6 +187,7 @@ class KvCache:
             op, os = _rows(q_out, "q_out", self.dtype, heads, dim, n, device)
         elif q_out is not None:
             raise ValueError("q_out without q")
+        b = self._batch(layer, pages, starts, lengths, n, status)
         _run(self._index, lib().moe_kv_append, b, self._rope, _codes[kind], kp, ks, vp, vs, qp, qs, op, os)
         return q_out
 
@@ -191,10 +196,10 @@ class KvCache:
         dtype) over their sequences, whose new tokens have been appended.  Returns out, like q."""
         n, device, heads, dim = q.shape[0], self.device, self.n_heads, self.head_dim
         qp, qs = _rows(q, "q", self.dtype, heads, dim, n, device)
-        b = self._batch(layer, pages, starts, lengths, n, status)
         if out is None:
             out = _torch.empty((n, heads, dim), dtype=self.dtype, device=device)
         op, os = _rows(out, "out", self.dtype, heads, dim, n, device)
+        b = self._batch(layer, pages, starts, lengths, n, status)
         counts = n, b.n_seqs, b.max_pages  # what the workspace's size goes by
         size = self._work_bytes.get(counts)
         if size is None:
@@ -212,7 +217,7 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None):
     """Choose a token from each row of logits [rows, vocab] (float32, bfloat16 or float16; rows may
     have a stride) with the uniform numbers u [rows] in [0, 1): moe_sample, which defines the filters
     and their order.  temperature, top_p, min_p (float32 [rows]) and top_k (int32 [rows]) may be
-    None.  Returns (tokens int32 [rows], probs float32 [rows])."""
+    None.  Returns (tokens int32 [rows], probs float32 [rows]); neither carries a gradient."""
     torch = _torch or _bind()
     if not isinstance(logits, torch.Tensor) or not logits.is_cuda:
         raise ValueError("logits must be a tensor on the GPU")

@@ -127,3 +127,26 @@ def test_the_cache_refuses_what_it_cannot_hold(mc):
         c.attend(torch.zeros(1, 8, 64, dtype=torch.bfloat16), i(1, 1), i(2), i(1))
     with pytest.raises(ValueError):
         sample(torch.zeros(1, 4), torch.zeros(1))
+
+
+def test_the_cache_refuses_to_drop_a_gradient(mc):
+    import torch
+    from paper_2607_09686_amd import KvCache
+    c = KvCache(n_layers=1, n_heads=4, n_kv_heads=2, head_dim=64, page_tokens=16, n_pages=3, device="cpu")
+    i = lambda *v: torch.zeros(*v, dtype=torch.int32)  # noqa: E731
+    index = i(1, 1), i(2), i(1)
+    t = lambda heads, grad: torch.zeros(1, heads, 64, dtype=torch.bfloat16, requires_grad=grad)  # noqa: E731
+    calls = [lambda g: c.attend(t(4, g), *index), lambda g: c.append(t(2, g), t(2, False), *index),
+             lambda g: c.append(t(2, False), t(2, g), *index),
+             lambda g: c.append(t(2, False), t(2, False), *index, q=t(4, g)),
+             lambda g: c.append(t(2, False), t(2, False), *index, q=t(4, False), q_out=t(4, g)),
+             lambda g: c.attend(t(4, False), *index, out=t(4, g))]
+    for call in calls:
+        with pytest.raises(ValueError, match="gradient"):
+            call(True)
+        with pytest.raises(ValueError, match="GPU"):  # no gradient to drop: refused for the host memory alone
+            call(False)
+        with torch.no_grad(), pytest.raises(ValueError, match="GPU"):
+            call(True)
+        with torch.inference_mode(), pytest.raises(ValueError, match="GPU"):
+            call(True)
