@@ -378,7 +378,7 @@ int moe_kv_append(const moe_kv_batch *b, const moe_kv_rope *rope, int32_t in_dty
 /* Attention of the new tokens over the cache (which holds them already):
  *   out = sum_t softmax_t(scale * q . k_t) v_t
  * over the sequence's tokens t at or before the row's own position and, with
- * window > 0, after position - window.  What a row does not see has no effect on
+ * window > 0, after position - window.  scale is positive, at most 2^127.  What a row does not see has no effect on
  * it, whatever it holds.  q, out: device, token rows of [n_heads][head_dim] in
  * the batch's dtype, strides in elements, multiples of 16 bytes; out must not
  * overlap q.  Sums and softmax in fp32; probabilities are rounded to the dtype

@@ -180,7 +180,9 @@ int moe_kv_attend(const moe_kv_batch *b, int32_t window, float scale, const void
   const int rc = check_kv(b, "moe_kv_attend", &a.kv);
   if (rc) return rc;
   if (window < 0) return fail(MOE_EINVAL, "moe_kv_attend: window must be >= 0");
-  if (!(scale > 0.f) || !std::isfinite(scale)) return fail(MOE_EINVAL, "moe_kv_attend: scale must be positive and finite");
+  a.scale_log2 = scale * 1.44269504088896340736f;
+  if (!(scale > 0.f) || !std::isfinite(a.scale_log2))
+    return fail(MOE_EINVAL, "moe_kv_attend: scale must be positive and finite, and its log2(e)-fold too");
   if (b->n_tokens == 0 || b->n_seqs == 0) return MOE_OK;
   if (!rows_ok(q, q_stride, b->n_heads, b->head_dim, 2) || !rows_ok(out, out_stride, b->n_heads, b->head_dim, 2))
     return fail(MOE_EINVAL, "moe_kv_attend: q and out must be 16-byte aligned rows of n_heads * head_dim elements");
@@ -191,7 +193,6 @@ int moe_kv_attend(const moe_kv_batch *b, int32_t window, float scale, const void
                 (unsigned long long)bytes);
   a.q = q, a.out = out, a.q_stride = q_stride, a.out_stride = out_stride;
   a.window = window;
-  a.scale_log2 = scale * 1.44269504088896340736f;
   a.work = workspace;
   const hipStream_t s = (hipStream_t)b->hip_stream;
   DeviceScope scope;

@@ -150,3 +150,16 @@ def test_the_cache_refuses_to_drop_a_gradient(mc):
             call(True)
         with torch.inference_mode(), pytest.raises(ValueError, match="GPU"):
             call(True)
+
+
+def test_a_scale_beyond_what_scores_can_hold_is_refused(mc):
+    """The kernels take scores in log2: a scale whose product with log2(e) is no finite fp32 is one as bad
+    as an infinite one."""
+    L, p = mc.lib(), 1 << 12
+    b = batch(mc)
+    size = ctypes.c_uint64()
+    assert L.moe_kv_attend_workspace(ctypes.byref(b), ctypes.byref(size)) == mc.MOE_OK
+    for scale in (2.4e38, 3.4e38):
+        assert L.moe_kv_attend(ctypes.byref(b), 0, scale, p, 1024, p, 1024, p, size.value) == mc.MOE_EINVAL, scale
+    none = batch(mc, n_tokens=0)  # as before: nothing to do, nothing launched
+    assert L.moe_kv_attend(ctypes.byref(none), 0, 2.3e38, None, 0, None, 0, None, 0) == mc.MOE_OK
