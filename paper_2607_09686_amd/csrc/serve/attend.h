@@ -273,7 +273,8 @@ __device__ __forceinline__ int key_of(int r, int half) { return 16 * (r / 8) + 8
 // Scores of keys that their row does not see become -inf: floor < t <= pos, as one comparison.
 template <int N>
 __device__ __forceinline__ void mask_scores(f32x16 (&s)[N], int t0, int pos, int floor) {
-  const uint32_t first = t0 + 8 * (threadIdx.x % kLanes / 32) - floor - 1, seen = pos - floor;
+  // unsigned from the start: a window near 2^31 puts keys behind pos 2^31 and more past the floor
+  const uint32_t first = (uint32_t)t0 + 8 * (threadIdx.x % kLanes / 32) - (uint32_t)floor - 1, seen = pos - floor;
 #pragma unroll
   for (int n = 0; n < N; ++n)
 #pragma unroll

@@ -652,3 +652,14 @@ def test_first_calls_of_several_threads(monkeypatch):
         cache, ready = b.cache(), threading.Barrier(4)
         run(*(threading.Thread(target=call, args=(cache, ready)) for _ in range(4)))
     assert not errors, errors[:3]
+
+
+@pytest.mark.parametrize("dim,new", [(64, 1), (128, 5), (256, 5), (128, 90)])
+def test_windows_longer_than_every_sequence(dim, new):
+    torch = torch_cuda()
+    b = Batch(torch, [(new, p) for p in (0, 3, 64, 500)] + [(1, 4000)], 8, 2, dim, 16, torch.bfloat16, seed=dim)
+    q, index = b.q_gpu(), (b.pages, b.starts, b.lengths)
+    want = b.cache().attend(q, *index)
+    b.check(want)
+    for window in (2 ** 31 - 1, 2 ** 31 - 65, 2 ** 30):
+        assert torch.equal(b.cache(window=window).attend(q, *index), want), window
