@@ -94,9 +94,12 @@ __device__ __forceinline__ int span_of(const AttendArgs &a, const Seq &q) {
   if (!a.window) return q.length;
   return (int)min((uint32_t)q.length, (uint32_t)a.window + (M + 64));  // of at most M tokens
 }
-// Units of a tile that spans `span` keys, which it shares out evenly.  Where the units are to run all at
-// once, span / C rounded down: one unit more than the card holds would double the time.  Where they
-// run in rounds, to the nearest whole number, which leaves their sizes closer to each other.
+// Units of a tile that spans `span` keys, which it shares out evenly: span / C rounded down, or with few
+// rows and tiles for a quarter of the card's places and more, to the nearest whole number, which leaves
+// the units' sizes closer to each other at the price of some more of them.  Measured (nearest, down): 64 sequences of
+// one token over 200 to 16000 204 and 208 us, 16 with heads of 256 65.8 and 72.9, but 24 windows of 5 68.7 and 67.1; with
+// fewer tiles the two are alike; in tiles of 128 rows 33 tokens over 60000 88.6 and 66.6, 1500 behind 1000 with heads
+// of 256 116 and 102.
 __device__ __forceinline__ int units_of(const AttendArgs &a, int span, int C) {
   return max(1, (int)((uint32_t)(span + (a.nearest ? C / 2 : 0)) / (uint32_t)C));  // both at most 2^30
 }
@@ -494,7 +497,9 @@ __device__ __forceinline__ float finish(float l) { return l == 0.f ? 0.f : 1.f /
 // cache).  Keys go straight from memory into the operand registers (LDS would only add a copy); a
 // step's are requested while the step before is multiplied.  Two blocks to a CU (249 registers of
 // 256 with heads of 128), 64 KB of requests in flight.  Measured, 4 KV heads of 128: 64 sequences of 200
-// to 16000 keys, 1.10 GB, 202 us = 5.5 TB/s; 24 windows of 40 rows over 1000 to 9000 keys, 219 MB, 50 us.
+// to 16000 keys, 1.10 GB, 203 us = 5.4 TB/s; 24 windows of 40 rows over 1000 to 9000 keys, 219 MB, 50 us where the
+// last-level cache holds them, the whole call 69 on keys that it does not (and 7 of the join).  Heads of 256, whole calls: 64
+// sequences of 8000 keys, 2.10 GB, 360 us = 5.8 TB/s; 24 windows of 40 rows, 494 MB, 132 us.
 // ---------------------------------------------------------------------------------------------
 template <class E, int D, int R>
 __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_few_kernel(AttendArgs a) {
@@ -635,7 +640,9 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_few_kernel(A
 // LDS for 1024 cycles of products, the full rate of LDS; the products take 40 % of the time, the
 // softmax's exponentials, sums and conversions about as much again.  The loop holds no step with
 // masks (those take a path of their own, with half the speed).  Measured: 4096 tokens behind
-// 12288, 32 heads of 128 on 4, 0.96 TFLOP in 0.95 ms = 1.01 PFLOP/s (a library product of 8192^3: 1.17).
+// 12288, 32 heads of 128 on 4, 0.96 TFLOP: the call 0.94 to 0.98 ms = 0.98 to 1.02 PFLOP/s from run to run (a library
+// product of 8192^3: 1.17), the kernel alone 0.98 to 1.03 where nothing else comes between its launches.  16 heads of 256
+// on 4, 4096 tokens behind 4096: 0.54 ms = 0.76 PFLOP/s.
 // ---------------------------------------------------------------------------------------------
 typedef __attribute__((address_space(3))) void lds_void;
 typedef const __attribute__((address_space(1))) void global_void;

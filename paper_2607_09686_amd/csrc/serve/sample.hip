@@ -16,10 +16,13 @@
 // logit, coarsely (32-bit exponentials); that tells which bin or two hold the top-k and the top-p cut.
 // Then one exact pass sums the weights before those bins by slice of the row and lists the bins' own
 // elements, some tens; these are sorted, which gives the cut; and the draw finds its slice, and in
-// it the element.  Bound by the exact pass's 64-bit exponentials (21 instructions a logit, those
-// behind a top-k cut or below min_p left out), short rows by the launches.  Measured: 64 rows of
-// 152001 fp32 logits, every row with settings of its own, 8.3 + 11.8 + 18.0 + 9.4 us (one read of the
-// logits: 8.3); one row 3.8 + 5.3 + 7.8 + 7.5; 320 rows of 32003 bf16 9.3 + 12.5 + 23.9 + 11.6.
+// it the element.  Bound by four passes in a chain, none of them near the rate of memory, short rows by
+// the launches.  Measured: 64 rows of 152001 fp32 logits, every row with settings of its own, 8.3 + 13.0 +
+// 18.1 + 9.5 us (one read of the logits: 8.3); one row 3.9 + 5.2 + 7.7 + 7.8; 320 rows of 32003 bf16 9.6 + 12.8 +
+// 23.9 + 11.8.  Of the exact pass's 18.1 (23.9) us 4 (4) are the launch and the row's settings, 3 (5) the bins and the
+// cuts in them, which every block of a row finds for itself, 11 (14.5) the logits: their places among the bins, and
+// 64-bit exponentials of 21 instructions for those not behind a top-k cut or below min_p (of all logits, with no
+// cuts to look for, 10 in either case; the instructions alone, at the card's rate, 5 for the 64 rows).
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -390,7 +393,8 @@ __device__ __forceinline__ uint64_t row_best(const RowWork &w, int blocks) {
 }
 
 // The cut as a code, found by going over the whole row: for rows with more elements in the bins
-// that hold a cut than the list takes (few distinct logits; 0.4 ms for 152001).  A total in falling order (of ones,
+// that hold a cut than the list takes (few distinct logits: a call over a row of 152001 equal ones takes 0.83 ms, over
+// 64 such rows 1.03; over bf16 logits of 12 to 28, a sixteenth to an eighth apart, 0.09 and 0.13).  A total in falling order (of ones,
 // or of weights), over elements up to the code `in`, first reaches `want` at the code returned; want is at least 1
 // and at most the total.
 template <class Z>

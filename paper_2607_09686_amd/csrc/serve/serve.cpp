@@ -98,7 +98,9 @@ bool rows_ok(const void *p, int64_t stride, int heads, int dim, int size) {
 // Rows (new tokens times the query heads of a KV head) of an attention tile.  New tokens per sequence
 // are known on the device only, so the rule goes by their mean.  Tiles of 32 and 64 rows read the
 // cache at full rate, once for every tile of a sequence.  In a tile of 128 the waves share the keys
-// through LDS and split the rows, and those without rows have nothing to do.
+// through LDS and split the rows, and those without rows have nothing to do.  A batch of both kinds takes one
+// size for all, which costs no more than a call for each: 63 single tokens over 4000 keys with a chunk of 2048 behind
+// 4000 (128) 294 us, in two calls 105 + 194; 255 with a chunk of 512 (32) 408, in two 365 + 71.
 int tile_rows(const KvView &kv) {
   const int64_t rows = (int64_t)kv.n_tokens * kv.group;
   return rows <= (int64_t)32 * kv.n_seqs ? 32 : rows <= (int64_t)64 * kv.n_seqs ? 64 : 128;
