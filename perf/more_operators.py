@@ -193,7 +193,7 @@ def prepare(case, seed):
         scales = {k: state[k][None] for k in ("key_scales", "value_scales")} if held else {}
         state["cache"] = KvCache(n_layers=1, n_heads=hq, n_kv_heads=hk, head_dim=d, page_tokens=page,
                                  n_pages=n_pages, dtype=t, rope_theta=case["theta"],
-                                 rope_dim=case["rope_dim"], rope_adjacent=case["adjacent"],
+                                 rope_dim=min(case["rope_dim"], d), rope_adjacent=case["adjacent"],
                                  window=case["window"], keys=state["keys"][None], values=state["values"][None],
                                  storage=torch.float8_e4m3fn if held else None, **scales)
     return state
@@ -336,7 +336,8 @@ def _attend(state):
 def _shared(state):
     case = state["case"]
     if own:
-        return state["cache"].attend(state["q"], state["pages"], state["starts"], state["lengths"],
+        q = state["q"].to(TYPES[case["dtype"]])  # a case's projections may come in another type
+        return state["cache"].attend(q, state["pages"], state["starts"], state["lengths"],
                                      prefix=state["prefix"], shared=state["shared"])
     hq, hk, d, most, seqs = case["heads"], case["kv_heads"], case["dim"], state["most_new"], case["seqs"]
     group, tokens = hq // hk, state["tokens"]
