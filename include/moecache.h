@@ -393,6 +393,66 @@ int moe_kv_attend(const moe_kv_batch *b, int32_t window, float scale, const void
                   int64_t out_stride, void *workspace, uint64_t workspace_bytes);
 int moe_kv_attend_workspace(const moe_kv_batch *b, uint64_t *bytes);
 
+/* Pools of 8 bits: keys and values hold e4m3 numbers (bytes), keys
+ * [n_pages][n_kv_heads][page_tokens / 16][head_dim / 16][16][16], element d of the
+ * token at place t at [t / 16][d / 16][t % 16][d % 16], values as ever,
+ * [n_pages][n_kv_heads][page_tokens / 16][2][head_dim][8]; and a head's vector x of
+ * one token has a power of two 2^e, held as the byte e + 127 at [page][head][t]:
+ *   e = ceil(log2(max |x_d| / 448)), within -100..119 (MOE_BF16) or -15..7 (MOE_F16)
+ *   c_d = e4m3(x_d / 2^e), rounded to nearest even, at most 448 in magnitude
+ * stands for c_d 2^e, which the batch's dtype holds exactly.  NaN and infinities are
+ * held as NaN and do not count for e (a vector without a finite element has the least
+ * e).  Rows are turned and normalised before, so each element is rounded once.  A
+ * token takes 2 (head_dim + 1) bytes a KV head. */
+typedef struct {
+  uint8_t *keys, *values; /* device, 16-byte aligned, [n_pages][n_kv_heads][page_tokens] */
+} moe_kv_scales;
+
+/* The norm of each head's queries and keys before their turn:
+ *   x_d / sqrt(mean of x^2 + eps) * weight_d
+ * over all head_dim elements, the sum in fp32.  A NULL weight: no norm there. */
+typedef struct {
+  const void *q_weight, *k_weight; /* device [head_dim], 16-byte aligned */
+  int32_t dtype;                   /* of the weights: MOE_F32 or the batch's dtype */
+  float eps;                       /* >= 0 */
+} moe_kv_norm;
+
+/* moe_kv_append with a norm (norm NULL: none), to pools of 8 bits (scales NULL: of the
+ * batch's dtype).  With both NULL it is moe_kv_append. */
+int moe_kv_append_ext(const moe_kv_batch *b, const moe_kv_scales *scales, const moe_kv_rope *rope, const moe_kv_norm *norm,
+                      int32_t in_dtype, const void *k, int64_t k_stride, const void *v, int64_t v_stride, const void *q,
+                      int64_t q_stride, void *q_out, int64_t q_out_stride);
+
+/* The batch's tokens taken out of the pools: row starts[s] + j of k and v gets what the
+ * token at position lengths[s] - count + j is held as (what it stands for, from 8
+ * bits), for the count = starts[s + 1] - starts[s] last tokens of each sequence; to have
+ * all, count them all.  k, v: device, rows as moe_kv_append's, in the batch's dtype.
+ * Rows of a token whose page is none, or of a sequence with a bad length, become NaN. */
+int moe_kv_read(const moe_kv_batch *b, const moe_kv_scales *scales, void *k, int64_t k_stride, void *v, int64_t v_stride);
+
+/* What every sequence of a batch begins with: its first *tokens tokens (of those with
+ * new ones), which lie in `pages` as well as in the sequences' own tables (the same pages,
+ * or pages with the same contents).  They come before every new token: a sequence for which
+ * *tokens is more than its length without the new ones is one with a bad length, and so are all
+ * where it is negative or more than the pages hold. */
+typedef struct {
+  const int32_t *pages;  /* device [n_pages] */
+  const int32_t *tokens; /* device */
+  int32_t n_pages;       /* n_pages * page_tokens <= 2^30 */
+  int32_t pad;
+} moe_kv_prefix;
+
+/* moe_kv_attend over pools of 8 bits (scales NULL: of the batch's dtype), with what
+ * all sequences begin with read once for all of them (prefix NULL: nothing; window
+ * must be 0 otherwise): the same result but for rounding.  A bad id among the
+ * prefix's pages makes every row NaN (MOE_KV_BAD_PAGE).  What a number of 8 bits stands
+ * for is multiplied as the batch's dtype holds it. */
+int moe_kv_attend_ext(const moe_kv_batch *b, const moe_kv_scales *scales, const moe_kv_prefix *prefix, int32_t window,
+                      float scale, const void *q, int64_t q_stride, void *out, int64_t out_stride, void *workspace,
+                      uint64_t workspace_bytes);
+int moe_kv_attend_ext_workspace(const moe_kv_batch *b, const moe_kv_scales *scales, const moe_kv_prefix *prefix,
+                                uint64_t *bytes);
+
 /* Choose one token from each row of logits.  Per row, in this order: weights
  * exp((z - max) / temperature); the top_k largest; of those, in falling order,
  * the ones before which less than top_p of their mass lies; of those, the ones of

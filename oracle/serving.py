@@ -1,5 +1,6 @@
 """What a decoder runs beside the layer calls, in fp64: rotation by position, the paged cache's
-layout, causal attention over a sequence, and the choice of a token from logits.
+layout, causal attention over a sequence, and the choice of a token from logits; norms of heads, and
+vectors held in 8 bits.
 """
 import numpy as np
 
@@ -18,6 +19,37 @@ def rotate(x, positions, freqs, adjacent=False):
     x[..., a] = xa * c - xb * s
     x[..., b] = xb * c + xa * s
     return x
+
+
+def head_norm(x, weight, eps):
+    """Each head (the last dimension) over the root of its mean square, times a weight."""
+    x = np.asarray(x, np.float64)
+    return x / np.sqrt((x * x).mean(-1, keepdims=True) + eps) * np.asarray(weight, np.float64)
+
+
+def _e4m3_values():
+    c = np.arange(256)
+    e, m = c >> 3 & 15, c & 7
+    v = np.where(e == 0, m * 2.0 ** -9, (1 + m / 8) * 2.0 ** (e - 7.0))
+    return np.where(c & 127 == 127, np.nan, np.where(c > 127, -v, v))
+
+
+E4M3 = _e4m3_values()
+
+
+def hold(x, least, most):
+    """(numbers, exponents) that stand for vectors x along the last dimension in 8 bits: number d is
+    x_d / 2^e rounded to e4m3 (nearest, ties to even, at most 448 in magnitude; NaN where x_d is not
+    finite), e = ceil(log2(max |x_d| / 448)) over the finite ones, within [least, most]."""
+    x = np.asarray(x, np.float64)
+    finite = np.isfinite(x)
+    big = np.where(finite, np.abs(x), 0).max(-1)
+    f, e = np.frexp(big)  # big = f 2^e, 1/2 <= f < 1; 448 = 7/8 2^9
+    e = np.where(big == 0, least, np.clip(e - 9 + (f > 0.875), least, most))
+    v = np.where(finite, x, 0) * 2.0 ** -e[..., None].astype(np.float64)
+    step = 2.0 ** (np.maximum(np.frexp(v)[1] - 1, -6) - 3.0)
+    v = np.clip(np.rint(v / step) * step, -448, 448)
+    return np.where(finite, v, np.nan), e
 
 
 def key_place(t, d):

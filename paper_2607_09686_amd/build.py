@@ -7,7 +7,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmoecache.so")
 SOURCES = ["wide_q6_k.hip", "wide_q4_k.hip", "wide_q8_0.hip", "wide_q4_0.hip", "kernels.hip", "tables.hip", "probe.hip", "moecache.cpp", "slot_lru.cpp", "planner.cpp", "policy.cpp", "pack.cpp",
-           "serve/attend_d256.hip", "serve/attend_d128.hip", "serve/attend_d64.hip", "serve/append.hip", "serve/sample.hip", "serve/serve.cpp"]
+           "serve/behind_d256.hip", "serve/behind_d128.hip", "serve/behind_d64.hip", "serve/attend_d256.hip", "serve/attend_d128.hip",
+           "serve/attend_d64.hip", "serve/append.hip", "serve/append_ext.hip", "serve/read.hip", "serve/sample.hip", "serve/serve.cpp"]
 ARCH = os.environ.get("MOECACHE_ARCH", "gfx950")
 # packed fp32 instructions are disabled: the compiler must not emit them
 HIPFLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-Wall",

@@ -28,7 +28,9 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
+#include "held.h"
 #include "serve.h"
 
 namespace moecache {
@@ -70,17 +72,39 @@ constexpr float kSlack = __is_same(E, _Float16) ? 4.f : 8.f;
 template <class E>
 constexpr float kBelow = __is_same(E, _Float16) ? 10.f : 0.f;
 
+// What a launch covers of the keys: all of them, those behind the tokens that every sequence begins
+// with, or these tokens' (behind.h).
+enum Cover { kAll, kBehind, kPrefix };
+
+// Of the tokens that every sequence begins with, the keys that the prefix's launch takes: whole 64s.
+// -1: a count that is none.
+__device__ __forceinline__ int shared_of(const AttendArgs &a) {
+  const int n = *a.shared;
+  return n < 0 || n > (a.prefix_pages << a.kv.page_shift) ? -1 : n;
+}
+
 // One sequence's share of the batch, read defensively: whatever starts and lengths hold, rows
 // stay within [0, n_tokens) and keys within the table.
 struct Seq {
   int first, count, length;  // rows first .. first + count - 1; keys 0 .. length - 1
   bool bad;                  // a length its table cannot hold, or shorter than its new tokens
 };
-__device__ __forceinline__ Seq seq_of(const KvView &kv, int s) {
+template <Cover C>
+__device__ __forceinline__ Seq seq_of(const AttendArgs &args, int s) {
+  const KvView &kv = args.kv;
   const int a = min(max(kv.starts[s], 0), kv.n_tokens), b = min(max(kv.starts[s + 1], a), kv.n_tokens);
   const int len = kv.lengths[s];
-  const bool bad = len < b - a || len > (kv.max_pages << kv.page_shift);
+  bool bad = len < b - a || len > (kv.max_pages << kv.page_shift);
+  if (C == kBehind && !bad && b > a) {  // what is shared comes before every new token
+    const int n = shared_of(args);
+    bad = n < 0 || n > len - (b - a);
+  }
   return Seq{a, b - a, bad ? 0 : len, bad};
+}
+// The first key that the launch covers.
+template <Cover C>
+__device__ __forceinline__ int skip_of(const AttendArgs &a) {
+  return C == kBehind ? max(0, shared_of(a)) & ~63 : 0;
 }
 
 // Tiles of a sequence, and the keys that one of them can span (its window starts at a multiple of
@@ -89,8 +113,9 @@ template <int M>
 __device__ __forceinline__ int tiles_of(const AttendArgs &a, const Seq &q) {
   return (int)((uint32_t)(q.count * a.kv.group + M - 1) / M);  // at most 2^27 rows
 }
-template <int M>
+template <int M, Cover C>
 __device__ __forceinline__ int span_of(const AttendArgs &a, const Seq &q) {
+  if (C == kBehind) return max(0, q.length - skip_of<C>(a));  // no window there
   if (!a.window) return q.length;
   return (int)min((uint32_t)q.length, (uint32_t)a.window + (M + 64));  // of at most M tokens
 }
@@ -141,11 +166,11 @@ __device__ __forceinline__ int keys_of(const AttendArgs &a, int64_t work) {
 struct Share {
   int units, slots, tiles;
 };
-template <int M>
+template <int M, Cover V>
 __device__ __forceinline__ Share share_of_seq(const AttendArgs &a, const Seq &q, int C) {
-  const int per = units_of(a, span_of<M>(a, q), C);
+  const int per = units_of(a, span_of<M, V>(a, q), C);
   const int n = (int)min((int64_t)1 << 24, (int64_t)tiles_of<M>(a, q) * per);
-  return per > 1 ? Share{n, n, n / per} : Share{n, 0, 0};
+  return per > 1 || V == kBehind ? Share{n, n, n / per} : Share{n, 0, 0};
 }
 // Inclusive sums over the first `lanes` lanes.
 __device__ __forceinline__ Share scan(Share s, int lanes) {
@@ -168,14 +193,14 @@ struct Place {
 // (64 sequences of 3000 keys: 70 us, with plan_kernel 76; one sequence: 14 and 18).  In rounds over more
 // sequences it would cost every block: 1024 of 400 keys took 277 us, with plan_kernel 145; 4096 of
 // 200 took 2325, now 371.
-template <int M>
+template <int M, Cover V>
 __device__ __forceinline__ bool plan_here(const AttendArgs &a, int unit, bool last, int *C, Place *out) {
   const int lane = threadIdx.x % kLanes, lanes = min(kLanes, a.kv.n_seqs);
-  const Seq q = lane < lanes ? seq_of(a.kv, lane) : Seq{0, 0, 0, false};
-  int64_t work = (int64_t)tiles_of<M>(a, q) * span_of<M>(a, q);
+  const Seq q = lane < lanes ? seq_of<V>(a, lane) : Seq{0, 0, 0, false};
+  int64_t work = (int64_t)tiles_of<M>(a, q) * span_of<M, V>(a, q);
   for (int o = 1; o < lanes; o <<= 1) work += __shfl_xor(work, o);
   *C = keys_of(a, __shfl(work, 0));  // lanes past the sequences have sums of nothing
-  const Share own = share_of_seq<M>(a, q, *C), sum = scan(own, lanes);
+  const Share own = share_of_seq<M, V>(a, q, *C), sum = scan(own, lanes);
   if (last) split_tiles(a)->count = min(a.max_tiles, __shfl(sum.tiles, lanes - 1));
   const uint64_t any = __ballot(lane < lanes && unit < sum.units);
   if (!any) return false;
@@ -190,16 +215,16 @@ __device__ __forceinline__ bool plan_here(const AttendArgs &a, int unit, bool la
 
 // More sequences: one block plans for all, and a unit's sequence is searched for, 64 at a time.
 constexpr int kPlanThreads = 1024;
-template <int M>
-__global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a) {
+template <int M, Cover V>
+__device__ __forceinline__ void plan_body(const AttendArgs &a) {
   constexpr int kW = kPlanThreads / kLanes;
   __shared__ int64_t works[kW];
   __shared__ Share sums[kW];
   const int lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes, n = a.kv.n_seqs;
   int64_t work = 0;
   for (int s = threadIdx.x; s < n; s += kPlanThreads) {
-    const Seq q = seq_of(a.kv, s);
-    work += (int64_t)tiles_of<M>(a, q) * span_of<M>(a, q);
+    const Seq q = seq_of<V>(a, s);
+    work += (int64_t)tiles_of<M>(a, q) * span_of<M, V>(a, q);
   }
   for (int o = 1; o < kLanes; o <<= 1) work += __shfl_xor(work, o);
   if (lane == 0) works[wave] = work;
@@ -212,7 +237,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a) {
   int64_t nu = 0, ns = 0, nt = 0;
   for (int s0 = 0; s0 < n; s0 += kPlanThreads) {
     const int s = s0 + threadIdx.x;
-    const Share own = s < n ? share_of_seq<M>(a, seq_of(a.kv, s), C) : Share{0, 0, 0}, sum = scan(own, kLanes);
+    const Share own = s < n ? share_of_seq<M, V>(a, seq_of<V>(a, s), C) : Share{0, 0, 0}, sum = scan(own, kLanes);
     __syncthreads();
     if (lane == kLanes - 1) sums[wave] = sum;
     __syncthreads();
@@ -230,6 +255,10 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a) {
   }
 }
 template <int M>
+__global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a) {
+  plan_body<M, kAll>(a);
+}
+template <int M, Cover V>
 __device__ __forceinline__ bool plan_search(const AttendArgs &a, int unit, int *C, Place *out) {
   const int32_t *units = plan_of(a, 0);
   *C = split_tiles(a)->keys;
@@ -243,7 +272,7 @@ __device__ __forceinline__ bool plan_search(const AttendArgs &a, int unit, int *
     lo += k * step;
     hi = min(hi, lo + step);
   }
-  *out = Place{lo, unit - units[lo], plan_of(a, 2)[lo], plan_of(a, 1)[lo], seq_of(a.kv, lo)};
+  *out = Place{lo, unit - units[lo], plan_of(a, 2)[lo], plan_of(a, 1)[lo], seq_of<V>(a, lo)};
   return true;
 }
 
@@ -252,14 +281,14 @@ __device__ __forceinline__ bool plan_search(const AttendArgs &a, int unit, int *
 struct Range {
   int lo, hi;
 };
-template <int M>
+template <int M, Cover V>
 __device__ __forceinline__ Range range_of(const AttendArgs &a, const Seq &q, int tile) {
   const int rows = q.count * a.kv.group;
   const int t0 = tile * M / a.kv.group, t1 = min(tile * M + M, rows) - 1;
   const int before = q.length - q.count;
   Range r;
   r.hi = before + t1 / a.kv.group + 1;
-  r.lo = a.window ? max(0, before + t0 - a.window + 1) & ~63 : 0;
+  r.lo = V == kBehind ? skip_of<V>(a) : a.window ? max(0, before + t0 - a.window + 1) & ~63 : 0;
   return r;
 }
 
@@ -288,9 +317,11 @@ __device__ __forceinline__ void mask_scores(f32x16 (&s)[N], int t0, int pos, int
 // Scores to probabilities over 32 * N keys: takes the new maximum, rescales the rows where some
 // row's maximum rose, and packs the B operands of the second product.
 // Probabilities are rounded to the cache's type, the type the matrix cores multiply; the sum
-// is taken in fp32 before that.
+// is taken in fp32 before that.  times, if given: a power of two that each key's probability is
+// multiplied by for the product, which rounds as without it.
 template <class E, int D, int N>
-__device__ __forceinline__ void softmax_step(f32x16 (&s)[N], Rows<D> &st, u32x4 (&p)[2 * N], float scale) {
+__device__ __forceinline__ void softmax_step(f32x16 (&s)[N], Rows<D> &st, u32x4 (&p)[2 * N], float scale,
+                                             const float *times = nullptr) {
   float mx = s[0][0];
 #pragma unroll
   for (int n = 0; n < N; ++n)
@@ -318,7 +349,7 @@ __device__ __forceinline__ void softmax_step(f32x16 (&s)[N], Rows<D> &st, u32x4 
       for (int j = 0; j < 8; ++j) {
         const float v = __builtin_amdgcn_exp2f(fmaf(s[n][8 * c + j], scale, -base));
         st.l += v;
-        e[j] = (E)v;
+        e[j] = (E)(times ? v * times[16 * n + 8 * c + j] : v);
       }
       p[2 * n + c] = __builtin_bit_cast(u32x4, e);
     }
@@ -358,23 +389,48 @@ __device__ __forceinline__ bool clean_values(u32x4 (&v)[D / 32], int t0, int end
   return true;
 }
 
+// Element d of a head that row m of product i stands for: 32 i + m, or where an operand load brings
+// two neighbouring elements (8 bits straight from memory), these are the products 2 i and 2 i + 1.
+template <bool Pairs>
+__device__ __forceinline__ constexpr int d_of(int i, int m) {
+  return Pairs ? 64 * (i / 2) + 2 * m + i % 2 : 32 * i + m;
+}
+// Four consecutive elements of this lane's row, the g-th of product i's, and the first one's place.
+template <int D, bool Pairs>
+__device__ __forceinline__ f32x4 four_of(const Rows<D> &st, int i, int g) {
+  if (!Pairs) return f32x4{st.acc[i][4 * g], st.acc[i][4 * g + 1], st.acc[i][4 * g + 2], st.acc[i][4 * g + 3]};
+  const int a = i & ~1, b = i | 1, r = 4 * g + 2 * (i % 2);
+  return f32x4{st.acc[a][r], st.acc[b][r], st.acc[a][r + 1], st.acc[b][r + 1]};
+}
+template <bool Pairs>
+__device__ __forceinline__ constexpr int four_at(int i, int g, int half) {
+  return Pairs ? 64 * (i / 2) + 16 * g + 8 * half + 4 * (i % 2) : 32 * i + 8 * g + 4 * half;
+}
+
 // Adds the values of keys t0 .. t1 - 1 that are not finite to the rows that see them (their weight
 // there is positive: an infinity stays the infinity it was).  Rare, and slow: element by element.
-template <class E, int D>
-__device__ __forceinline__ void add_odd(Rows<D> &st, const uint16_t *values, const int *ids, int pg0, int shift,
-                                        int64_t page_elems, int t0, int t1, int pos, int floor) {
+template <class E, int D, class S, bool Pairs>
+__device__ __forceinline__ void add_odd(Rows<D> &st, const S *values, const uint8_t *scales, int heads, const int *ids,
+                                        int pg0, int shift, int64_t page_elems, int t0, int t1, int pos, int floor) {
   constexpr uint32_t exponent = __is_same(E, __bf16) ? 0x7f80u : 0x7c00u;
   const int half = threadIdx.x % kLanes / 32;
 #pragma unroll 1
   for (int t = t0; t < t1; ++t) {
-    const uint16_t *src =
-        values + ids[(t >> shift) - pg0] * page_elems + ((t & ((1 << shift) - 1)) >> 3) * 8 * D + (t & 7);
+    const int64_t id = ids[(t >> shift) - pg0];
+    const S *src = values + id * page_elems + ((t & ((1 << shift) - 1)) >> 3) * 8 * D + (t & 7);
     const bool sees = t <= pos && t > floor;
+    float scale = 1.f;
+    if constexpr (sizeof(S) == 1) scale = scale_of(scales[(id * heads << shift) + (t & ((1 << shift) - 1))]);
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const uint16_t e = src[(32 * i + 8 * (r / 4) + 4 * half + r % 4) * 8];
+        const S c = src[d_of<Pairs>(i, 8 * (r / 4) + 4 * half + r % 4) * 8];
+        uint16_t e;
+        if constexpr (sizeof(S) == 1)
+          e = (uint16_t)decode2(c, false, scale, scale, E());
+        else
+          e = c;
         st.acc[i][r] += sees && (e & exponent) == exponent ? (float)__builtin_bit_cast(E, e) : 0.f;
       }
       __builtin_amdgcn_sched_barrier(0);  // 16 values' registers at a time
@@ -382,15 +438,17 @@ __device__ __forceinline__ void add_odd(Rows<D> &st, const uint16_t *values, con
   }
 }
 
-// This lane's row of the tile as the B operand of S^T = K Q^T: q[c] = elements 16 c + 8 half ...
-template <int D>
+// This lane's row of the tile as the B operand of S^T = K Q^T: q[c] = elements 16 c + 8 half ..., or for
+// keys of 8 bits straight from memory, 16 elements to a load, 32 (c / 2) + 16 half + 8 (c % 2) ...
+template <int D, bool Pairs>
 __device__ __forceinline__ void load_q(const AttendArgs &a, const Seq &q, int kvh, int row, u32x4 (&out)[D / 16]) {
   const int half = threadIdx.x % kLanes / 32, rows = q.count * a.kv.group;
   if (row < rows) {
     const int tok = q.first + row / a.kv.group, head = kvh * a.kv.group + row % a.kv.group;
-    const uint16_t *src = (const uint16_t *)a.q + (int64_t)tok * a.q_stride + (int64_t)head * D + 8 * half;
+    const uint16_t *src = (const uint16_t *)a.q + (int64_t)tok * a.q_stride + (int64_t)head * D;
 #pragma unroll
-    for (int c = 0; c < D / 16; ++c) out[c] = *(const u32x4 *)(src + 16 * c);
+    for (int c = 0; c < D / 16; ++c)
+      out[c] = *(const u32x4 *)(src + (Pairs ? c / 2 * 32 + 16 * half + c % 2 * 8 : 16 * c + 8 * half));
   } else {
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) out[c] = u32x4{};
@@ -416,14 +474,37 @@ __device__ __forceinline__ float *part_ml(const AttendArgs &a, int64_t slot, int
   return part_base(a) + (int64_t)a.max_slots * a.kv.kv_heads * M * D + ((slot * a.kv.kv_heads + kvh) * M + row) * 2;
 }
 
+// The prefix's partial results: the o rows of its slots, then their (m, l) pairs.
+__device__ __forceinline__ int64_t front_row(const AttendArgs &a, int64_t slot, int kvh, int row) {
+  return (slot * a.kv.kv_heads + kvh) * a.prefix_rows + row;
+}
+template <int D>
+__device__ __forceinline__ float *front_o(const AttendArgs &a, int64_t row) {
+  return a.front + row * D;
+}
+template <int D>
+__device__ __forceinline__ float *front_ml(const AttendArgs &a, int64_t row) {
+  return a.front + front_row(a, (int64_t)a.prefix_tiles * a.prefix_splits, 0, 0) * D + row * 2;
+}
+// Where a unit's row goes that is not the whole of it.
+template <int D, int M, Cover V>
+__device__ __forceinline__ float *unit_o(const AttendArgs &a, int64_t slot, int kvh, int row) {
+  return V == kPrefix ? front_o<D>(a, front_row(a, slot, kvh, row)) : part_o<D, M>(a, slot, kvh, row);
+}
+template <int D, int M, Cover V>
+__device__ __forceinline__ float *unit_ml(const AttendArgs &a, int64_t slot, int kvh, int row) {
+  return V == kPrefix ? front_ml<D>(a, front_row(a, slot, kvh, row)) : part_ml<D, M>(a, slot, kvh, row);
+}
+
 // The ids of the unit's pages pg0 .. , at most kIds of them, into LDS; an id outside the pool is
 // taken as page 0, and reported if its page is at or past `seen`, the first one that a row of the tile
 // sees (a range that begins at a multiple of 64 holds up to three pages of 16 before it, whose entries may
 // be anything).  Ends with a barrier.
-__device__ __forceinline__ void load_ids(const KvView &kv, int seq, int pg0, int pg_last, int seen, int *ids, int *bad) {
+__device__ __forceinline__ void load_ids(const KvView &kv, const int32_t *pages, int pg0, int pg_last, int seen, int *ids,
+                                         int *bad) {
   const int n = min(kIds, pg_last - pg0 + 1);
   for (int i = threadIdx.x; i < n; i += kThreads) {
-    const int id = kv.pages[(int64_t)seq * kv.max_pages + pg0 + i];
+    const int id = pages[pg0 + i];
     const bool ok = (unsigned)id < (unsigned)kv.n_pages;
     ids[i] = ok ? id : 0;
     if (!ok && pg0 + i >= seen) {
@@ -444,35 +525,66 @@ struct Unit {
   int64_t slot;                // partial-result slot, -1: the tile is this unit's alone
   Seq q;
 };
+// Of what all sequences begin with: the batch's rows, from its first sequence's to its last one's, as those of
+// one sequence, cut into tiles and these tiles' keys into prefix_splits units alike.
+struct Prefix {
+  int first, rows;   // the first token's row; rows of a KV head
+  int share, units;  // a unit's keys; units that have any
+  int keys;
+};
+__device__ __forceinline__ Prefix prefix_of(const AttendArgs &a) {
+  Prefix p;
+  p.first = min(max(a.kv.starts[0], 0), a.kv.n_tokens);
+  p.rows = (min(max(a.kv.starts[a.kv.n_seqs], p.first), a.kv.n_tokens) - p.first) * a.kv.group;
+  p.keys = skip_of<kBehind>(a);
+  p.share = share_of(p.keys, a.prefix_splits);
+  p.units = p.keys ? (p.keys + p.share - 1) / p.share : 0;
+  return p;
+}
 template <int M>
+__device__ __forceinline__ bool prefix_unit(const AttendArgs &a, Unit *u) {
+  const Prefix p = prefix_of(a);
+  const int unit = blockIdx.x / a.kv.kv_heads, split = unit % a.prefix_splits;
+  u->kvh = blockIdx.x % a.kv.kv_heads;
+  u->tile = unit / a.prefix_splits;
+  u->seq = 0;
+  u->q = Seq{p.first, p.rows / a.kv.group, p.keys, false};
+  u->k0 = split * p.share;
+  u->k1 = min(p.keys, u->k0 + p.share);
+  u->slot = unit;
+  return split < p.units && u->tile * M < p.rows;
+}
+
+template <int M, Cover V>
 __device__ __forceinline__ bool unit_of(const AttendArgs &a, Unit *u) {
+  if constexpr (V == kPrefix) return prefix_unit<M>(a, u);
   Place pl;
   int C;
   u->kvh = blockIdx.x % a.kv.kv_heads;
   const int unit = blockIdx.x / a.kv.kv_heads;
   const bool found = a.kv.n_seqs > kPlanSeqs
-                         ? plan_search<M>(a, unit, &C, &pl)
-                         : plan_here<M>(a, unit, blockIdx.x == 0 && threadIdx.x < kLanes, &C, &pl);
+                         ? plan_search<M, V>(a, unit, &C, &pl)
+                         : plan_here<M, V>(a, unit, blockIdx.x == 0 && threadIdx.x < kLanes, &C, &pl);
   if (!found) return false;
-  const int per = units_of(a, span_of<M>(a, pl.q), C);
+  const int per = units_of(a, span_of<M, V>(a, pl.q), C);
   if (pl.index >= (int64_t)tiles_of<M>(a, pl.q) * per) return false;  // starts out of order
   // the tiles with the most keys first
   const int order = pl.index / per, split = pl.index % per;
   u->seq = pl.seq;
   u->q = pl.q;
   u->tile = tiles_of<M>(a, pl.q) - 1 - order;
-  const Range r = range_of<M>(a, pl.q, u->tile);
+  const Range r = range_of<M, V>(a, pl.q, u->tile);
   const int share = share_of(r.hi - r.lo, per);
   const int real = max(1, (r.hi - r.lo + share - 1) / max(1, share));  // the tile's units that have keys
   u->k0 = r.lo + split * share;
   u->k1 = min(r.hi, u->k0 + share);
-  u->slot = real > 1 ? pl.slots + pl.index : -1;
-  if (per > 1) {
+  u->slot = real > 1 || V == kBehind ? pl.slots + pl.index : -1;
+  if (per > 1 || V == kBehind) {
     // starts out of order can ask for more than there are
     if ((int64_t)pl.slots + (int64_t)(order + 1) * per > a.max_slots || pl.tiles + order >= a.max_tiles) return false;
     if (split == 0 && u->kvh == 0 && threadIdx.x == 0)
       split_tiles(a)->tile[pl.tiles + order] =
-          SplitTile{(int)(pl.slots + pl.index), real, pl.q.first, u->tile * M,
+          SplitTile{(int)(pl.slots + pl.index), pl.q.bad ? 0 : real, pl.q.first, u->tile * M,
                     min(M, pl.q.count * a.kv.group - u->tile * M), {0, 0, 0}};
   }
   return split < real;
@@ -501,15 +613,46 @@ __device__ __forceinline__ float finish(float l) { return l == 0.f ? 0.f : 1.f /
 // last-level cache holds them, the whole call 69 on keys that it does not (and 7 of the join).  Heads of 256, whole calls: 64
 // sequences of 8000 keys, 2.10 GB, 360 us = 5.8 TB/s; 24 windows of 40 rows, 494 MB, 132 us.
 // ---------------------------------------------------------------------------------------------
-template <class E, int D, int R>
-__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_few_kernel(AttendArgs a) {
+// An operand of eight numbers of 8 bits (two words) times a power of two.
+template <class E>
+__device__ __forceinline__ u32x4 operand(uint32_t lo, uint32_t hi, float scale) {
+  return u32x4{decode(lo, false, scale, E()), decode(lo, true, scale, E()), decode(hi, false, scale, E()),
+               decode(hi, true, scale, E())};
+}
+// An operand of eight tokens' values times their powers of two.
+__device__ __forceinline__ u32x4 times_pairs(u32x4 v, const float *s) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const f16x2 t = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(s[2 * i], s[2 * i + 1]));
+    const uint32_t pair = v[i];  // (a cast of the vector's element would be one of its first)
+    v[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, pair) * t);
+  }
+  return v;
+}
+// The scales of eight tokens' values, for this lane's half of 16.
+__device__ __forceinline__ void scales_of(uint2 bytes, float *s) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) s[j] = scale_of((j < 4 ? bytes.x : bytes.y) >> (8 * (j % 4)) & 255);
+}
+
+// Keys and values of one step of 32 keys as they lie in memory, and their scales.
+template <int D, bool Held>
+struct Step {
+  u32x4 k[Held ? D / 32 : D / 16], v[2][Held ? D / 64 : D / 32];
+  uint32_t ks;
+  uint2 vs[2];
+};
+
+template <class E, int D, int R, bool Held, Cover V>
+__device__ __forceinline__ void few_body(const AttendArgs &a) {
   constexpr int M = 32 * R, kTurns = kWaves / R;  // waves that take turns at the steps of the same rows
+  typedef typename std::conditional<Held, uint8_t, uint16_t>::type S;
   __shared__ __align__(16) float sums[kWaves][D / 32 * 4][kLanes][4];
   __shared__ float stat[kWaves][32][2];
   __shared__ int ids[kIds];
   __shared__ int bad;
   Unit u;
-  if (!unit_of<M>(a, &u)) return;
+  if (!unit_of<M, V>(a, &u)) return;
   if (u.q.bad) {
     refuse<E, D, M>(a, u);
     return;
@@ -521,10 +664,10 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_few_kernel(A
   const int rows = u.q.count * kv.group, before = u.q.length - u.q.count;
   const int trow = 32 * part + n, row = u.tile * M + trow;
   const int pos = row < rows ? before + row / kv.group : -1;
-  const int floor = a.window ? pos - a.window : -1;
+  const int window = V == kAll ? a.window : 0, floor = window ? pos - window : -1;
   const int first = before + u.tile * M / kv.group, last = before + (min(u.tile * M + M, rows) - 1) / kv.group;
   u32x4 q[D / 16];
-  load_q<D>(a, u.q, u.kvh, row, q);
+  load_q<D, Held>(a, u.q, u.kvh, row, q);
   // heads of 256: the queries stay in LDS, where the joining of the waves has its place later
   constexpr bool kQInLds = D > 128;
   u32x4 *q_lds = (u32x4 *)&sums[0][0][0][0] + part * (D / 16) * kLanes;
@@ -541,31 +684,47 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_few_kernel(A
   const int shift = kv.page_shift, P = 1 << shift;
   const int key = (lane & 19) | (lane & 4) << 1 | (lane & 8) >> 1;  // pi(lane): bits 2 and 3 swapped
   const int64_t head_elems = (int64_t)D << shift, page_elems = head_elems * kv.kv_heads;
-  const uint16_t *keys = kv.keys + u.kvh * head_elems, *values = kv.values + u.kvh * head_elems;
-  const int pg_last = (u.k1 - 1) >> shift, pg_seen = first_page(a, first);
+  const S *keys = (const S *)kv.keys + u.kvh * head_elems, *values = (const S *)kv.values + u.kvh * head_elems;
+  const uint8_t *ks = kv.key_scales + (u.kvh << shift), *vs = kv.value_scales + (u.kvh << shift);
+  const int pg_last = (u.k1 - 1) >> shift, pg_seen = V == kPrefix ? 0 : first_page(a, first);
+  const int32_t *pages = V == kPrefix ? a.prefix : kv.pages + (int64_t)u.seq * kv.max_pages;
 
   for (int pg0 = u.k0 >> shift; pg0 <= pg_last; pg0 += kIds) {
     __syncthreads();  // the ids of the round before have been read
-    load_ids(kv, u.seq, pg0, pg_last, pg_seen, ids, &bad);
+    load_ids(kv, pages, pg0, pg_last, pg_seen, ids, &bad);
     const int begin = max(u.k0, pg0 << shift);
     const int end = (int)min((int64_t)u.k1, ((int64_t)pg0 + kIds) << shift);
     const int id_last = min(pg_last, pg0 + kIds - 1) - pg0;
-    u32x4 k[D / 16], v[2][D / 32];
+    Step<D, Held> x;
     auto load_k = [&](int t0) {
       const int t = t0 + key;
       const int id = ids[min((t >> shift) - pg0, id_last)];
-      const uint16_t *src = keys + id * page_elems + (t & (P - 1) & ~15) * D + (16 * half + t % 16) * 8;
+      if constexpr (Held) {
+        const S *src = keys + id * page_elems + (t & (P - 1) & ~15) * D + (16 * half + t % 16) * 16;
 #pragma unroll
-      for (int c = 0; c < D / 16; ++c) k[c] = *(const u32x4 *)(src + 2 * c * 16 * 8);
+        for (int c = 0; c < D / 32; ++c) x.k[c] = *(const u32x4 *)(src + c * 512);
+        x.ks = ks[((int64_t)id * kv.kv_heads << shift) + (t & (P - 1))];
+      } else {
+        const S *src = keys + id * page_elems + (t & (P - 1) & ~15) * D + (16 * half + t % 16) * 8;
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) x.k[c] = *(const u32x4 *)(src + 2 * c * 16 * 8);
+      }
     };
     auto load_v = [&](int t0) {
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const int t = t0 + 16 * c;
         const int id = ids[min((t >> shift) - pg0, id_last)];
-        const uint16_t *src = values + id * page_elems + (t & (P - 1)) * D + (half * D + n) * 8;
+        if constexpr (Held) {
+          const S *src = values + id * page_elems + (t & (P - 1)) * D + (half * D + 2 * n) * 8;
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) v[c][i] = *(const u32x4 *)(src + 32 * i * 8);
+          for (int i = 0; i < D / 64; ++i) x.v[c][i] = *(const u32x4 *)(src + 64 * i * 8);
+          x.vs[c] = *(const uint2 *)(vs + ((int64_t)id * kv.kv_heads << shift) + (t & (P - 1)) + 8 * half);
+        } else {
+          const S *src = values + id * page_elems + (t & (P - 1)) * D + (half * D + n) * 8;
+#pragma unroll
+          for (int i = 0; i < D / 32; ++i) x.v[c][i] = *(const u32x4 *)(src + 32 * i * 8);
+        }
       }
     };
     int t0 = begin + 32 * turn;
@@ -573,24 +732,47 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_few_kernel(A
     for (; t0 < end; t0 += 32 * kTurns) {
       const int next = t0 + 32 * kTurns;
       f32x16 s[1] = {};
+      const float k_scale = Held ? scale_of(x.ks) : 1.f;
 #pragma unroll
-      for (int c = 0; c < D / 16; ++c) s[0] = mma(k[c], kQInLds ? q_lds[c * kLanes + lane] : q[c], s[0], E());
+      for (int c = 0; c < D / 16; ++c) {
+        const u32x4 k = Held ? operand<E>(x.k[c / 2][c % 2 * 2], x.k[c / 2][c % 2 * 2 + 1], k_scale) : x.k[Held ? c / 2 : c];
+        s[0] = mma(k, kQInLds ? q_lds[c * kLanes + lane] : q[c], s[0], E());
+      }
       if (next < end) load_k(next);
       // whether some row does not see some key of the step
-      const bool edge = t0 + 31 > first || (a.window && t0 <= last - a.window);
+      const bool edge = V != kPrefix && (t0 + 31 > first || (window && t0 <= last - window));
       u32x4 p[2];
       if (edge) mask_scores<1>(s, t0, pos, floor);
-      softmax_step<E, D, 1>(s, st, p, a.scale_log2);
+      float times[16];
+      if constexpr (Held) scales_of(x.vs[0], times), scales_of(x.vs[1], times + 8);
+      constexpr bool kFold = Held && __is_same(E, __bf16);
+      softmax_step<E, D, 1>(s, st, p, a.scale_log2, kFold ? times : nullptr);
       bool odd = false;
-      if (edge) {
+      if constexpr (Held) {
 #pragma unroll
-        for (int c = 0; c < 2; ++c) odd |= clean_values<E, D>(v[c], t0 + 16 * c, u.q.length);
+        for (int c = 0; c < 2; ++c) {
+          u32x4 v[D / 32];
+#pragma unroll
+          for (int i = 0; i < D / 32; ++i) {
+            v[i] = operand<E>(x.v[c][i / 2][i % 2 * 2], x.v[c][i / 2][i % 2 * 2 + 1], 1.f);
+            if constexpr (!kFold) v[i] = times_pairs(v[i], times + 8 * c);
+          }
+          if (edge) odd |= clean_values<E, D>(v, t0 + 16 * c, u.q.length);
+#pragma unroll
+          for (int i = 0; i < D / 32; ++i) st.acc[i] = mma(v[i], p[c], st.acc[i], E());
+        }
+      } else {
+        if (edge) {
+#pragma unroll
+          for (int c = 0; c < 2; ++c) odd |= clean_values<E, D>(x.v[c], t0 + 16 * c, u.q.length);
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int i = 0; i < D / 32; ++i) st.acc[i] = mma(x.v[c][i], p[c], st.acc[i], E());
       }
-#pragma unroll
-      for (int c = 0; c < 2; ++c)
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) st.acc[i] = mma(v[c][i], p[c], st.acc[i], E());
-      if (odd) add_odd<E, D>(st, values, ids, pg0, shift, page_elems, t0, min(t0 + 32, end), pos, floor);
+      if (odd)
+        add_odd<E, D, S, Held>(st, values, vs, kv.kv_heads, ids, pg0, shift, page_elems, t0, min(t0 + 32, end), pos, floor);
       if (next < end) load_v(next);
     }
   }
@@ -606,9 +788,7 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_few_kernel(A
 #pragma unroll
   for (int i = 0; i < D / 32; ++i)
 #pragma unroll
-    for (int g = 0; g < 4; ++g)
-      *(f32x4 *)sums[wave][4 * i + g][lane] = f32x4{st.acc[i][4 * g] * mine, st.acc[i][4 * g + 1] * mine,
-                                                    st.acc[i][4 * g + 2] * mine, st.acc[i][4 * g + 3] * mine};
+    for (int g = 0; g < 4; ++g) *(f32x4 *)sums[wave][4 * i + g][lane] = four_of<D, Held>(st, i, g) * mine;
   float l = 0.f;
 #pragma unroll
   for (int w = 0; w < kTurns; ++w) l += stat[w * R + part][n][1] * __builtin_amdgcn_exp2f(stat[w * R + part][n][0] - base);
@@ -616,7 +796,7 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_few_kernel(A
   if (bad) l = __builtin_nanf("");
   if (row >= rows) return;
   if (u.slot >= 0 && turn == 0 && half == 0) {
-    float *ml = part_ml<D, M>(a, u.slot, u.kvh, trow);
+    float *ml = unit_ml<D, M, V>(a, u.slot, u.kvh, trow);
     ml[0] = top, ml[1] = l;
   }
   const float inv = finish(l);
@@ -624,12 +804,17 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_few_kernel(A
     f32x4 o{};
 #pragma unroll
     for (int w = 0; w < kTurns; ++w) o += *(const f32x4 *)sums[w * R + part][i][lane];
-    const int d = 32 * (i / 4) + 8 * (i % 4) + 4 * half;
+    const int d = four_at<Held>(i / 4, i % 4, half);
     if (u.slot >= 0)
-      *(f32x4 *)(part_o<D, M>(a, u.slot, u.kvh, trow) + d) = o;
+      *(f32x4 *)(unit_o<D, M, V>(a, u.slot, u.kvh, trow) + d) = o;
     else
       store_out<E, D>(a, u.q, u.kvh, row, d, o * inv);
   }
+}
+
+template <class E, int D, int R>
+__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_few_kernel(AttendArgs a) {
+  few_body<E, D, R, false, kAll>(a);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -647,15 +832,16 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_few_kernel(A
 typedef __attribute__((address_space(3))) void lds_void;
 typedef const __attribute__((address_space(1))) void global_void;
 
-template <class E, int D>
-__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_many_kernel(AttendArgs a) {
+template <class E, int D, bool Held, Cover V>
+__device__ __forceinline__ void many_body(const AttendArgs &a) {
   constexpr int M = 128, KT = 64;
+  typedef typename std::conditional<Held, uint8_t, uint16_t>::type S;
   constexpr int kTileBytes = KT * D * 2;
   __shared__ __align__(16) uint8_t lds[4 * kTileBytes];  // [2][K tile, V tile], each four groups
   __shared__ int ids[kIds];
   __shared__ int bad;
   Unit u;
-  if (!unit_of<M>(a, &u)) return;
+  if (!unit_of<M, V>(a, &u)) return;
   if (u.q.bad) {
     refuse<E, D, M>(a, u);
     return;
@@ -666,12 +852,12 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_many_kernel(
   const int rows = u.q.count * kv.group, wrow = u.tile * M + 32 * wave, row = wrow + n;
   const int before = u.q.length - u.q.count;
   const int pos = row < rows ? before + row / kv.group : -1;
-  const int floor = a.window ? pos - a.window : -1;
+  const int window = V == kAll ? a.window : 0, floor = window ? pos - window : -1;
   // positions of this wave's first and last row (none: last below every key)
   const int first = before + wrow / kv.group;
   const int last = wrow < rows ? before + (min(wrow + 32, rows) - 1) / kv.group : -1;
   u32x4 q[D / 16];
-  load_q<D>(a, u.q, u.kvh, row, q);
+  load_q<D, false>(a, u.q, u.kvh, row, q);
 
   Rows<D> st;
 #pragma unroll
@@ -682,17 +868,21 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_many_kernel(
   const int shift = kv.page_shift, P = 1 << shift;
   const int key = (lane & 19) | (lane & 4) << 1 | (lane & 8) >> 1;  // pi(lane): bits 2 and 3 swapped
   const int64_t head_elems = (int64_t)D << shift, page_elems = head_elems * kv.kv_heads;
-  const uint16_t *keys = kv.keys + u.kvh * head_elems, *values = kv.values + u.kvh * head_elems;
-  const int pg_last = (u.k1 - 1) >> shift, pg_seen = first_page(a, before + u.tile * M / kv.group);
+  const S *keys = (const S *)kv.keys + u.kvh * head_elems, *values = (const S *)kv.values + u.kvh * head_elems;
+  const uint8_t *ks = kv.key_scales + (u.kvh << shift), *vs = kv.value_scales + (u.kvh << shift);
+  const int pg_last = (u.k1 - 1) >> shift;
+  const int pg_seen = V == kPrefix ? 0 : first_page(a, before + u.tile * M / kv.group);
+  const int32_t *pages = V == kPrefix ? a.prefix : kv.pages + (int64_t)u.seq * kv.max_pages;
 
   for (int pg0 = u.k0 >> shift; pg0 <= pg_last; pg0 += kIds) {
     __syncthreads();  // ids and tiles of the round before have been read
-    load_ids(kv, u.seq, pg0, pg_last, pg_seen, ids, &bad);
+    load_ids(kv, pages, pg0, pg_last, pg_seen, ids, &bad);
     const int begin = max(u.k0, pg0 << shift);
     const int end = (int)min((int64_t)u.k1, ((int64_t)pg0 + kIds) << shift);
     // tile t0 into buffer b: four groups' keys and values as they lie in memory, one group to
     // a wave; a group past the end is read from the last one's place
     auto stage = [&](int t0, int b) {
+      if constexpr (Held) return;
       const int t = min(t0 + 16 * wave, (end - 1) & ~15);
       const int64_t at = ids[(t >> shift) - pg0] * page_elems + (t & (P - 1)) * D + lane * 8;
       uint8_t *dst = lds + b * 2 * kTileBytes + wave * 16 * D * 2;
@@ -703,17 +893,66 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_many_kernel(
                                          (lds_void *)(dst + kTileBytes + i * 1024), 16, 0, 0);
       }
     };
+    // 8 bits: into registers, from which a tile goes to LDS in 16 bits, laid out alike
+    u32x4 kr[Held ? D / 64 : 1], vr[Held ? D / 64 : 1];
+    uint32_t kb;
+    uint2 vb[Held ? D / 64 : 1];
+    auto fetch = [&](int t0) {
+      if constexpr (Held) {
+        const int t = min(t0 + 16 * wave, (end - 1) & ~15);
+        const int64_t id = ids[(t >> shift) - pg0], at = id * page_elems + (t & (P - 1)) * D + lane * 16;
+        const int64_t sc = ((id * kv.kv_heads) << shift) + (t & (P - 1));
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+          kr[i] = *(const u32x4 *)(keys + at + i * 1024);
+          vr[i] = *(const u32x4 *)(values + at + i * 1024);
+          vb[i] = *(const uint2 *)(vs + sc + 8 * ((i * 64 + lane) / (D / 2)));
+        }
+        kb = ks[sc + lane % 16];
+      }
+    };
+    auto unpack = [&](int b) {
+      if constexpr (Held) {
+        uint8_t *dst = lds + b * 2 * kTileBytes + wave * 16 * D * 2;
+        const float s = scale_of(kb);
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+          const int unit = i * 64 + lane;  // keys: 16 elements of a token; values: eight tokens of two elements
+          uint8_t *kd = dst + (unit / 16 * 32 + unit % 16) * 16, *vd = dst + kTileBytes + unit * 32;
+          float t[8];
+          scales_of(vb[i], t);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            *(u32x4 *)(kd + j * 256) = operand<E>(kr[i][2 * j], kr[i][2 * j + 1], s);
+            const uint32_t lo = vr[i][2 * j], hi = vr[i][2 * j + 1];
+            *(u32x4 *)(vd + j * 16) = u32x4{decode2(lo, false, t[0], t[1], E()), decode2(lo, true, t[2], t[3], E()),
+                                            decode2(hi, false, t[4], t[5], E()), decode2(hi, true, t[6], t[7], E())};
+          }
+        }
+      }
+    };
     // this lane's operands within 32 keys' and 16 values' bytes
     const int koff = key / 16 * 32 * D + (16 * half + key % 16) * 16, voff = (half * D + n) * 16;
     stage(begin, 0);
+    if constexpr (Held) {
+      fetch(begin);
+      unpack(0);
+      if (begin + KT < end) fetch(begin + KT);
+    }
     int b = 0;
     for (int t0 = begin; t0 < end; t0 += KT, b ^= 1) {
       asm volatile("" ::: "memory");
-      __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's part of the tile has landed
-      __builtin_amdgcn_s_barrier();        // everyone's has, and the other buffer is free
+      // this wave's part of the tile has landed: vmcnt(0), or where it was written from registers lgkmcnt(0)
+      __builtin_amdgcn_s_waitcnt(Held ? 0xc07f : 0x0f70);
+      __builtin_amdgcn_s_barrier();  // everyone's has, and the other buffer is free
       asm volatile("" ::: "memory");
-      if (t0 + KT < end) stage(t0 + KT, b ^ 1);
-      if (t0 > last || (a.window && t0 + KT - 1 <= first - a.window)) continue;  // none of the wave's rows sees it
+      if (t0 + KT < end) {
+        stage(t0 + KT, b ^ 1);
+        unpack(b ^ 1);
+        if (Held && t0 + 2 * KT < end) fetch(t0 + 2 * KT);
+      }
+      // none of the wave's rows sees it
+      if (V != kPrefix && (t0 > last || (window && t0 + KT - 1 <= first - window))) continue;
       const uint8_t *kt = lds + b * 2 * kTileBytes, *vt = kt + kTileBytes;
       f32x16 s[2] = {};
 #pragma unroll
@@ -721,7 +960,7 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_many_kernel(
 #pragma unroll
         for (int j = 0; j < 2; ++j)
           s[j] = mma(*(const u32x4 *)(kt + j * 64 * D + c * 512 + koff), q[c], s[j], E());
-      const bool edge = t0 + KT - 1 > first || (a.window && t0 <= last - a.window);
+      const bool edge = V != kPrefix && (t0 + KT - 1 > first || (window && t0 <= last - window));
       u32x4 p[4];
       if (!edge) {
         softmax_step<E, D, 2>(s, st, p, a.scale_log2);
@@ -744,7 +983,8 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_many_kernel(
           for (int i = 0; i < D / 32; ++i) st.acc[i] = mma(v[i], p[c], st.acc[i], E());
           __builtin_amdgcn_sched_barrier(0);
         }
-        if (odd) add_odd<E, D>(st, values, ids, pg0, shift, page_elems, t0, min(t0 + KT, end), pos, floor);
+        if (odd)
+          add_odd<E, D, S, false>(st, values, vs, kv.kv_heads, ids, pg0, shift, page_elems, t0, min(t0 + KT, end), pos, floor);
       }
     }
   }
@@ -754,7 +994,7 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_many_kernel(
   if (bad) l = __builtin_nanf("");
   const int trow = 32 * wave + n;
   if (u.slot >= 0 && half == 0) {
-    float *ml = part_ml<D, M>(a, u.slot, u.kvh, trow);
+    float *ml = unit_ml<D, M, V>(a, u.slot, u.kvh, trow);
     ml[0] = st.m, ml[1] = l;
   }
   const float inv = finish(l);
@@ -765,10 +1005,15 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_many_kernel(
       const f32x4 o{st.acc[i][4 * g], st.acc[i][4 * g + 1], st.acc[i][4 * g + 2], st.acc[i][4 * g + 3]};
       const int d = 32 * i + 8 * g + 4 * half;
       if (u.slot >= 0)
-        *(f32x4 *)(part_o<D, M>(a, u.slot, u.kvh, trow) + d) = o;
+        *(f32x4 *)(unit_o<D, M, V>(a, u.slot, u.kvh, trow) + d) = o;
       else
         store_out<E, D>(a, u.q, u.kvh, row, d, o * inv);
     }
+}
+
+template <class E, int D>
+__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_many_kernel(AttendArgs a) {
+  many_body<E, D, false, kAll>(a);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -777,8 +1022,8 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_many_kernel(
 // lanes share out a row's units, or several rows' where there are fewer units than groups.  Bound by the
 // latency of three dependent reads: 6 us for 512 units of one token, 3.5 with nothing to join.
 // ---------------------------------------------------------------------------------------------
-template <class E, int D, int M>
-__global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
+template <class E, int D, int M, Cover V>
+__device__ __forceinline__ void join_body(const AttendArgs &a) {
   constexpr int kPer = D / 4, kGroups = kThreads / kPer;
   __shared__ __align__(16) float sum[kGroups][D];
   __shared__ float stat[kGroups][2];
@@ -786,13 +1031,22 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
   const SplitTile t = split_tiles(a)->tile[item];
   if (item >= split_tiles(a)->count) return;
   // starts out of order can leave a note unwritten: nothing is taken from one that makes no sense
-  if (t.units < 2 || t.slot < 0 || t.slot > a.max_slots - t.units || t.rows < 1 || t.rows > M || t.first < 0 ||
+  if (t.units < (V == kBehind ? 1 : 2) || t.slot < 0 || t.slot > a.max_slots - t.units || t.rows < 1 || t.rows > M || t.first < 0 ||
       t.row0 < 0 || t.row0 > (1 << 28) || t.first > a.kv.n_tokens - 1 - (t.row0 + t.rows - 1) / a.kv.group)
     return;
+  // what the prefix's launch left of these rows: its units come first
+  Prefix pre{};
+  int pre_units = 0;
+  if constexpr (V == kBehind) {
+    pre = prefix_of(a);
+    const int64_t from = (int64_t)(t.first - pre.first) * a.kv.group + t.row0;
+    if (from >= 0 && from + t.rows <= pre.rows) pre_units = pre.units;
+  }
+  const int units = pre_units + t.units;
   const int g = threadIdx.x / kPer, d = threadIdx.x % kPer * 4;
   // groups to a row: a power of two, so that a tile of few units has several rows joined at once
   int per = 1;
-  while (per < kGroups && per < t.units) per *= 2;
+  while (per < kGroups && per < units) per *= 2;
   const int own = g / per, at_once = kGroups / per;
   const int64_t step = (int64_t)a.kv.kv_heads * M;  // rows from unit to unit
   for (int r0 = 0; (int)(blockIdx.y + gridDim.y * r0) < t.rows; r0 += at_once) {
@@ -801,10 +1055,18 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
     f32x4 o{};
     if (row < t.rows) {
       const float *ml = part_ml<D, M>(a, t.slot, kvh, row), *part = part_o<D, M>(a, t.slot, kvh, row) + d;
+      const int at = V == kBehind ? (t.first - pre.first) * a.kv.group + t.row0 + row : 0;
+      const int64_t front = V == kBehind ? front_row(a, at / a.prefix_rows * a.prefix_splits, kvh, at % a.prefix_rows) : 0;
 #pragma unroll 4
-      for (int i = g % per; i < t.units; i += per) {
-        const float mi = ml[i * step * 2], li = ml[i * step * 2 + 1];
-        const f32x4 oi = *(const f32x4 *)(part + i * step * D);
+      for (int i = g % per; i < units; i += per) {
+        const float *mli = ml + (i - pre_units) * step * 2, *parti = part + (i - pre_units) * step * D;
+        if (V == kBehind && i < pre_units) {
+          const int64_t from = front + (int64_t)i * a.kv.kv_heads * a.prefix_rows;
+          mli = front_ml<D>(a, from);
+          parti = front_o<D>(a, from) + d;
+        }
+        const float mi = mli[0], li = mli[1];
+        const f32x4 oi = *(const f32x4 *)parti;
         const float top = fmaxf(m, mi), base = top == kNegInf ? 0.f : top;
         const float w = __builtin_amdgcn_exp2f(mi - base), shrink = __builtin_amdgcn_exp2f(m - base);
         l = l * shrink + w * li;
@@ -832,12 +1094,31 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
   }
 }
 
+template <class E, int D, int M>
+__global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
+  join_body<E, D, M, kAll>(a);
+}
+
 }  // namespace
 static inline uint64_t attend_work_size(const AttendArgs &a, int rows, int dim) {
   return sizeof(SplitTiles) + a.max_tiles * sizeof(SplitTile) + plan_ints(a) * sizeof(int32_t) +
          (uint64_t)a.max_slots * a.kv.kv_heads * rows * (dim + 2) * sizeof(float);
 }
 namespace {
+
+// Blocks that join: most have nothing to do.  About 4096 in all, 8 to rows / 4 of them to a tile.
+static inline dim3 join_grid(const AttendArgs &a, int rows) {
+  const int tiles = a.max_tiles * a.kv.kv_heads;
+  int y = 8;
+  while (2 * y <= rows / 4 && 2 * y * tiles <= 4096) y *= 2;
+  return dim3(tiles, y);
+}
+template <class E, int D>
+const void *join_kernel(int rows) {
+  return rows == 32   ? (const void *)attend_join_kernel<E, D, 32>
+         : rows == 64 ? (const void *)attend_join_kernel<E, D, 64>
+                      : (const void *)attend_join_kernel<E, D, 128>;
+}
 
 template <class E, int D, int M>
 hipError_t launch_kernels(const AttendArgs &a, hipStream_t s) {
@@ -848,18 +1129,30 @@ hipError_t launch_kernels(const AttendArgs &a, hipStream_t s) {
     fn = (const void *)attend_many_kernel<E, D>;
   else
     fn = (const void *)attend_few_kernel<E, D, M / 32>;
-  hipError_t e = hipSuccess;
-  if (a.kv.n_seqs > kPlanSeqs) e = hipLaunchKernel((const void *)plan_kernel<M>, dim3(1), dim3(kPlanThreads), args, 0, s);
+  hipError_t e = launch_plan<D>(a, M, s);
   if (e == hipSuccess) e = hipLaunchKernel(fn, grid, dim3(kThreads), args, 0, s);
   if (e != hipSuccess) return e;
-  // most blocks have nothing to join: about 4096 in all, 8 to M / 4 of them to a tile
-  const int tiles = a.max_tiles * a.kv.kv_heads;
-  int y = 8;
-  while (2 * y <= M / 4 && 2 * y * tiles <= 4096) y *= 2;
-  return hipLaunchKernel((const void *)attend_join_kernel<E, D, M>, dim3(tiles, y), dim3(kThreads), args, 0, s);
+  return hipLaunchKernel(join_kernel<E, D>(M), join_grid(a, M), dim3(kThreads), args, 0, s);
 }
 
 }  // namespace
+
+template <int D>
+hipError_t launch_plan(const AttendArgs &a, int rows, hipStream_t s) {
+  if (a.kv.n_seqs <= kPlanSeqs) return hipSuccess;
+  void *args[] = {const_cast<AttendArgs *>(&a)};
+  const void *fn = rows == 32   ? (const void *)plan_kernel<32>
+                   : rows == 64 ? (const void *)plan_kernel<64>
+                                : (const void *)plan_kernel<128>;
+  return hipLaunchKernel(fn, dim3(1), dim3(kPlanThreads), args, 0, s);
+}
+
+template <int D>
+hipError_t launch_join(const AttendArgs &a, bool half, int rows, hipStream_t s) {
+  void *args[] = {const_cast<AttendArgs *>(&a)};
+  return hipLaunchKernel(half ? join_kernel<_Float16, D>(rows) : join_kernel<__bf16, D>(rows), join_grid(a, rows),
+                         dim3(kThreads), args, 0, s);
+}
 
 template <int D>
 hipError_t launch_attend(const AttendArgs &a, bool half, int rows, hipStream_t s) {

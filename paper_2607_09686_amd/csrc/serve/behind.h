@@ -1,0 +1,108 @@
+// Attention over a cache of 8 bits, and of a batch whose sequences begin with the same tokens.
+//
+// What all sequences begin with is read once: with S its tokens (whole 64s of them),
+//
+//   o = (l1 o1 2^(m1 - m) + l2 o2 2^(m2 - m)) / (l1 2^(m1 - m) + l2 2^(m2 - m)),   m = max(m1, m2)
+//
+// joins a row's sums over the keys before S and from S on.  The first come from a launch that takes the whole
+// batch's rows as those of one sequence (no row there has a mask, so they need not know their own), the second
+// from the ordinary one with its ranges cut at S, every tile of which leaves partial results.
+#pragma once
+
+#include "attend.h"
+
+namespace moecache {
+// these are in the ordinary attention's files
+extern template hipError_t launch_plan<64>(const AttendArgs &, int, hipStream_t);
+extern template hipError_t launch_plan<128>(const AttendArgs &, int, hipStream_t);
+extern template hipError_t launch_plan<256>(const AttendArgs &, int, hipStream_t);
+extern template hipError_t launch_join<64>(const AttendArgs &, bool, int, hipStream_t);
+extern template hipError_t launch_join<128>(const AttendArgs &, bool, int, hipStream_t);
+extern template hipError_t launch_join<256>(const AttendArgs &, bool, int, hipStream_t);
+namespace {
+
+template <class E, int D, int R>
+__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void held_few_kernel(AttendArgs a) {
+  few_body<E, D, R, true, kAll>(a);
+}
+template <class E, int D>
+__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void held_many_kernel(AttendArgs a) {
+  many_body<E, D, true, kAll>(a);
+}
+template <class E, int D, int R, bool Held>
+__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void behind_few_kernel(AttendArgs a) {
+  few_body<E, D, R, Held, kBehind>(a);
+}
+template <class E, int D, bool Held>
+__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void behind_many_kernel(AttendArgs a) {
+  many_body<E, D, Held, kBehind>(a);
+}
+template <class E, int D, int R, bool Held>
+__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void prefix_few_kernel(AttendArgs a) {
+  few_body<E, D, R, Held, kPrefix>(a);
+}
+template <class E, int D, bool Held>
+__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void prefix_many_kernel(AttendArgs a) {
+  many_body<E, D, Held, kPrefix>(a);
+}
+template <int M>
+__global__ __launch_bounds__(kPlanThreads) void plan_behind_kernel(AttendArgs a) {
+  plan_body<M, kBehind>(a);
+}
+template <class E, int D, int M>
+__global__ __launch_bounds__(kThreads) void join_behind_kernel(AttendArgs a) {
+  join_body<E, D, M, kBehind>(a);
+}
+
+template <class E, int D, bool Held>
+hipError_t launch_behind(const AttendArgs &a, int rows, hipStream_t s) {
+  void *args[] = {const_cast<AttendArgs *>(&a)};
+  hipError_t e = hipSuccess;
+  if (a.kv.n_seqs > kPlanSeqs)
+    e = hipLaunchKernel(rows == 32   ? (const void *)plan_behind_kernel<32>
+                        : rows == 64 ? (const void *)plan_behind_kernel<64>
+                                     : (const void *)plan_behind_kernel<128>,
+                        dim3(1), dim3(kPlanThreads), args, 0, s);
+  if (e == hipSuccess)
+    e = hipLaunchKernel(a.prefix_rows == 32   ? (const void *)prefix_few_kernel<E, D, 1, Held>
+                        : a.prefix_rows == 64 ? (const void *)prefix_few_kernel<E, D, 2, Held>
+                                              : (const void *)prefix_many_kernel<E, D, Held>,
+                        dim3((unsigned)((int64_t)a.prefix_tiles * a.prefix_splits * a.kv.kv_heads)), dim3(kThreads), args, 0, s);
+  if (e == hipSuccess)
+    e = hipLaunchKernel(rows == 32   ? (const void *)behind_few_kernel<E, D, 1, Held>
+                        : rows == 64 ? (const void *)behind_few_kernel<E, D, 2, Held>
+                                     : (const void *)behind_many_kernel<E, D, Held>,
+                        dim3((unsigned)((int64_t)a.max_units * a.kv.kv_heads)), dim3(kThreads), args, 0, s);
+  if (e != hipSuccess) return e;
+  return hipLaunchKernel(rows == 32   ? (const void *)join_behind_kernel<E, D, 32>
+                         : rows == 64 ? (const void *)join_behind_kernel<E, D, 64>
+                                      : (const void *)join_behind_kernel<E, D, 128>,
+                         join_grid(a, rows), dim3(kThreads), args, 0, s);
+}
+
+template <class E, int D>
+hipError_t launch_held(const AttendArgs &a, int rows, hipStream_t s) {
+  void *args[] = {const_cast<AttendArgs *>(&a)};
+  hipError_t e = launch_plan<D>(a, rows, s);
+  if (e == hipSuccess)
+    e = hipLaunchKernel(rows == 32   ? (const void *)held_few_kernel<E, D, 1>
+                        : rows == 64 ? (const void *)held_few_kernel<E, D, 2>
+                                     : (const void *)held_many_kernel<E, D>,
+                        dim3((unsigned)((int64_t)a.max_units * a.kv.kv_heads)), dim3(kThreads), args, 0, s);
+  return e == hipSuccess ? launch_join<D>(a, __is_same(E, _Float16), rows, s) : e;
+}
+
+template <class E, int D>
+hipError_t launch_ext(const AttendArgs &a, int rows, hipStream_t s) {
+  if (!a.shared) return launch_held<E, D>(a, rows, s);
+  return a.kv.key_scales ? launch_behind<E, D, true>(a, rows, s) : launch_behind<E, D, false>(a, rows, s);
+}
+
+}  // namespace
+
+template <int D>
+hipError_t launch_attend_ext(const AttendArgs &a, bool half, int rows, hipStream_t s) {
+  return half ? launch_ext<_Float16, D>(a, rows, s) : launch_ext<__bf16, D>(a, rows, s);
+}
+
+}  // namespace moecache

@@ -1,0 +1,6 @@
+// Attention over a cache of 8 bits and behind shared tokens, for heads of 128 elements.
+#include "behind.h"
+
+namespace moecache {
+template hipError_t launch_attend_ext<128>(const AttendArgs &, bool, int, hipStream_t);
+}  // namespace moecache

@@ -1,0 +1,95 @@
+// The keys and values of the batch's tokens, taken out of a paged cache of 16 or 8 bits as rows (the
+// inverse of appending, without its turn).
+//
+// Bound by the bytes it moves.  A block takes the tokens of one sequence within one aligned run of
+// eight positions, as appending does.  Of keys a lane takes 16 bytes of the cache; of values 16 bytes
+// of eight tokens, which it writes as a piece of each token's row, a wave's pieces next to each other.
+#include "append.h"
+#include "held.h"
+
+namespace moecache {
+namespace {
+
+template <class E, bool Held>
+__global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a) {
+  constexpr int kUnit = Held ? 16 : 8;  // elements in 16 bytes
+  const KvView &kv = a.kv;
+  Run r;
+  if (!run_of(kv, &r)) return;
+  const int n = r.n, D = a.dim, P = 1 << kv.page_shift, in_page = r.position & (P - 1);
+  const int64_t pool = (int64_t)r.page * kv.kv_heads, head_elems = (int64_t)D << kv.page_shift;
+  const u32x4 nan = __builtin_bit_cast(u32x4, pack<E>({__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""),
+                                                       __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""),
+                                                       __builtin_nanf(""), __builtin_nanf("")}));
+  const int units = D / kUnit;
+  for (int i = blockIdx.y * kThreads + threadIdx.x; i < kv.kv_heads * units * kRun; i += gridDim.y * kThreads) {
+    const int t = i % kRun, u = i / kRun % units, head = i / kRun / units, tp = in_page + t;
+    if (t >= n) continue;
+    uint16_t *dst = (uint16_t *)a.k + (int64_t)(r.row + t) * a.k_stride + head * D + u * kUnit;
+    if (!r.write) {
+      *(u32x4 *)dst = nan;
+      if (Held) *(u32x4 *)(dst + 8) = nan;
+      continue;
+    }
+    const int64_t at = (pool + head) * head_elems + (tp & ~15) * D + (u * 16 + (tp & 15)) * kUnit;
+    if constexpr (Held) {
+      const u32x4 c = *(const u32x4 *)((const uint8_t *)kv.keys + at);
+      const float s = scale_of(kv.key_scales[((pool + head) << kv.page_shift) + tp]);
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        *(u32x4 *)(dst + 8 * j) = u32x4{decode(c[2 * j], false, s, E()), decode(c[2 * j], true, s, E()),
+                                        decode(c[2 * j + 1], false, s, E()), decode(c[2 * j + 1], true, s, E())};
+    } else {
+      *(u32x4 *)dst = *(const u32x4 *)(kv.keys + at);
+    }
+  }
+  // two neighbouring elements of all eight tokens to a thread
+  const int tp = in_page & ~7;
+  for (int i = blockIdx.y * kThreads + threadIdx.x; i < kv.kv_heads * D / 2; i += gridDim.y * kThreads) {
+    const int head = i / (D / 2), d = i % (D / 2) * 2;
+    uint32_t out[kRun];
+    if (!r.write) {
+#pragma unroll
+      for (int t = 0; t < kRun; ++t) out[t] = nan[0];
+    } else if constexpr (Held) {
+      const u32x4 c = *(const u32x4 *)((const uint8_t *)kv.values + (pool + head) * head_elems + tp * D + d * 8);
+      const uint2 e = *(const uint2 *)(kv.value_scales + ((pool + head) << kv.page_shift) + tp);
+#pragma unroll
+      for (int t = 0; t < kRun; t += 2) {
+        const float s0 = scale_of((t < 4 ? e.x : e.y) >> (8 * (t % 4)) & 255), s1 = scale_of((t < 4 ? e.x : e.y) >> (8 * (t % 4) + 8) & 255);
+        const uint32_t x = decode2(c[t / 4], t % 4 != 0, s0, s1, E()), y = decode2(c[2 + t / 4], t % 4 != 0, s0, s1, E());
+        out[t] = __builtin_amdgcn_perm(y, x, 0x05040100);
+        out[t + 1] = __builtin_amdgcn_perm(y, x, 0x07060302);
+      }
+    } else {
+      const u32x4 *src = (const u32x4 *)(kv.values + (pool + head) * head_elems + tp * D + d * 8);
+      const u32x4 x = src[0], y = src[1];
+#pragma unroll
+      for (int t = 0; t < kRun; t += 2) {
+        out[t] = __builtin_amdgcn_perm(y[t / 2], x[t / 2], 0x05040100);
+        out[t + 1] = __builtin_amdgcn_perm(y[t / 2], x[t / 2], 0x07060302);
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < kRun; ++t) {
+      const int row = t - (in_page & 7);
+      if (row >= 0 && row < n) *(uint32_t *)((uint16_t *)a.v + (int64_t)(r.row + row) * a.v_stride + head * D + d) = out[t];
+    }
+  }
+}
+
+template <class E>
+hipError_t launch(const ReadArgs &a, hipStream_t s) {
+  void *args[] = {const_cast<ReadArgs *>(&a)};
+  const int runs = a.kv.n_tokens / kRun + 2 * a.kv.n_seqs;
+  const void *fn = a.kv.key_scales ? (const void *)read_kernel<E, true> : (const void *)read_kernel<E, false>;
+  return hipLaunchKernel(fn, dim3(runs, kShares), dim3(kThreads), args, 0, s);
+}
+
+}  // namespace
+
+hipError_t launch_read(const ReadArgs &a, bool half, hipStream_t s) {
+  return half ? launch<_Float16>(a, s) : launch<__bf16>(a, s);
+}
+
+}  // namespace moecache

@@ -86,7 +86,17 @@ int check_kv(const moe_kv_batch *b, const char *who, KvView *kv) {
   while (1 << shift < P) ++shift;
   *kv = KvView{(uint16_t *)b->keys, (uint16_t *)b->values, b->pages, b->starts, b->lengths, b->status,
                b->n_seqs, b->n_tokens, b->n_heads, b->n_kv_heads, b->n_heads / b->n_kv_heads,
-               shift, b->n_pages, b->max_pages};
+               shift, b->n_pages, b->max_pages, nullptr, nullptr};
+  return MOE_OK;
+}
+
+// The same with the scales of pools of 8 bits, if given.
+int check_kv_ext(const moe_kv_batch *b, const moe_kv_scales *scales, const char *who, KvView *kv) {
+  const int rc = check_kv(b, who, kv);
+  if (rc || !scales) return rc;
+  if (!scales->keys || !scales->values || !aligned(scales->keys) || !aligned(scales->values))
+    return fail(MOE_EINVAL, "%s: the scales must be 16-byte aligned device pointers", who);
+  kv->key_scales = scales->keys, kv->value_scales = scales->values;
   return MOE_OK;
 }
 
@@ -104,6 +114,19 @@ bool rows_ok(const void *p, int64_t stride, int heads, int dim, int size) {
 int tile_rows(const KvView &kv) {
   const int64_t rows = (int64_t)kv.n_tokens * kv.group;
   return rows <= (int64_t)32 * kv.n_seqs ? 32 : rows <= (int64_t)64 * kv.n_seqs ? 64 : 128;
+}
+
+// The launch over what all sequences begin with: tiles of all rows together, each cut into as many units
+// as the card has places for it, of kManyMinKeys keys and more where its pages are full.
+void plan_prefix(AttendArgs *a, int dim) {
+  const KvView &kv = a->kv;
+  const int64_t rows = (int64_t)kv.n_tokens * kv.group, keys = (int64_t)a->prefix_pages << kv.page_shift;
+  a->prefix_rows = rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+  a->prefix_tiles = (int)((rows + a->prefix_rows - 1) / a->prefix_rows);
+  const int resident = a->prefix_rows < 128 && dim > 128 ? kResident / 2 : kResident;
+  const int min_keys = a->prefix_rows < 128 ? kFewMinKeys : kManyMinKeys;
+  const int64_t most = std::max<int64_t>(1, keys / min_keys);
+  a->prefix_splits = (int)std::min(most, std::max<int64_t>(1, resident / ((int64_t)a->prefix_tiles * kv.kv_heads)));
 }
 
 int plan(AttendArgs *a, uint64_t *bytes, int dim) {
@@ -126,8 +149,90 @@ int plan(AttendArgs *a, uint64_t *bytes, int dim) {
   a->max_units = (int)std::min(share + tiles, tiles * most);
   a->max_slots = (int)std::min(2 * share, tiles * most);
   a->max_tiles = (int)std::min(share, tiles);
+  if (a->shared) {  // every tile's units leave partial results, and a note
+    a->max_slots = a->max_units;
+    a->max_tiles = (int)tiles;
+    plan_prefix(a, dim);
+  }
   *bytes = attend_work_bytes(*a, rows, dim);
+  if (a->shared) *bytes += front_bytes(*a, dim);
   return rows;
+}
+
+int check_prefix(const moe_kv_prefix *p, const char *who, AttendArgs *a) {
+  if (!p) return MOE_OK;
+  if (!p->pages || !p->tokens) return fail(MOE_EINVAL, "%s: the prefix's pages and tokens must not be NULL", who);
+  if (p->n_pages < 1 || ((int64_t)p->n_pages << a->kv.page_shift) > (1 << 30))
+    return fail(MOE_EINVAL, "%s: the prefix's n_pages must be >= 1, n_pages * page_tokens <= 2^30", who);
+  a->prefix = p->pages, a->shared = p->tokens, a->prefix_pages = p->n_pages;
+  return MOE_OK;
+}
+
+// What the two forms of appending have in common, from the checked view on.
+int append(AppendArgs &a, const moe_kv_batch *b, const moe_kv_rope *rope, int32_t in_dtype, const void *k,
+           int64_t k_stride, const void *v, int64_t v_stride, const void *q, int64_t q_stride, void *q_out,
+           int64_t q_out_stride, const char *who) {
+  if (in_dtype != MOE_F32 && in_dtype != b->dtype)
+    return fail(MOE_EINVAL, "%s: in_dtype must be the cache's dtype or MOE_F32", who);
+  if (rope) {
+    if (rope->dim < 0 || rope->dim > b->head_dim || rope->dim % 16)
+      return fail(MOE_EINVAL, "%s: rope dim must be a multiple of 16 up to head_dim", who);
+    if (rope->dim && !rope->freq) return fail(MOE_EINVAL, "%s: rope freq is NULL", who);
+  }
+  if (b->n_tokens == 0 || b->n_seqs == 0) return MOE_OK;
+  const int size = in_dtype == MOE_F32 ? 4 : 2;
+  if (!rows_ok(k, k_stride, b->n_kv_heads, b->head_dim, size) || !rows_ok(v, v_stride, b->n_kv_heads, b->head_dim, size))
+    return fail(MOE_EINVAL, "%s: k and v must be 16-byte aligned rows of n_kv_heads * head_dim elements", who);
+  if (q && (!rows_ok(q, q_stride, b->n_heads, b->head_dim, size) ||
+            !rows_ok(q_out, q_out_stride, b->n_heads, b->head_dim, 2)))
+    return fail(MOE_EINVAL, "%s: q and q_out must be 16-byte aligned rows of n_heads * head_dim elements", who);
+  a.q = q, a.k = k, a.v = v, a.q_out = q_out;
+  a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride, a.q_out_stride = q_out_stride;
+  a.freq = rope ? rope->freq : nullptr;
+  a.dim = b->head_dim;
+  a.rope_dim = rope ? rope->dim : 0;
+  a.adjacent = rope ? rope->adjacent != 0 : 0;
+  const hipStream_t s = (hipStream_t)b->hip_stream;
+  const bool half = b->dtype == MOE_F16, in_f32 = in_dtype == MOE_F32;
+  DeviceScope scope;
+  hipError_t e = scope.enter(s);
+  if (e == hipSuccess)
+    e = a.q_norm || a.k_norm || a.kv.key_scales ? launch_append_ext(a, half, in_f32, s) : launch_append(a, half, in_f32, s);
+  return e == hipSuccess ? MOE_OK : hip_fail(who, e);
+}
+
+// And of attention: the plan, the launches.
+int attend(AttendArgs &a, const moe_kv_batch *b, int32_t window, float scale, const void *q, int64_t q_stride, void *out,
+           int64_t out_stride, void *workspace, uint64_t workspace_bytes, const char *who) {
+  if (window < 0) return fail(MOE_EINVAL, "%s: window must be >= 0", who);
+  a.scale_log2 = scale * 1.44269504088896340736f;
+  if (!(scale > 0.f) || !std::isfinite(a.scale_log2))
+    return fail(MOE_EINVAL, "%s: scale must be positive and finite, and its log2(e)-fold too", who);
+  if (b->n_tokens == 0 || b->n_seqs == 0) return MOE_OK;
+  if (!rows_ok(q, q_stride, b->n_heads, b->head_dim, 2) || !rows_ok(out, out_stride, b->n_heads, b->head_dim, 2))
+    return fail(MOE_EINVAL, "%s: q and out must be 16-byte aligned rows of n_heads * head_dim elements", who);
+  uint64_t bytes;
+  const int rows = plan(&a, &bytes, b->head_dim);
+  if (!workspace || !aligned(workspace) || workspace_bytes < bytes)
+    return fail(MOE_EINVAL, "%s: the workspace must be 16-byte aligned and of at least %llu bytes", who,
+                (unsigned long long)bytes);
+  a.q = q, a.out = out, a.q_stride = q_stride, a.out_stride = out_stride;
+  a.window = window;
+  a.work = workspace;
+  const bool half = b->dtype == MOE_F16, ext = a.shared || a.kv.key_scales;
+  if (a.shared) a.front = (float *)((uint8_t *)workspace + attend_work_bytes(a, rows, b->head_dim));
+  const hipStream_t s = (hipStream_t)b->hip_stream;
+  DeviceScope scope;
+  hipError_t e = scope.enter(s);
+  if (e == hipSuccess) {
+    if (b->head_dim == 64)
+      e = ext ? launch_attend_ext<64>(a, half, rows, s) : launch_attend<64>(a, half, rows, s);
+    else if (b->head_dim == 128)
+      e = ext ? launch_attend_ext<128>(a, half, rows, s) : launch_attend<128>(a, half, rows, s);
+    else
+      e = ext ? launch_attend_ext<256>(a, half, rows, s) : launch_attend<256>(a, half, rows, s);
+  }
+  return e == hipSuccess ? MOE_OK : hip_fail(who, e);
 }
 
 }  // namespace
@@ -139,32 +244,43 @@ int moe_kv_append(const moe_kv_batch *b, const moe_kv_rope *rope, int32_t in_dty
                   int64_t q_out_stride) {
   AppendArgs a{};
   const int rc = check_kv(b, "moe_kv_append", &a.kv);
+  return rc ? rc : append(a, b, rope, in_dtype, k, k_stride, v, v_stride, q, q_stride, q_out, q_out_stride, "moe_kv_append");
+}
+
+int moe_kv_append_ext(const moe_kv_batch *b, const moe_kv_scales *scales, const moe_kv_rope *rope, const moe_kv_norm *norm,
+                      int32_t in_dtype, const void *k, int64_t k_stride, const void *v, int64_t v_stride, const void *q,
+                      int64_t q_stride, void *q_out, int64_t q_out_stride) {
+  const char *who = "moe_kv_append_ext";
+  AppendArgs a{};
+  const int rc = check_kv_ext(b, scales, who, &a.kv);
   if (rc) return rc;
-  if (in_dtype != MOE_F32 && in_dtype != b->dtype)
-    return fail(MOE_EINVAL, "moe_kv_append: in_dtype must be the cache's dtype or MOE_F32");
-  if (rope) {
-    if (rope->dim < 0 || rope->dim > b->head_dim || rope->dim % 16)
-      return fail(MOE_EINVAL, "moe_kv_append: rope dim must be a multiple of 16 up to head_dim");
-    if (rope->dim && !rope->freq) return fail(MOE_EINVAL, "moe_kv_append: rope freq is NULL");
+  if (norm) {
+    if (norm->dtype != MOE_F32 && norm->dtype != b->dtype)
+      return fail(MOE_EINVAL, "%s: the norm's dtype must be the cache's or MOE_F32", who);
+    if (!(norm->eps >= 0.f) || !std::isfinite(norm->eps))
+      return fail(MOE_EINVAL, "%s: the norm's eps must not be negative, and finite", who);
+    if (!aligned(norm->q_weight) || !aligned(norm->k_weight))
+      return fail(MOE_EINVAL, "%s: the norm's weights must be 16-byte aligned device pointers", who);
+    if (norm->q_weight && !q && b->n_tokens && b->n_seqs) return fail(MOE_EINVAL, "%s: a norm of q without q", who);
+    a.q_norm = norm->q_weight, a.k_norm = norm->k_weight;
+    a.norm_f32 = norm->dtype == MOE_F32, a.eps = norm->eps;
   }
+  return append(a, b, rope, in_dtype, k, k_stride, v, v_stride, q, q_stride, q_out, q_out_stride, who);
+}
+
+int moe_kv_read(const moe_kv_batch *b, const moe_kv_scales *scales, void *k, int64_t k_stride, void *v, int64_t v_stride) {
+  ReadArgs a{};
+  const int rc = check_kv_ext(b, scales, "moe_kv_read", &a.kv);
+  if (rc) return rc;
   if (b->n_tokens == 0 || b->n_seqs == 0) return MOE_OK;
-  const int size = in_dtype == MOE_F32 ? 4 : 2;
-  if (!rows_ok(k, k_stride, b->n_kv_heads, b->head_dim, size) || !rows_ok(v, v_stride, b->n_kv_heads, b->head_dim, size))
-    return fail(MOE_EINVAL, "moe_kv_append: k and v must be 16-byte aligned rows of n_kv_heads * head_dim elements");
-  if (q && (!rows_ok(q, q_stride, b->n_heads, b->head_dim, size) ||
-            !rows_ok(q_out, q_out_stride, b->n_heads, b->head_dim, 2)))
-    return fail(MOE_EINVAL, "moe_kv_append: q and q_out must be 16-byte aligned rows of n_heads * head_dim elements");
-  a.q = q, a.k = k, a.v = v, a.q_out = q_out;
-  a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride, a.q_out_stride = q_out_stride;
-  a.freq = rope ? rope->freq : nullptr;
-  a.dim = b->head_dim;
-  a.rope_dim = rope ? rope->dim : 0;
-  a.adjacent = rope ? rope->adjacent != 0 : 0;
+  if (!rows_ok(k, k_stride, b->n_kv_heads, b->head_dim, 2) || !rows_ok(v, v_stride, b->n_kv_heads, b->head_dim, 2))
+    return fail(MOE_EINVAL, "moe_kv_read: k and v must be 16-byte aligned rows of n_kv_heads * head_dim elements");
+  a.k = k, a.v = v, a.k_stride = k_stride, a.v_stride = v_stride, a.dim = b->head_dim;
   const hipStream_t s = (hipStream_t)b->hip_stream;
   DeviceScope scope;
   hipError_t e = scope.enter(s);
-  if (e == hipSuccess) e = launch_append(a, b->dtype == MOE_F16, in_dtype == MOE_F32, s);
-  return e == hipSuccess ? MOE_OK : hip_fail("moe_kv_append", e);
+  if (e == hipSuccess) e = launch_read(a, b->dtype == MOE_F16, s);
+  return e == hipSuccess ? MOE_OK : hip_fail("moe_kv_read", e);
 }
 
 int moe_kv_attend_workspace(const moe_kv_batch *b, uint64_t *bytes) {
@@ -180,31 +296,31 @@ int moe_kv_attend(const moe_kv_batch *b, int32_t window, float scale, const void
                   int64_t out_stride, void *workspace, uint64_t workspace_bytes) {
   AttendArgs a{};
   const int rc = check_kv(b, "moe_kv_attend", &a.kv);
+  return rc ? rc : attend(a, b, window, scale, q, q_stride, out, out_stride, workspace, workspace_bytes, "moe_kv_attend");
+}
+
+int moe_kv_attend_ext_workspace(const moe_kv_batch *b, const moe_kv_scales *scales, const moe_kv_prefix *prefix,
+                                uint64_t *bytes) {
+  const char *who = "moe_kv_attend_ext_workspace";
+  AttendArgs a{};
+  if (!bytes) return fail(MOE_EINVAL, "%s: bytes is NULL", who);
+  int rc = check_kv_ext(b, scales, who, &a.kv);
+  if (!rc) rc = check_prefix(prefix, who, &a);
   if (rc) return rc;
-  if (window < 0) return fail(MOE_EINVAL, "moe_kv_attend: window must be >= 0");
-  a.scale_log2 = scale * 1.44269504088896340736f;
-  if (!(scale > 0.f) || !std::isfinite(a.scale_log2))
-    return fail(MOE_EINVAL, "moe_kv_attend: scale must be positive and finite, and its log2(e)-fold too");
-  if (b->n_tokens == 0 || b->n_seqs == 0) return MOE_OK;
-  if (!rows_ok(q, q_stride, b->n_heads, b->head_dim, 2) || !rows_ok(out, out_stride, b->n_heads, b->head_dim, 2))
-    return fail(MOE_EINVAL, "moe_kv_attend: q and out must be 16-byte aligned rows of n_heads * head_dim elements");
-  uint64_t bytes;
-  const int rows = plan(&a, &bytes, b->head_dim);
-  if (!workspace || !aligned(workspace) || workspace_bytes < bytes)
-    return fail(MOE_EINVAL, "moe_kv_attend: the workspace must be 16-byte aligned and of at least %llu bytes",
-                (unsigned long long)bytes);
-  a.q = q, a.out = out, a.q_stride = q_stride, a.out_stride = out_stride;
-  a.window = window;
-  a.work = workspace;
-  const hipStream_t s = (hipStream_t)b->hip_stream;
-  DeviceScope scope;
-  hipError_t e = scope.enter(s);
-  const bool half = b->dtype == MOE_F16;
-  if (e == hipSuccess)
-    e = b->head_dim == 64    ? launch_attend<64>(a, half, rows, s)
-        : b->head_dim == 128 ? launch_attend<128>(a, half, rows, s)
-                             : launch_attend<256>(a, half, rows, s);
-  return e == hipSuccess ? MOE_OK : hip_fail("moe_kv_attend", e);
+  plan(&a, bytes, b->head_dim);
+  return MOE_OK;
+}
+
+int moe_kv_attend_ext(const moe_kv_batch *b, const moe_kv_scales *scales, const moe_kv_prefix *prefix, int32_t window,
+                      float scale, const void *q, int64_t q_stride, void *out, int64_t out_stride, void *workspace,
+                      uint64_t workspace_bytes) {
+  const char *who = "moe_kv_attend_ext";
+  AttendArgs a{};
+  int rc = check_kv_ext(b, scales, who, &a.kv);
+  if (!rc) rc = check_prefix(prefix, who, &a);
+  if (rc) return rc;
+  if (prefix && window) return fail(MOE_EINVAL, "%s: a window and a prefix do not go together", who);
+  return attend(a, b, window, scale, q, q_stride, out, out_stride, workspace, workspace_bytes, who);
 }
 
 int moe_sample_workspace(const moe_sample_batch *b, uint64_t *bytes) {

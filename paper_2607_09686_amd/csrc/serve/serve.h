@@ -17,6 +17,7 @@ struct KvView {
   int32_t *status;           // nullable
   int n_seqs, n_tokens, heads, kv_heads, group;
   int page_shift, n_pages, max_pages;
+  uint8_t *key_scales, *value_scales;  // 8-bit pools' exponents, [n_pages][kv_heads][P]; null: pools of 16 bits
 };
 
 // bits of *status
@@ -29,6 +30,16 @@ struct AppendArgs {
   int64_t q_stride, k_stride, v_stride, q_out_stride;  // elements from token to token
   const double *freq;                // [rope_dim / 2] radians per position
   int dim, rope_dim, adjacent;
+  const void *q_norm, *k_norm;       // [dim] weights, nullable
+  int norm_f32;                      // their type: fp32, else the cache's
+  float eps;
+};
+
+struct ReadArgs {
+  KvView kv;
+  void *k, *v;
+  int64_t k_stride, v_stride;  // elements from token to token
+  int dim;
 };
 
 struct AttendArgs {
@@ -45,15 +56,35 @@ struct AttendArgs {
   int max_tiles;       // split tiles
   bool nearest;        // how a tile's units are rounded, see units_of
   void *work;          // attend_work_bytes
+  // what all sequences begin with (shared null: nothing), see behind.h
+  const int32_t *prefix;  // [prefix_pages] page ids
+  const int32_t *shared;  // tokens
+  int prefix_pages;
+  int prefix_rows;     // rows of a tile of the prefix's launch
+  int prefix_tiles;
+  int prefix_splits;   // a tile's units
+  float *front;        // its partial results, front_floats of them
 };
 
 // in_f32: q, k, v hold fp32 instead of the cache's type; half: the cache's type is fp16
 hipError_t launch_append(const AppendArgs &a, bool half, bool in_f32, hipStream_t s);
+// the same with norms, or to a cache of 8 bits
+hipError_t launch_append_ext(const AppendArgs &a, bool half, bool in_f32, hipStream_t s);
+hipError_t launch_read(const ReadArgs &a, bool half, hipStream_t s);
 
 // rows: of a tile, 32, 64 or 128
 uint64_t attend_work_bytes(const AttendArgs &a, int rows, int dim);
 template <int D>
 hipError_t launch_attend(const AttendArgs &a, bool half, int rows, hipStream_t s);
+// the parts of it that do not read the cache: the plan of many sequences, and the joining of split tiles
+template <int D>
+hipError_t launch_plan(const AttendArgs &a, int rows, hipStream_t s);
+template <int D>
+hipError_t launch_join(const AttendArgs &a, bool half, int rows, hipStream_t s);
+// over a cache of 8 bits, or behind tokens that all sequences begin with
+uint64_t front_bytes(const AttendArgs &a, int dim);
+template <int D>
+hipError_t launch_attend_ext(const AttendArgs &a, bool half, int rows, hipStream_t s);
 
 struct SampleArgs {
   const void *logits;

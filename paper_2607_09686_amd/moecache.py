@@ -99,6 +99,20 @@ class KvRope(ctypes.Structure):
     _fields_ = [("dim", ctypes.c_int32), ("adjacent", ctypes.c_int32), ("freq", ctypes.c_void_p)]
 
 
+class KvScales(ctypes.Structure):
+    _fields_ = [("keys", ctypes.c_void_p), ("values", ctypes.c_void_p)]
+
+
+class KvNorm(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("dtype", ctypes.c_int32),
+                ("eps", ctypes.c_float)]
+
+
+class KvPrefix(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_void_p), ("tokens", ctypes.c_void_p), ("n_pages", ctypes.c_int32),
+                ("pad", ctypes.c_int32)]
+
+
 class SampleBatch(ctypes.Structure):
     _fields_ = [("dtype", ctypes.c_int32), ("n_rows", ctypes.c_int32), ("vocab", ctypes.c_int32),
                 ("pad", ctypes.c_int32), ("logits", ctypes.c_void_p), ("row_stride", ctypes.c_int64),
@@ -174,6 +188,12 @@ def lib():
         "moe_kv_append": ([P(KvBatch), P(KvRope), i32, vp, i64, vp, i64, vp, i64, vp, i64], ctypes.c_int),
         "moe_kv_attend": ([P(KvBatch), i32, ctypes.c_float, vp, i64, vp, i64, vp, u64], ctypes.c_int),
         "moe_kv_attend_workspace": ([P(KvBatch), P(u64)], ctypes.c_int),
+        "moe_kv_append_ext": ([P(KvBatch), P(KvScales), P(KvRope), P(KvNorm), i32, vp, i64, vp, i64, vp, i64, vp, i64],
+                              ctypes.c_int),
+        "moe_kv_read": ([P(KvBatch), P(KvScales), vp, i64, vp, i64], ctypes.c_int),
+        "moe_kv_attend_ext": ([P(KvBatch), P(KvScales), P(KvPrefix), i32, ctypes.c_float, vp, i64, vp, i64, vp, u64],
+                              ctypes.c_int),
+        "moe_kv_attend_ext_workspace": ([P(KvBatch), P(KvScales), P(KvPrefix), P(u64)], ctypes.c_int),
         "moe_sample": ([P(SampleBatch), vp, vp, vp, u64], ctypes.c_int),
         "moe_sample_workspace": ([P(SampleBatch), P(u64)], ctypes.c_int),
         "moe_pack_gguf": ([ctypes.c_char_p] * 4 + [P(PackInfo)], ctypes.c_int),

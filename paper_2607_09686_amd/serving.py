@@ -1,5 +1,6 @@
 """What a decoder runs beside the MoE layer calls: a paged key/value cache with the attention that
-reads it (moe_kv_append, moe_kv_attend) and the choice of the next tokens (moe_sample).
+reads it (moe_kv_append, moe_kv_attend, their _ext forms and moe_kv_read) and the choice of the
+next tokens (moe_sample).
 
 Argument marshalling only.  Every call queues its kernels on torch's current stream of the
 tensors' device and returns without waiting.  Buffers that a call returns and its workspace come
@@ -8,7 +9,8 @@ share them.  Kernels never touch memory outside the tensors given, whatever the 
 """
 import ctypes
 
-from .moecache import KvBatch, KvRope, MOE_BF16, MOE_F16, MOE_F32, SampleBatch, _check, lib
+from .moecache import (KvBatch, KvNorm, KvPrefix, KvRope, KvScales, MOE_BF16, MOE_F16, MOE_F32, SampleBatch, _check,
+                       lib)
 
 # torch and its dtypes' codes: bound on first use, so that importing the package does not import torch
 _torch = None
@@ -92,11 +94,17 @@ class KvCache:
     rope_dim elements of each head turn by position * rope_theta ** (-2 i / rope_dim), or by
     rope_freqs[i], as pairs (i, i + rope_dim / 2), or (2 i, 2 i + 1) with rope_adjacent; 0: none.
     scale defaults to head_dim ** -0.5; window > 0 limits a token to that many last tokens.
+
+    storage=torch.float8_e4m3fn holds keys and values in 8 bits (moe_kv_scales): `keys`
+    [n_layers, n_pages, n_kv_heads, page_tokens / 16, head_dim / 16, 16, 16] and `values` of that
+    type, and a power of two for each token and KV head in `key_scales` and `value_scales`
+    [n_layers, n_pages, n_kv_heads, page_tokens], of torch.float8_e8m0fnu.  dtype is then that of
+    queries, results and what the numbers stand for.
     """
 
     def __init__(self, n_layers, n_heads, n_kv_heads, head_dim, page_tokens, n_pages, dtype=None,
                  rope_theta=10000.0, rope_dim=None, rope_adjacent=False, rope_freqs=None, scale=None,
-                 window=0, device="cuda", keys=None, values=None):
+                 window=0, device="cuda", keys=None, values=None, storage=None, key_scales=None, value_scales=None):
         torch = _bind()
         dtype = torch.bfloat16 if dtype is None else dtype
         if dtype not in (torch.bfloat16, torch.float16):
@@ -111,18 +119,30 @@ class KvCache:
         self.n_layers, self.n_heads, self.n_kv_heads = n_layers, n_heads, n_kv_heads
         self.head_dim, self.page_tokens, self.n_pages = head_dim, page_tokens, n_pages
         self.dtype, self.window = dtype, int(window)
+        if storage not in (None, dtype, torch.float8_e4m3fn):
+            raise TypeError(f"storage must be dtype or torch.float8_e4m3fn, got {storage}")
+        held = storage == torch.float8_e4m3fn
+        self.storage = storage = torch.float8_e4m3fn if held else dtype
+        if not held and (key_scales is not None or value_scales is not None):
+            raise ValueError("key_scales and value_scales belong to a cache of 8 bits")
         self.scale = head_dim ** -0.5 if scale is None else float(scale)
         front = (n_layers, n_pages, n_kv_heads, page_tokens // 16)
-        shapes = front + (head_dim // 8, 16, 8), front + (2, head_dim, 8)
-        for name, t, shape in (("keys", keys, shapes[0]), ("values", values, shapes[1])):
+        unit = 16 if held else 8
+        pools = [("keys", keys, front + (head_dim // unit, 16, unit), storage),
+                 ("values", values, front + (2, head_dim, 8), storage)]
+        if held:
+            exponents = (n_layers, n_pages, n_kv_heads, page_tokens), torch.float8_e8m0fnu
+            pools += [("key_scales", key_scales, *exponents), ("value_scales", value_scales, *exponents)]
+        self._key_scales = self._value_scales = None
+        for name, t, shape, kind in pools:
             if t is None:
-                t = torch.empty(shape, dtype=dtype, device=device)
-            elif t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
-                raise ValueError(f"{name} must be contiguous {dtype} of shape {shape}")
+                t = torch.empty(shape, dtype=kind, device=device)
+            elif t.dtype != kind or tuple(t.shape) != shape or not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous {kind} of shape {shape}")
             setattr(self, "_" + name, t)  # fixed from here on: calls hold their addresses
         self.device = self.keys.device
-        if self.values.device != self.device:
-            raise ValueError("keys and values must live on one device")
+        if any(getattr(self, "_" + p[0]).device != self.device for p in pools):
+            raise ValueError("keys, values and their scales must live on one device")
         self.rope_dim = head_dim if rope_dim is None else int(rope_dim)
         self.rope_adjacent = bool(rope_adjacent)
         if rope_freqs is None:
@@ -137,18 +157,33 @@ class KvCache:
             self._blank = [bytes(KvBatch(_codes[dtype], n_heads, n_kv_heads, head_dim, page_tokens, n_pages,
                                          0, 0, 0, 0, k.data_ptr(), v.data_ptr()))
                            for k, v in zip(self.keys, self.values)]
+            self._scales = [None] * n_layers
+            if held:
+                self._scales = [KvScales(k.data_ptr(), v.data_ptr())
+                                for k, v in zip(self._key_scales, self._value_scales)]
             self._index = self.device.index
             self._rope = KvRope(self.rope_dim, self.rope_adjacent, self.rope_freqs.data_ptr())
         self._work_bytes = {}  # a batch's counts: bytes of moe_kv_attend's workspace
 
     keys = property(lambda self: self._keys)
     values = property(lambda self: self._values)
+    key_scales = property(lambda self: self._key_scales)
+    value_scales = property(lambda self: self._value_scales)
     rope_freqs = property(lambda self: self._rope_freqs)
 
     @property
     def token_bytes(self):
         """Bytes of one token in every layer: kv_bytes_per_token of plan_percent and plan_bytes."""
-        return 4 * self.n_layers * self.n_kv_heads * self.head_dim
+        head = self.head_dim + 1 if self._key_scales is not None else 2 * self.head_dim
+        return 2 * self.n_layers * self.n_kv_heads * head
+
+    def _norm(self, weight, what):
+        kind = getattr(weight, "dtype", None)
+        _gpu(weight, what, kind if kind == _torch.float32 else self.dtype, self.device)
+        if weight.requires_grad and _torch.is_grad_enabled():
+            raise ValueError(f"{what} requires a gradient, which the cache's calls do not give: detach it, or call "
+                             "under torch.no_grad()")
+        return _vector(weight, what, kind, self.head_dim, self.device)
 
     def _batch(self, layer, pages, starts, lengths, n_tokens, status):
         if self._blank is None:
@@ -170,10 +205,13 @@ class KvCache:
         b.hip_stream = _stream(self._index)
         return b
 
-    def append(self, k, v, pages, starts, lengths, layer=0, q=None, q_out=None, status=None):
+    def append(self, k, v, pages, starts, lengths, layer=0, q=None, q_out=None, status=None, q_norm=None,
+               k_norm=None, norm_eps=1e-6):
         """Turn k by its positions and write k and v, [tokens, n_kv_heads, head_dim] in the cache's
         dtype or float32, into their pages; with q [tokens, n_heads, head_dim] of the same dtype, also
-        turn q and return it in the cache's dtype (in q_out if given, which may be q)."""
+        turn q and return it in the cache's dtype (in q_out if given, which may be q).  q_norm and
+        k_norm [head_dim], of dtype or float32 (both alike): before its turn each head becomes
+        x / sqrt(mean(x ** 2) + norm_eps) * weight."""
         n, kind, device, heads, dim = k.shape[0], k.dtype, self.device, self.n_heads, self.head_dim
         if kind != self.dtype and kind != _torch.float32:
             raise TypeError(f"k must be {self.dtype} or torch.float32, got {kind}")
@@ -188,28 +226,72 @@ class KvCache:
         elif q_out is not None:
             raise ValueError("q_out without q")
         b = self._batch(layer, pages, starts, lengths, n, status)
-        _run(self._index, lib().moe_kv_append, b, self._rope, _codes[kind], kp, ks, vp, vs, qp, qs, op, os)
+        if q_norm is None and k_norm is None and self._key_scales is None:
+            _run(self._index, lib().moe_kv_append, b, self._rope, _codes[kind], kp, ks, vp, vs, qp, qs, op, os)
+            return q_out
+        norm = None
+        if q_norm is not None or k_norm is not None:
+            if q_norm is not None and q is None:
+                raise ValueError("q_norm without q")
+            one = k_norm if q_norm is None else q_norm
+            norm = KvNorm(self._norm(q_norm, "q_norm") if q_norm is not None else None,
+                          self._norm(k_norm, "k_norm") if k_norm is not None else None, _codes[one.dtype], norm_eps)
+            if q_norm is not None and k_norm is not None and q_norm.dtype != k_norm.dtype:
+                raise TypeError(f"q_norm and k_norm must be alike, got {q_norm.dtype} and {k_norm.dtype}")
+        _run(self._index, lib().moe_kv_append_ext, b, self._scales[layer], self._rope, norm, _codes[kind], kp, ks, vp, vs,
+             qp, qs, op, os)
         return q_out
 
-    def attend(self, q, pages, starts, lengths, layer=0, out=None, status=None):
+    def read(self, n_tokens, pages, starts, lengths, layer=0, k=None, v=None, status=None):
+        """The last starts[s + 1] - starts[s] tokens of each sequence as the cache holds them: (k, v),
+        [n_tokens, n_kv_heads, head_dim] in dtype, allocated unless given (rows from starts[n_seqs] on
+        are left alone).  To have a sequence whole, let starts count all of its tokens."""
+        rows, device = (n_tokens, self.n_kv_heads, self.head_dim), self.device
+        b = self._batch(layer, pages, starts, lengths, n_tokens, status)
+        k = _torch.empty(rows, dtype=self.dtype, device=device) if k is None else k
+        v = _torch.empty(rows, dtype=self.dtype, device=device) if v is None else v
+        kp, ks = _rows(k, "k", self.dtype, *rows[1:], n_tokens, device)
+        vp, vs = _rows(v, "v", self.dtype, *rows[1:], n_tokens, device)
+        _run(self._index, lib().moe_kv_read, b, self._scales[layer], kp, ks, vp, vs)
+        return k, v
+
+    def attend(self, q, pages, starts, lengths, layer=0, out=None, status=None, prefix=None, shared=None):
         """Attention of the new tokens' queries q [tokens, n_heads, head_dim] (turned, in the cache's
-        dtype) over their sequences, whose new tokens have been appended.  Returns out, like q."""
+        dtype) over their sequences, whose new tokens have been appended.  Returns out, like q.
+
+        Where all sequences begin with the same tokens, prefix (int32 [n], the pages that hold them)
+        and shared (int32 [1], their number, none of them new) let these be read once for all: the
+        same result but for rounding (moe_kv_prefix).  Not with a window."""
         n, device, heads, dim = q.shape[0], self.device, self.n_heads, self.head_dim
         qp, qs = _rows(q, "q", self.dtype, heads, dim, n, device)
         if out is None:
             out = _torch.empty((n, heads, dim), dtype=self.dtype, device=device)
         op, os = _rows(out, "out", self.dtype, heads, dim, n, device)
         b = self._batch(layer, pages, starts, lengths, n, status)
-        counts = n, b.n_seqs, b.max_pages  # what the workspace's size goes by
+        front = None
+        if prefix is not None or shared is not None:
+            if prefix is None or shared is None:
+                raise ValueError("prefix and shared go together")
+            _gpu(prefix, "prefix", _torch.int32, device)
+            if prefix.dim() != 1:
+                raise ValueError("prefix must be a vector of page ids")
+            front = KvPrefix(_vector(prefix, "prefix", _torch.int32, prefix.shape[0], device),
+                             _vector(shared, "shared", _torch.int32, 1, device), prefix.shape[0])
+        scales = self._scales[layer]
+        counts = n, b.n_seqs, b.max_pages, front and front.n_pages  # what the workspace's size goes by
         size = self._work_bytes.get(counts)
         if size is None:
             need = ctypes.c_uint64()
-            _check(lib().moe_kv_attend_workspace(b, need))
+            _check(lib().moe_kv_attend_ext_workspace(b, scales, front, need))
             if len(self._work_bytes) > 4096:
                 self._work_bytes.clear()
             size = self._work_bytes[counts] = need.value
         work = _torch.empty(size, dtype=_torch.uint8, device=device)
-        _run(self._index, lib().moe_kv_attend, b, self.window, self.scale, qp, qs, op, os, work.data_ptr(), size)
+        if front is None and scales is None:
+            _run(self._index, lib().moe_kv_attend, b, self.window, self.scale, qp, qs, op, os, work.data_ptr(), size)
+        else:
+            _run(self._index, lib().moe_kv_attend_ext, b, scales, front, self.window, self.scale, qp, qs, op, os,
+                 work.data_ptr(), size)
         return out
 
 
