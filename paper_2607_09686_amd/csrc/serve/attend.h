@@ -542,10 +542,10 @@ __device__ __forceinline__ Prefix prefix_of(const AttendArgs &a) {
   return p;
 }
 template <int M>
-__device__ __forceinline__ bool prefix_unit(const AttendArgs &a, Unit *u) {
+__device__ __forceinline__ bool prefix_unit(const AttendArgs &a, int block, Unit *u) {
   const Prefix p = prefix_of(a);
-  const int unit = blockIdx.x / a.kv.kv_heads, split = unit % a.prefix_splits;
-  u->kvh = blockIdx.x % a.kv.kv_heads;
+  const int unit = block / a.kv.kv_heads, split = unit % a.prefix_splits;
+  u->kvh = block % a.kv.kv_heads;
   u->tile = unit / a.prefix_splits;
   u->seq = 0;
   u->q = Seq{p.first, p.rows / a.kv.group, p.keys, false};
@@ -556,15 +556,15 @@ __device__ __forceinline__ bool prefix_unit(const AttendArgs &a, Unit *u) {
 }
 
 template <int M, Cover V>
-__device__ __forceinline__ bool unit_of(const AttendArgs &a, Unit *u) {
-  if constexpr (V == kPrefix) return prefix_unit<M>(a, u);
+__device__ __forceinline__ bool unit_of(const AttendArgs &a, int block, Unit *u) {
+  if constexpr (V == kPrefix) return prefix_unit<M>(a, block, u);
   Place pl;
   int C;
-  u->kvh = blockIdx.x % a.kv.kv_heads;
-  const int unit = blockIdx.x / a.kv.kv_heads;
+  u->kvh = block % a.kv.kv_heads;
+  const int unit = block / a.kv.kv_heads;
   const bool found = a.kv.n_seqs > kPlanSeqs
                          ? plan_search<M, V>(a, unit, &C, &pl)
-                         : plan_here<M, V>(a, unit, blockIdx.x == 0 && threadIdx.x < kLanes, &C, &pl);
+                         : plan_here<M, V>(a, unit, block == 0 && threadIdx.x < kLanes, &C, &pl);
   if (!found) return false;
   const int per = units_of(a, span_of<M, V>(a, pl.q), C);
   if (pl.index >= (int64_t)tiles_of<M>(a, pl.q) * per) return false;  // starts out of order
@@ -643,16 +643,24 @@ struct Step {
   uint2 vs[2];
 };
 
+template <int D>
+struct FewLds {
+  float sums[kWaves][D / 32 * 4][kLanes][4];
+  float stat[kWaves][32][2];
+  int ids[kIds];
+  int bad;
+};
 template <class E, int D, int R, bool Held, Cover V>
-__device__ __forceinline__ void few_body(const AttendArgs &a) {
+__device__ __forceinline__ void few_body(const AttendArgs &a, FewLds<D> &lds, int block) {
   constexpr int M = 32 * R, kTurns = kWaves / R;  // waves that take turns at the steps of the same rows
+  constexpr int kAhead = Held && D <= 128 ? 2 : 1;
   typedef typename std::conditional<Held, uint8_t, uint16_t>::type S;
-  __shared__ __align__(16) float sums[kWaves][D / 32 * 4][kLanes][4];
-  __shared__ float stat[kWaves][32][2];
-  __shared__ int ids[kIds];
-  __shared__ int bad;
+  auto &sums = lds.sums;
+  auto &stat = lds.stat;
+  auto &ids = lds.ids;
+  int &bad = lds.bad;
   Unit u;
-  if (!unit_of<M, V>(a, &u)) return;
+  if (!unit_of<M, V>(a, block, &u)) return;
   if (u.q.bad) {
     refuse<E, D, M>(a, u);
     return;
@@ -668,8 +676,8 @@ __device__ __forceinline__ void few_body(const AttendArgs &a) {
   const int first = before + u.tile * M / kv.group, last = before + (min(u.tile * M + M, rows) - 1) / kv.group;
   u32x4 q[D / 16];
   load_q<D, Held>(a, u.q, u.kvh, row, q);
-  // heads of 256: the queries stay in LDS, where the joining of the waves has its place later
-  constexpr bool kQInLds = D > 128;
+  // heads of 256, or two steps' requests: the queries stay in LDS, where the joining of the waves has its place later
+  constexpr bool kQInLds = D > 128 || (D == 128 && kAhead == 2);
   u32x4 *q_lds = (u32x4 *)&sums[0][0][0][0] + part * (D / 16) * kLanes;
   if (kQInLds && turn == 0)
 #pragma unroll
@@ -695,8 +703,8 @@ __device__ __forceinline__ void few_body(const AttendArgs &a) {
     const int begin = max(u.k0, pg0 << shift);
     const int end = (int)min((int64_t)u.k1, ((int64_t)pg0 + kIds) << shift);
     const int id_last = min(pg_last, pg0 + kIds - 1) - pg0;
-    Step<D, Held> x;
-    auto load_k = [&](int t0) {
+    typedef Step<D, Held> Loads;
+    auto load_k = [&](Loads &x, int t0) {
       const int t = t0 + key;
       const int id = ids[min((t >> shift) - pg0, id_last)];
       if constexpr (Held) {
@@ -710,7 +718,7 @@ __device__ __forceinline__ void few_body(const AttendArgs &a) {
         for (int c = 0; c < D / 16; ++c) x.k[c] = *(const u32x4 *)(src + 2 * c * 16 * 8);
       }
     };
-    auto load_v = [&](int t0) {
+    auto load_v = [&](Loads &x, int t0) {
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const int t = t0 + 16 * c;
@@ -727,10 +735,9 @@ __device__ __forceinline__ void few_body(const AttendArgs &a) {
         }
       }
     };
-    int t0 = begin + 32 * turn;
-    if (t0 < end) load_k(t0), load_v(t0);
-    for (; t0 < end; t0 += 32 * kTurns) {
-      const int next = t0 + 32 * kTurns;
+    // requests for the wave's next kAhead steps are under way
+    auto step = [&](Loads &x, int t0) {
+      const int next = t0 + 32 * kTurns * kAhead;
       f32x16 s[1] = {};
       const float k_scale = Held ? scale_of(x.ks) : 1.f;
 #pragma unroll
@@ -738,7 +745,7 @@ __device__ __forceinline__ void few_body(const AttendArgs &a) {
         const u32x4 k = Held ? operand<E>(x.k[c / 2][c % 2 * 2], x.k[c / 2][c % 2 * 2 + 1], k_scale) : x.k[Held ? c / 2 : c];
         s[0] = mma(k, kQInLds ? q_lds[c * kLanes + lane] : q[c], s[0], E());
       }
-      if (next < end) load_k(next);
+      if (next < end) load_k(x, next);
       // whether some row does not see some key of the step
       const bool edge = V != kPrefix && (t0 + 31 > first || (window && t0 <= last - window));
       u32x4 p[2];
@@ -773,7 +780,21 @@ __device__ __forceinline__ void few_body(const AttendArgs &a) {
       }
       if (odd)
         add_odd<E, D, S, Held>(st, values, vs, kv.kv_heads, ids, pg0, shift, page_elems, t0, min(t0 + 32, end), pos, floor);
-      if (next < end) load_v(next);
+      if (next < end) load_v(x, next);
+    };
+    int t0 = begin + 32 * turn;
+    if constexpr (kAhead == 1) {
+      Loads x;
+      if (t0 < end) load_k(x, t0), load_v(x, t0);
+      for (; t0 < end; t0 += 32 * kTurns) step(x, t0);
+    } else {
+      Loads x[2];
+      if (t0 < end) load_k(x[0], t0), load_v(x[0], t0);
+      if (t0 + 32 * kTurns < end) load_k(x[1], t0 + 32 * kTurns), load_v(x[1], t0 + 32 * kTurns);
+      for (; t0 < end; t0 += 64 * kTurns) {
+        step(x[0], t0);
+        if (t0 + 32 * kTurns < end) step(x[1], t0 + 32 * kTurns);
+      }
     }
   }
 
@@ -814,7 +835,8 @@ __device__ __forceinline__ void few_body(const AttendArgs &a) {
 
 template <class E, int D, int R>
 __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_few_kernel(AttendArgs a) {
-  few_body<E, D, R, false, kAll>(a);
+  __shared__ __align__(16) FewLds<D> lds;
+  few_body<E, D, R, false, kAll>(a, lds, blockIdx.x);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -832,16 +854,22 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_few_kernel(A
 typedef __attribute__((address_space(3))) void lds_void;
 typedef const __attribute__((address_space(1))) void global_void;
 
+template <int D>
+struct ManyLds {
+  uint8_t tiles[4 * 64 * D * 2];  // [2][K tile, V tile], each four groups
+  int ids[kIds];
+  int bad;
+};
 template <class E, int D, bool Held, Cover V>
-__device__ __forceinline__ void many_body(const AttendArgs &a) {
+__device__ __forceinline__ void many_body(const AttendArgs &a, ManyLds<D> &shared, int block) {
   constexpr int M = 128, KT = 64;
   typedef typename std::conditional<Held, uint8_t, uint16_t>::type S;
   constexpr int kTileBytes = KT * D * 2;
-  __shared__ __align__(16) uint8_t lds[4 * kTileBytes];  // [2][K tile, V tile], each four groups
-  __shared__ int ids[kIds];
-  __shared__ int bad;
+  auto &lds = shared.tiles;
+  auto &ids = shared.ids;
+  int &bad = shared.bad;
   Unit u;
-  if (!unit_of<M, V>(a, &u)) return;
+  if (!unit_of<M, V>(a, block, &u)) return;
   if (u.q.bad) {
     refuse<E, D, M>(a, u);
     return;
@@ -1013,7 +1041,8 @@ __device__ __forceinline__ void many_body(const AttendArgs &a) {
 
 template <class E, int D>
 __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_many_kernel(AttendArgs a) {
-  many_body<E, D, false, kAll>(a);
+  __shared__ __align__(16) ManyLds<D> lds;
+  many_body<E, D, false, kAll>(a, lds, blockIdx.x);
 }
 
 // ---------------------------------------------------------------------------------------------

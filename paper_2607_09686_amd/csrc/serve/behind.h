@@ -23,27 +23,35 @@ namespace {
 
 template <class E, int D, int R>
 __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void held_few_kernel(AttendArgs a) {
-  few_body<E, D, R, true, kAll>(a);
+  __shared__ __align__(16) FewLds<D> lds;
+  few_body<E, D, R, true, kAll>(a, lds, blockIdx.x);
 }
 template <class E, int D>
 __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void held_many_kernel(AttendArgs a) {
-  many_body<E, D, true, kAll>(a);
+  __shared__ __align__(16) ManyLds<D> lds;
+  many_body<E, D, true, kAll>(a, lds, blockIdx.x);
 }
-template <class E, int D, int R, bool Held>
-__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void behind_few_kernel(AttendArgs a) {
-  few_body<E, D, R, Held, kBehind>(a);
-}
-template <class E, int D, bool Held>
-__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void behind_many_kernel(AttendArgs a) {
-  many_body<E, D, Held, kBehind>(a);
-}
-template <class E, int D, int R, bool Held>
-__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void prefix_few_kernel(AttendArgs a) {
-  few_body<E, D, R, Held, kPrefix>(a);
-}
-template <class E, int D, bool Held>
-__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void prefix_many_kernel(AttendArgs a) {
-  many_body<E, D, Held, kPrefix>(a);
+
+// Units over what is shared, in tiles of FM rows, and then units behind it, in tiles of M, in one launch: the first
+// are bound by the matrix cores where the batch is large, the others by the cache's bytes.
+template <class E, int D, int FM, int M, bool Held>
+__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void behind_kernel(AttendArgs a) {
+  __shared__ __align__(16) union {
+    FewLds<D> few;
+    ManyLds<D> many;
+  } lds;
+  const int front = a.prefix_tiles * a.prefix_splits * a.kv.kv_heads, block = blockIdx.x;
+  if (block < front) {
+    if constexpr (FM == 128)
+      many_body<E, D, Held, kPrefix>(a, lds.many, block);
+    else
+      few_body<E, D, FM / 32, Held, kPrefix>(a, lds.few, block);
+  } else {
+    if constexpr (M == 128)
+      many_body<E, D, Held, kBehind>(a, lds.many, block - front);
+    else
+      few_body<E, D, M / 32, Held, kBehind>(a, lds.few, block - front);
+  }
 }
 template <int M>
 __global__ __launch_bounds__(kPlanThreads) void plan_behind_kernel(AttendArgs a) {
@@ -63,16 +71,15 @@ hipError_t launch_behind(const AttendArgs &a, int rows, hipStream_t s) {
                         : rows == 64 ? (const void *)plan_behind_kernel<64>
                                      : (const void *)plan_behind_kernel<128>,
                         dim3(1), dim3(kPlanThreads), args, 0, s);
-  if (e == hipSuccess)
-    e = hipLaunchKernel(a.prefix_rows == 32   ? (const void *)prefix_few_kernel<E, D, 1, Held>
-                        : a.prefix_rows == 64 ? (const void *)prefix_few_kernel<E, D, 2, Held>
-                                              : (const void *)prefix_many_kernel<E, D, Held>,
-                        dim3((unsigned)((int64_t)a.prefix_tiles * a.prefix_splits * a.kv.kv_heads)), dim3(kThreads), args, 0, s);
-  if (e == hipSuccess)
-    e = hipLaunchKernel(rows == 32   ? (const void *)behind_few_kernel<E, D, 1, Held>
-                        : rows == 64 ? (const void *)behind_few_kernel<E, D, 2, Held>
-                                     : (const void *)behind_many_kernel<E, D, Held>,
-                        dim3((unsigned)((int64_t)a.max_units * a.kv.kv_heads)), dim3(kThreads), args, 0, s);
+  // all rows together are at least as many as the mean sequence's
+  const void *fn = rows == 128              ? (const void *)behind_kernel<E, D, 128, 128, Held>
+                   : a.prefix_rows == 128   ? rows == 64 ? (const void *)behind_kernel<E, D, 128, 64, Held>
+                                                         : (const void *)behind_kernel<E, D, 128, 32, Held>
+                   : a.prefix_rows == 64    ? rows == 64 ? (const void *)behind_kernel<E, D, 64, 64, Held>
+                                                         : (const void *)behind_kernel<E, D, 64, 32, Held>
+                                            : (const void *)behind_kernel<E, D, 32, 32, Held>;
+  const int64_t units = (int64_t)a.prefix_tiles * a.prefix_splits + a.max_units;
+  if (e == hipSuccess) e = hipLaunchKernel(fn, dim3((unsigned)(units * a.kv.kv_heads)), dim3(kThreads), args, 0, s);
   if (e != hipSuccess) return e;
   return hipLaunchKernel(rows == 32   ? (const void *)join_behind_kernel<E, D, 32>
                          : rows == 64 ? (const void *)join_behind_kernel<E, D, 64>

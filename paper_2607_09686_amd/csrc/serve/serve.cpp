@@ -118,12 +118,13 @@ int tile_rows(const KvView &kv) {
 
 // The launch over what all sequences begin with: tiles of all rows together, each cut into as many units
 // as the card has places for it, of kManyMinKeys keys and more where its pages are full.
-void plan_prefix(AttendArgs *a, int dim) {
+void plan_prefix(AttendArgs *a, int64_t tiles, int dim) {
   const KvView &kv = a->kv;
   const int64_t rows = (int64_t)kv.n_tokens * kv.group, keys = (int64_t)a->prefix_pages << kv.page_shift;
   a->prefix_rows = rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
   a->prefix_tiles = (int)((rows + a->prefix_rows - 1) / a->prefix_rows);
-  const int resident = a->prefix_rows < 128 && dim > 128 ? kResident / 2 : kResident;
+  int resident = a->prefix_rows < 128 && dim > 128 ? kResident / 2 : kResident;
+  resident -= (int)std::min<int64_t>(resident / 2, tiles * kv.kv_heads);  // places for what comes behind
   const int min_keys = a->prefix_rows < 128 ? kFewMinKeys : kManyMinKeys;
   const int64_t most = std::max<int64_t>(1, keys / min_keys);
   a->prefix_splits = (int)std::min(most, std::max<int64_t>(1, resident / ((int64_t)a->prefix_tiles * kv.kv_heads)));
@@ -152,7 +153,7 @@ int plan(AttendArgs *a, uint64_t *bytes, int dim) {
   if (a->shared) {  // every tile's units leave partial results, and a note
     a->max_slots = a->max_units;
     a->max_tiles = (int)tiles;
-    plan_prefix(a, dim);
+    plan_prefix(a, tiles, dim);
   }
   *bytes = attend_work_bytes(*a, rows, dim);
   if (a->shared) *bytes += front_bytes(*a, dim);

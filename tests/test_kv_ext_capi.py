@@ -166,9 +166,9 @@ def test_numbers_of_8_bits():
 
 def test_the_kernels_use_no_scratch(mc):
     found = {n: k for n, k in kernels(mc.LIB_PATH).items()
-             if any(s in n for s in ("held_", "behind_", "prefix_", "append_ext_kernel", "read_kernel"))}
-    # 8 bits: three tiles; behind shared tokens and over them: of both storages; planned and joined: three tiles;
+             if any(s in n for s in ("held_", "behind_", "append_ext_kernel", "read_kernel"))}
+    # 8 bits: three tiles; behind shared tokens: six pairs of tiles, two storages; planned and joined: three tiles;
     # appended: two sources and storages, read: two storages; two types, three head sizes (plans: of all sizes and types)
-    assert len(found) == 3 * 2 * (3 + 6 + 6 + 3) + 3 + 2 * 4 + 2 * 2
+    assert len(found) == 3 * 2 * (3 + 12 + 3) + 3 + 2 * 4 + 2 * 2
     for name, k in found.items():
         assert (k[".vgpr_spill_count"], k[".private_segment_fixed_size"]) == (0, 0), name
