@@ -1051,8 +1051,8 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_many_kernel(
 // lanes share out a row's units, or several rows' where there are fewer units than groups.  Bound by the
 // latency of three dependent reads: 6 us for 512 units of one token, 3.5 with nothing to join.
 // ---------------------------------------------------------------------------------------------
-template <class E, int D, int M, Cover V>
-__device__ __forceinline__ void join_body(const AttendArgs &a) {
+template <class E, int D, int M>
+__global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
   constexpr int kPer = D / 4, kGroups = kThreads / kPer;
   __shared__ __align__(16) float sum[kGroups][D];
   __shared__ float stat[kGroups][2];
@@ -1060,22 +1060,13 @@ __device__ __forceinline__ void join_body(const AttendArgs &a) {
   const SplitTile t = split_tiles(a)->tile[item];
   if (item >= split_tiles(a)->count) return;
   // starts out of order can leave a note unwritten: nothing is taken from one that makes no sense
-  if (t.units < (V == kBehind ? 1 : 2) || t.slot < 0 || t.slot > a.max_slots - t.units || t.rows < 1 || t.rows > M || t.first < 0 ||
+  if (t.units < 2 || t.slot < 0 || t.slot > a.max_slots - t.units || t.rows < 1 || t.rows > M || t.first < 0 ||
       t.row0 < 0 || t.row0 > (1 << 28) || t.first > a.kv.n_tokens - 1 - (t.row0 + t.rows - 1) / a.kv.group)
     return;
-  // what the prefix's launch left of these rows: its units come first
-  Prefix pre{};
-  int pre_units = 0;
-  if constexpr (V == kBehind) {
-    pre = prefix_of(a);
-    const int64_t from = (int64_t)(t.first - pre.first) * a.kv.group + t.row0;
-    if (from >= 0 && from + t.rows <= pre.rows) pre_units = pre.units;
-  }
-  const int units = pre_units + t.units;
   const int g = threadIdx.x / kPer, d = threadIdx.x % kPer * 4;
   // groups to a row: a power of two, so that a tile of few units has several rows joined at once
   int per = 1;
-  while (per < kGroups && per < units) per *= 2;
+  while (per < kGroups && per < t.units) per *= 2;
   const int own = g / per, at_once = kGroups / per;
   const int64_t step = (int64_t)a.kv.kv_heads * M;  // rows from unit to unit
   for (int r0 = 0; (int)(blockIdx.y + gridDim.y * r0) < t.rows; r0 += at_once) {
@@ -1084,18 +1075,10 @@ __device__ __forceinline__ void join_body(const AttendArgs &a) {
     f32x4 o{};
     if (row < t.rows) {
       const float *ml = part_ml<D, M>(a, t.slot, kvh, row), *part = part_o<D, M>(a, t.slot, kvh, row) + d;
-      const int at = V == kBehind ? (t.first - pre.first) * a.kv.group + t.row0 + row : 0;
-      const int64_t front = V == kBehind ? front_row(a, at / a.prefix_rows * a.prefix_splits, kvh, at % a.prefix_rows) : 0;
 #pragma unroll 4
-      for (int i = g % per; i < units; i += per) {
-        const float *mli = ml + (i - pre_units) * step * 2, *parti = part + (i - pre_units) * step * D;
-        if (V == kBehind && i < pre_units) {
-          const int64_t from = front + (int64_t)i * a.kv.kv_heads * a.prefix_rows;
-          mli = front_ml<D>(a, from);
-          parti = front_o<D>(a, from) + d;
-        }
-        const float mi = mli[0], li = mli[1];
-        const f32x4 oi = *(const f32x4 *)parti;
+      for (int i = g % per; i < t.units; i += per) {
+        const float mi = ml[i * step * 2], li = ml[i * step * 2 + 1];
+        const f32x4 oi = *(const f32x4 *)(part + i * step * D);
         const float top = fmaxf(m, mi), base = top == kNegInf ? 0.f : top;
         const float w = __builtin_amdgcn_exp2f(mi - base), shrink = __builtin_amdgcn_exp2f(m - base);
         l = l * shrink + w * li;
@@ -1121,11 +1104,6 @@ __device__ __forceinline__ void join_body(const AttendArgs &a) {
     }
     __syncthreads();
   }
-}
-
-template <class E, int D, int M>
-__global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
-  join_body<E, D, M, kAll>(a);
 }
 
 }  // namespace

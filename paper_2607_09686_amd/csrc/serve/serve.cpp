@@ -116,18 +116,22 @@ int tile_rows(const KvView &kv) {
   return rows <= (int64_t)32 * kv.n_seqs ? 32 : rows <= (int64_t)64 * kv.n_seqs ? 64 : 128;
 }
 
-// The launch over what all sequences begin with: tiles of all rows together, each cut into as many units
-// as the card has places for it, of kManyMinKeys keys and more where its pages are full.
-void plan_prefix(AttendArgs *a, int64_t tiles, int dim) {
+// The launch over what all sequences begin with: tiles of all rows together, each cut into units alike.  A unit's
+// time goes with its keys, and each unit more leaves a tile's partial results to write and to read; with x tiles (of all
+// KV heads) of S keys the two balance at sqrt(S x) units, up to a factor that measured as 1/2, rounded down to a power of
+// two per tile.  us with half as many units, as many, and twice: 64 sequences behind 8192 (16 tiles, 8 units each) 61, 43,
+// 46; 8 behind 65536 in 8 bits (4, 64) 40, 30, 39; 16 behind 4096 (4, 16) 21, 17, 17; 32 behind 32768 (8, 32) 54, 37, 43;
+// 8 chunks of 50 to 200 behind 8192 (256, 2) 186, 148, 146.  S is what the prefix's pages hold, its count is on the device.
+constexpr int kPrefixMinKeys = 128;
+void plan_prefix(AttendArgs *a) {
   const KvView &kv = a->kv;
   const int64_t rows = (int64_t)kv.n_tokens * kv.group, keys = (int64_t)a->prefix_pages << kv.page_shift;
   a->prefix_rows = rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
   a->prefix_tiles = (int)((rows + a->prefix_rows - 1) / a->prefix_rows);
-  int resident = a->prefix_rows < 128 && dim > 128 ? kResident / 2 : kResident;
-  resident -= (int)std::min<int64_t>(resident / 2, tiles * kv.kv_heads);  // places for what comes behind
-  const int min_keys = a->prefix_rows < 128 ? kFewMinKeys : kManyMinKeys;
-  const int64_t most = std::max<int64_t>(1, keys / min_keys);
-  a->prefix_splits = (int)std::min(most, std::max<int64_t>(1, resident / ((int64_t)a->prefix_tiles * kv.kv_heads)));
+  const int64_t tiles = (int64_t)a->prefix_tiles * kv.kv_heads;
+  int64_t n = 1;
+  while (4 * (2 * n) * (2 * n) * tiles <= keys && keys / (2 * n) >= kPrefixMinKeys) n *= 2;
+  a->prefix_splits = (int)n;
 }
 
 int plan(AttendArgs *a, uint64_t *bytes, int dim) {
@@ -153,7 +157,7 @@ int plan(AttendArgs *a, uint64_t *bytes, int dim) {
   if (a->shared) {  // every tile's units leave partial results, and a note
     a->max_slots = a->max_units;
     a->max_tiles = (int)tiles;
-    plan_prefix(a, tiles, dim);
+    plan_prefix(a);
   }
   *bytes = attend_work_bytes(*a, rows, dim);
   if (a->shared) *bytes += front_bytes(*a, dim);
