@@ -58,8 +58,9 @@ struct Run {
   int page;
   bool bad, write;  // a sequence that cannot be served; whether the page is one
 };
-__device__ __forceinline__ bool run_of(const KvView &kv, Run *r) {
-  const int lane = threadIdx.x % 64, run = blockIdx.x;
+// `teller`: the thread that reports what is wrong with the run
+__device__ __forceinline__ bool run_of(const KvView &kv, int run, bool teller, Run *r) {
+  const int lane = threadIdx.x % 64;
   // the last sequence whose first run is at or before this one, 64 probes at a time
   int lo = 0, hi = kv.n_seqs;
   while (hi - lo > 1) {
@@ -84,13 +85,13 @@ __device__ __forceinline__ bool run_of(const KvView &kv, Run *r) {
   if (j0 >= j1) return false;
   *r = Run{first + j0, before + j0, j1 - j0, 0, bad, !bad};
   if (bad) {
-    if (threadIdx.x == 0 && blockIdx.y == 0 && kv.status) atomicOr(kv.status, kKvBadLength);
+    if (teller && kv.status) atomicOr(kv.status, kKvBadLength);
   } else {
     r->page = kv.pages[(int64_t)seq * kv.max_pages + (int)(p0 >> kv.page_shift)];
     if ((unsigned)r->page >= (unsigned)kv.n_pages) {
       r->write = false;
       r->page = 0;
-      if (threadIdx.x == 0 && blockIdx.y == 0 && kv.status) atomicOr(kv.status, kKvBadPage);
+      if (teller && kv.status) atomicOr(kv.status, kKvBadPage);
     }
   }
   return true;
@@ -122,31 +123,27 @@ __device__ __forceinline__ Part part_of(const AppendArgs &a, int part) {
   const bool turned = part * 16 < R, halves = turned && !a.adjacent;
   return Part{turned, halves, halves ? part * 8 : part * 16, halves ? R / 2 + part * 8 : part * 16 + 8};
 }
-__device__ __forceinline__ void turn(const Part &p, const float *cs, const float *sn, int part, bool bad,
-                                     const float (&x)[8], const float (&y)[8], float (&ox)[8], float (&oy)[8]) {
+// Turns them in place by a part's eight sines and cosines.
+__device__ __forceinline__ void turn(const Part &p, const float *c, const float *s, bool bad, float (&x)[8], float (&y)[8]) {
   if (p.halves) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float c = cs[part * 8 + j], s = sn[part * 8 + j];
-      ox[j] = x[j] * c - y[j] * s;
-      oy[j] = y[j] * c + x[j] * s;
+      const float a = x[j], b = y[j];
+      x[j] = a * c[j] - b * s[j];
+      y[j] = b * c[j] + a * s[j];
     }
   } else if (p.turned) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float c = cs[part * 8 + j], s = sn[part * 8 + j];
-      const float c2 = cs[part * 8 + 4 + j], s2 = sn[part * 8 + 4 + j];
-      ox[2 * j] = x[2 * j] * c - x[2 * j + 1] * s;
-      ox[2 * j + 1] = x[2 * j + 1] * c + x[2 * j] * s;
-      oy[2 * j] = y[2 * j] * c2 - y[2 * j + 1] * s2;
-      oy[2 * j + 1] = y[2 * j + 1] * c2 + y[2 * j] * s2;
+      const float a = x[2 * j], b = x[2 * j + 1], d = y[2 * j], e = y[2 * j + 1];
+      x[2 * j] = a * c[j] - b * s[j];
+      x[2 * j + 1] = b * c[j] + a * s[j];
+      y[2 * j] = d * c[4 + j] - e * s[4 + j];
+      y[2 * j + 1] = e * c[4 + j] + d * s[4 + j];
     }
-  } else {
+  } else if (bad) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      ox[j] = bad ? __builtin_nanf("") : x[j];
-      oy[j] = bad ? __builtin_nanf("") : y[j];
-    }
+    for (int j = 0; j < 8; ++j) x[j] = y[j] = __builtin_nanf("");
   }
 }
 

@@ -23,7 +23,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
   const KvView &kv = a.kv;
   __shared__ Turns cs, sn;
   Run r;
-  if (!run_of(kv, &r)) return;
+  if (!run_of(kv, blockIdx.x, threadIdx.x == 0 && blockIdx.y == 0, &r)) return;
   turns_of(a, r, cs, sn);
 
   const int n = r.n, D = a.dim;
@@ -42,19 +42,19 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
     const Part p = part_of(a, part);
     const void *src = is_q ? a.q : a.k;
     const int64_t at = row * (is_q ? a.q_stride : a.k_stride) + (int64_t)head * D;
-    float x[8], y[8], ox[8], oy[8];
+    float x[8], y[8];
     In<I>::load(src, at + p.ea, x);
     In<I>::load(src, at + p.eb, y);
-    turn(p, cs[t], sn[t], part, r.bad, x, y, ox, oy);
+    turn(p, cs[t] + part * 8, sn[t] + part * 8, r.bad, x, y);
     if (is_q) {
       uint16_t *dst = (uint16_t *)a.q_out + row * a.q_out_stride + (int64_t)head * D;
-      *(u32x4 *)(dst + p.ea) = pack<E>(ox);
-      *(u32x4 *)(dst + p.eb) = pack<E>(oy);
+      *(u32x4 *)(dst + p.ea) = pack<E>(x);
+      *(u32x4 *)(dst + p.eb) = pack<E>(y);
     } else if (r.write) {
       const int tp = in_page + t;  // keys: [P/16][D/8][16][8]
       uint16_t *dst = kv.keys + ((int64_t)r.page * kv.kv_heads + head) * head_elems + (tp & ~15) * D + (tp & 15) * 8;
-      *(u32x4 *)(dst + p.ea / 8 * 128) = pack<E>(ox);
-      *(u32x4 *)(dst + p.eb / 8 * 128) = pack<E>(oy);
+      *(u32x4 *)(dst + p.ea / 8 * 128) = pack<E>(x);
+      *(u32x4 *)(dst + p.eb / 8 * 128) = pack<E>(y);
     }
   }
   if (r.write) append_values<E, I>(a, r, in_page);

@@ -327,7 +327,8 @@ __device__ __forceinline__ void softmax_step(f32x16 (&s)[N], Rows<D> &st, u32x4 
   for (int n = 0; n < N; ++n)
 #pragma unroll
     for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[n][r]);
-  mx = fmaxf(mx, __shfl_xor(mx, 32));
+  const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+  mx = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
   mx = mx * scale - kBelow<E>;  // where the base would be now
   if (__any(mx > st.m + kSlack<E>)) {
     const float top = fmaxf(st.m, mx), shrink = __builtin_amdgcn_exp2f(st.m - (top == kNegInf ? 0.f : top));

@@ -61,6 +61,14 @@ __global__ __launch_bounds__(kPlanThreads) void plan_behind_kernel(AttendArgs a)
 // group of D / 4 lanes reads kAtOnce of a row's partial results at once.  Bound by where they lie (the writers' caches are
 // other ones): 64 sequences behind 8192 tokens, calls of 45.6 us; 46.5 with four at once, 50 to 52 with 512 threads.
 constexpr int kJoinThreads = 256, kAtOnce = 2;
+// Blocks that join, up to rows / 4 and at least 4 of them to a tile: about 2048 in all, what the card holds at once (the
+// 64 sequences' 320 tiles with 8 each 43.2 us, with 4 42.0; the 36 of 8 sequences 29.5 and 32.8).
+static inline dim3 join_behind_grid(const AttendArgs &a, int rows) {
+  const int tiles = a.max_tiles * a.kv.kv_heads;
+  int y = 4;
+  while (2 * y <= rows / 4 && 2 * y * tiles <= 2048) y *= 2;
+  return dim3(tiles, y);
+}
 template <class E, int D, int M>
 __global__ __launch_bounds__(kJoinThreads) void join_behind_kernel(AttendArgs a) {
   constexpr int kPer = D / 4, kGroups = kJoinThreads / kPer;
@@ -79,7 +87,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_behind_kernel(AttendArgs a)
   const int front = row0 >= 0 && row0 + t.rows <= pre.rows ? pre.units : 0, units = front + t.units;
   const int g = threadIdx.x / kPer, d = threadIdx.x % kPer * 4;
   int per = 1;  // groups to a row
-  while (per < kGroups && per < units) per *= 2;
+  while (per < kGroups && per * kAtOnce < units) per *= 2;
   const int own = g / per, at_once = kGroups / per;
   const int64_t step = (int64_t)a.kv.kv_heads * M, front_step = (int64_t)a.kv.kv_heads * a.prefix_rows;
   for (int r0 = 0; (int)(blockIdx.y + gridDim.y * r0) < t.rows; r0 += at_once) {
@@ -159,7 +167,7 @@ hipError_t launch_behind(const AttendArgs &a, int rows, hipStream_t s) {
   return hipLaunchKernel(rows == 32   ? (const void *)join_behind_kernel<E, D, 32>
                          : rows == 64 ? (const void *)join_behind_kernel<E, D, 64>
                                       : (const void *)join_behind_kernel<E, D, 128>,
-                         join_grid(a, rows), dim3(kJoinThreads), args, 0, s);
+                         join_behind_grid(a, rows), dim3(kJoinThreads), args, 0, s);
 }
 
 template <class E, int D>

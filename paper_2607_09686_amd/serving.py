@@ -178,12 +178,13 @@ class KvCache:
         return 2 * self.n_layers * self.n_kv_heads * head
 
     def _norm(self, weight, what):
-        kind = getattr(weight, "dtype", None)
-        _gpu(weight, what, kind if kind == _torch.float32 else self.dtype, self.device)
+        """(pointer, dtype) of a norm's weights."""
+        kind = _torch.float32 if getattr(weight, "dtype", None) == _torch.float32 else self.dtype
+        pointer = _vector(weight, what, kind, self.head_dim, self.device)
         if weight.requires_grad and _torch.is_grad_enabled():
             raise ValueError(f"{what} requires a gradient, which the cache's calls do not give: detach it, or call "
                              "under torch.no_grad()")
-        return _vector(weight, what, kind, self.head_dim, self.device)
+        return pointer, kind
 
     def _batch(self, layer, pages, starts, lengths, n_tokens, status):
         if self._blank is None:
@@ -233,11 +234,11 @@ class KvCache:
         if q_norm is not None or k_norm is not None:
             if q_norm is not None and q is None:
                 raise ValueError("q_norm without q")
-            one = k_norm if q_norm is None else q_norm
-            norm = KvNorm(self._norm(q_norm, "q_norm") if q_norm is not None else None,
-                          self._norm(k_norm, "k_norm") if k_norm is not None else None, _codes[one.dtype], norm_eps)
-            if q_norm is not None and k_norm is not None and q_norm.dtype != k_norm.dtype:
-                raise TypeError(f"q_norm and k_norm must be alike, got {q_norm.dtype} and {k_norm.dtype}")
+            qw, kind_q = (None, None) if q_norm is None else self._norm(q_norm, "q_norm")
+            kw, kind_k = (None, kind_q) if k_norm is None else self._norm(k_norm, "k_norm")
+            if kind_q is not None and kind_q != kind_k:
+                raise TypeError(f"q_norm and k_norm must be alike, got {kind_q} and {kind_k}")
+            norm = KvNorm(qw, kw, _codes[kind_k], norm_eps)
         _run(self._index, lib().moe_kv_append_ext, b, self._scales[layer], self._rope, norm, _codes[kind], kp, ks, vp, vs,
              qp, qs, op, os)
         return q_out
