@@ -146,7 +146,9 @@ int plan(AttendArgs *a, uint64_t *bytes, int dim) {
   a->target_log2 = 0;
   while (1 << a->target_log2 < target) ++a->target_log2;
   a->nearest = few && 4 * tiles * kv.kv_heads >= resident;
-  a->min_keys = few ? kFewMinKeys : kManyMinKeys;
+  // where there are tiles enough, keys of 8 bits are as many again: 64 sequences of 50 to 1500, 24.8 us, with 256 keys 28.5
+  const bool wide = few && kv.key_scales && target > resident;
+  a->min_keys = few && !wide ? kFewMinKeys : kManyMinKeys;
   // units: a tile's keys / C, to the nearest whole number; with C >= all tiles' keys / (target /
   // kv_heads) that is at most target / kv_heads in all, and one more per tile; nor can a tile
   // have more than its table's keys give.  A split tile's units, x + 1/2 at x >= 3/2, are fewer than 2 x.
