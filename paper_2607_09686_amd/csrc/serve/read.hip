@@ -2,15 +2,22 @@
 // inverse of appending, without its turn).
 //
 // Bound by the bytes it moves.  A wave takes the tokens of one sequence within one aligned run of
-// eight positions, as a block does in appending, or a share of them where runs are few.  Of keys a lane takes 16 bytes of the
-// cache; of values 16 bytes of eight tokens, which it writes as a piece of each token's row, a wave's pieces next to each other.
-// Measured: 65531 tokens of 4 heads of 128 from 8 bits, 202 MB, 39 us = 5.2 TB/s (a block to a run: 49); 32000 from 16 bits,
-// 131 MB, 23 us in all.
+// eight positions, as a block does in appending, or a share of them where runs are few.  Of keys a lane takes eight
+// elements of a token, of values two of eight tokens, which it writes as a piece of each token's row: a wave's pieces
+// lie next to each other.  Measured: 65531 tokens of 4 heads of 128 from 8 bits, 202 MB, 33 us = 6.1 TB/s (a third of them
+// read); with 16 elements of a key to a lane, whose two stores leave every other 16 bytes out, 38.6.
 #include "append.h"
 #include "held.h"
 
 namespace moecache {
 namespace {
+
+// Rows go past the second-level caches, where they would only take the place of what is read: 65531 tokens of 4 heads of
+// 128 33 us, else 44 (32000 from 16 bits 22.4 and 25.4).
+template <class T>
+__device__ __forceinline__ void put(void *p, T v) {
+  __builtin_nontemporal_store(v, (T *)p);
+}
 
 template <class E, bool Held>
 __global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a) {
@@ -22,25 +29,22 @@ __global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a) {
   const int64_t pool = (int64_t)r.page * kv.kv_heads, head_elems = (int64_t)D << kv.page_shift;
   const float none = __builtin_nanf("");
   const u32x4 nan = pack<E>({none, none, none, none, none, none, none, none});
-  const int units = D / kUnit, keys = kv.kv_heads * units * kRun, all = keys + kv.kv_heads * D / 2;
+  const int units = D / 8, keys = kv.kv_heads * units * kRun, all = keys + kv.kv_heads * D / 2;
   for (int i = blockIdx.y * 64 + threadIdx.x % 64; i < all; i += gridDim.y * 64) {
-    if (i < keys) {
-      const int t = i % kRun, u = i / kRun % units, head = i / kRun / units, tp = in_page + t;
+    if (i < keys) {  // eight elements of a token
+      const int t = i / 2 % kRun, u = i / (2 * kRun) % (units / 2) * 2 + i % 2, head = i / kRun / units, tp = in_page + t;
       if (t >= n) continue;
-      uint16_t *dst = (uint16_t *)a.k + (int64_t)(r.row + t) * a.k_stride + head * D + u * kUnit;
-      const int64_t at = (pool + head) * head_elems + (tp & ~15) * D + (u * 16 + (tp & 15)) * kUnit;
+      uint16_t *dst = (uint16_t *)a.k + (int64_t)(r.row + t) * a.k_stride + head * D + u * 8;
+      const int64_t at = (pool + head) * head_elems + (tp & ~15) * D + (tp & 15) * kUnit;
       if (!r.write) {
-        *(u32x4 *)dst = nan;
-        if (Held) *(u32x4 *)(dst + 8) = nan;
+        put(dst, nan);
       } else if constexpr (Held) {
-        const u32x4 c = *(const u32x4 *)((const uint8_t *)kv.keys + at);
+        const uint2 c = *(const uint2 *)((const uint8_t *)kv.keys + at + u / 2 * 256 + u % 2 * 8);
         const float s = scale_of(kv.key_scales[((pool + head) << kv.page_shift) + tp]);
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-          *(u32x4 *)(dst + 8 * j) = u32x4{decode(c[2 * j], false, s, E()), decode(c[2 * j], true, s, E()),
-                                          decode(c[2 * j + 1], false, s, E()), decode(c[2 * j + 1], true, s, E())};
+        put(dst, u32x4{decode(c.x, false, s, E()), decode(c.x, true, s, E()), decode(c.y, false, s, E()),
+                       decode(c.y, true, s, E())});
       } else {
-        *(u32x4 *)dst = *(const u32x4 *)(kv.keys + at);
+        put(dst, *(const u32x4 *)(kv.keys + at + u * 128));
       }
       continue;
     }
@@ -73,7 +77,7 @@ __global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a) {
 #pragma unroll
     for (int t = 0; t < kRun; ++t) {
       const int row = t - (in_page & 7);
-      if (row >= 0 && row < n) *(uint32_t *)((uint16_t *)a.v + (int64_t)(r.row + row) * a.v_stride + head * D + d) = out[t];
+      if (row >= 0 && row < n) put((uint16_t *)a.v + (int64_t)(r.row + row) * a.v_stride + head * D + d, out[t]);
     }
   }
 }
@@ -84,7 +88,7 @@ hipError_t launch(const ReadArgs &a, hipStream_t s) {
   const int runs = a.kv.n_tokens / kRun + 2 * a.kv.n_seqs;
   const void *fn = a.kv.key_scales ? (const void *)read_kernel<E, true> : (const void *)read_kernel<E, false>;
   int shares = 1;
-  while (shares < 8 && 2 * shares * runs <= 8192) shares *= 2;
+  while (shares < 8 && 2 * shares * runs <= 16384) shares *= 2;  // waves enough to fill the card twice
   return hipLaunchKernel(fn, dim3((runs + kThreads / 64 - 1) / (kThreads / 64), shares), dim3(kThreads), args, 0, s);
 }
 
