@@ -118,10 +118,11 @@ int tile_rows(const KvView &kv) {
 
 // The launch over what all sequences begin with: tiles of all rows together, each cut into units alike.  A unit's
 // time goes with its keys, and each unit more leaves a tile's partial results to write and to read; with x tiles (of all
-// KV heads) of S keys the two balance at sqrt(S x) units, up to a factor that measured as 1/2, rounded down to a power of
-// two per tile.  us with half as many units, as many, and twice: 64 sequences behind 8192 (16 tiles, 8 units each) 61, 43,
-// 46; 8 behind 65536 in 8 bits (4, 64) 40, 30, 39; 16 behind 4096 (4, 16) 21, 17, 17; 32 behind 32768 (8, 32) 54, 37, 43;
-// 8 chunks of 50 to 200 behind 8192 (256, 2) 186, 148, 146.  Not more than the card holds twice, for the workspace's sake.
+// KV heads) of S keys the two balance at sqrt(S x) units, up to a factor that measured as about 0.45: n = 0.45 sqrt(S / x)
+// to a tile, to the nearest power of two (5 n^2 x <= 2 S).  us with half as many, as many, and twice: 64 sequences behind
+// 8192 (16 tiles, 8 units each) 61, 41, 46; 8 behind 65536 in 8 bits (4, 64) 40, 29, 39; 24 windows behind 2992 (16, 8) 25,
+// 22, 28; 16 behind 4096 (4, 16) 21, 17, 17; 32 behind 32768 (8, 32) 54, 37, 43; 8 chunks of 50 to 200 behind 8192 (256, 2)
+// 186, 148, 146.  Not more than the card holds twice, for the workspace's sake.
 // S is what the prefix's pages hold, its count is on the device.
 constexpr int kPrefixMinKeys = 128;
 void plan_prefix(AttendArgs *a) {
@@ -131,7 +132,7 @@ void plan_prefix(AttendArgs *a) {
   a->prefix_tiles = (int)((rows + a->prefix_rows - 1) / a->prefix_rows);
   const int64_t tiles = (int64_t)a->prefix_tiles * kv.kv_heads;
   int64_t n = 1;
-  while (4 * (2 * n) * (2 * n) * tiles <= keys && keys / (2 * n) >= kPrefixMinKeys && 2 * n * tiles <= 2 * kResident) n *= 2;
+  while (5 * (2 * n) * (2 * n) * tiles <= 2 * keys && keys / (2 * n) >= kPrefixMinKeys && 2 * n * tiles <= 2 * kResident) n *= 2;
   a->prefix_splits = (int)n;
 }
 
