@@ -328,11 +328,15 @@ __device__ __forceinline__ void mask_scores(f32x16 (&s)[N], int t0, int pos, int
 // Scores to probabilities over 32 * N keys: takes the new maximum, rescales the rows where some
 // row's maximum rose, and packs the B operands of the second product.
 // Probabilities are rounded to the cache's type, the type the matrix cores multiply; the sum
-// is taken in fp32 before that.  times, if given: a power of two that each key's probability is
-// multiplied by for the product, which rounds as without it.
-template <class E, int D, int N>
-__device__ __forceinline__ void softmax_step(f32x16 (&s)[N], Rows<D> &st, u32x4 (&p)[2 * N], float scale,
-                                             const float *times = nullptr) {
+// is taken in fp32 before that.  times(i), if given: powers of two that the probabilities of the i-th eight of this
+// lane's keys are multiplied by for the product, which rounds as without them.
+struct alignas(16) Eight {
+  float v[8];
+};
+struct AsIs {};
+template <class E, int D, int N, class T = AsIs>
+__device__ __forceinline__ void softmax_step(f32x16 (&s)[N], Rows<D> &st, u32x4 (&p)[2 * N], float scale, T times = T()) {
+  constexpr bool kTimes = !__is_same(T, AsIs);
   float mx = s[0][0];
 #pragma unroll
   for (int n = 0; n < N; ++n)
@@ -357,11 +361,16 @@ __device__ __forceinline__ void softmax_step(f32x16 (&s)[N], Rows<D> &st, u32x4 
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       x8 e;
+      Eight f;
+      if constexpr (kTimes) f = times(2 * n + c);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float v = __builtin_amdgcn_exp2f(fmaf(s[n][8 * c + j], scale, -base));
         st.l += v;
-        e[j] = (E)(times ? v * times[16 * n + 8 * c + j] : v);
+        if constexpr (kTimes)
+          e[j] = (E)(v * f.v[j]);
+        else
+          e[j] = (E)v;
       }
       p[2 * n + c] = __builtin_bit_cast(u32x4, e);
     }
@@ -632,19 +641,21 @@ __device__ __forceinline__ u32x4 operand(uint32_t lo, uint32_t hi, float scale) 
                decode(hi, true, scale, E())};
 }
 // An operand of eight tokens' values times their powers of two.
-__device__ __forceinline__ u32x4 times_pairs(u32x4 v, const float *s) {
+__device__ __forceinline__ u32x4 times_pairs(u32x4 v, const Eight &s) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const f16x2 t = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(s[2 * i], s[2 * i + 1]));
+    const f16x2 t = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(s.v[2 * i], s.v[2 * i + 1]));
     const uint32_t pair = v[i];  // (a cast of the vector's element would be one of its first)
     v[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, pair) * t);
   }
   return v;
 }
 // The scales of eight tokens' values, for this lane's half of 16.
-__device__ __forceinline__ void scales_of(uint2 bytes, float *s) {
+__device__ __forceinline__ Eight scales_of(uint2 bytes) {
+  Eight s;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) s[j] = scale_of((j < 4 ? bytes.x : bytes.y) >> (8 * (j % 4)) & 255);
+  for (int j = 0; j < 8; ++j) s.v[j] = scale_of((j < 4 ? bytes.x : bytes.y) >> (8 * (j % 4)) & 255);
+  return s;
 }
 
 // Keys and values of one step of 32 keys as they lie in memory, and their scales.
@@ -678,7 +689,8 @@ __device__ __forceinline__ void few_body(const AttendArgs &a, FewLds<D> &lds, in
     return;
   }
   const KvView &kv = a.kv;
-  const int lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes, half = lane / 32, n = lane % 32;
+  const int lane = threadIdx.x % kLanes, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+  const int half = lane / 32, n = lane % 32;
   if (threadIdx.x == 0) bad = 0;
   const int part = wave % R, turn = wave / R;
   const int rows = u.q.count * kv.group, before = u.q.length - u.q.count;
@@ -762,10 +774,12 @@ __device__ __forceinline__ void few_body(const AttendArgs &a, FewLds<D> &lds, in
       const bool edge = V != kPrefix && (t0 + 31 > first || (window && t0 <= last - window));
       u32x4 p[2];
       if (edge) mask_scores<1>(s, t0, pos, floor);
-      float times[16];
-      if constexpr (Held) scales_of(x.vs[0], times), scales_of(x.vs[1], times + 8);
-      constexpr bool kFold = Held && __is_same(E, __bf16);
-      softmax_step<E, D, 1>(s, st, p, a.scale_log2, kFold ? times : nullptr);
+      constexpr bool kFold = Held && __is_same(E, __bf16);  // else the values are multiplied
+      auto times = [&](int c) { return scales_of(x.vs[c]); };
+      if constexpr (kFold)
+        softmax_step<E, D, 1>(s, st, p, a.scale_log2, times);
+      else
+        softmax_step<E, D, 1>(s, st, p, a.scale_log2);
       bool odd = false;
       if constexpr (Held) {
 #pragma unroll
@@ -774,7 +788,7 @@ __device__ __forceinline__ void few_body(const AttendArgs &a, FewLds<D> &lds, in
 #pragma unroll
           for (int i = 0; i < D / 32; ++i) {
             v[i] = operand<E>(x.v[c][i / 2][i % 2 * 2], x.v[c][i / 2][i % 2 * 2 + 1], 1.f);
-            if constexpr (!kFold) v[i] = times_pairs(v[i], times + 8 * c);
+            if constexpr (!kFold) v[i] = times_pairs(v[i], times(c));
           }
           if (edge) odd |= clean_values<E, D>(v, t0 + 16 * c, u.q.length);
 #pragma unroll
@@ -871,11 +885,14 @@ struct ManyLds {
   uint8_t tiles[4 * 64 * D * 2];  // [2][K tile, V tile], each four groups
   int ids[kIds];
   int bad;
+  alignas(16) float scales[2][64];  // of the V tiles' tokens, where they are not in the tile's values
 };
 template <class E, int D, bool Held, Cover V>
 __device__ __forceinline__ void many_body(const AttendArgs &a, ManyLds<D> &shared, int block) {
   constexpr int M = 128, KT = 64;
   typedef typename std::conditional<Held, uint8_t, uint16_t>::type S;
+  // bf16: values' powers of two go to the probabilities (which fp16 has no room for)
+  constexpr bool kFold = Held && __is_same(E, __bf16);
   constexpr int kTileBytes = KT * D * 2;
   auto &lds = shared.tiles;
   auto &ids = shared.ids;
@@ -887,7 +904,8 @@ __device__ __forceinline__ void many_body(const AttendArgs &a, ManyLds<D> &share
     return;
   }
   const KvView &kv = a.kv;
-  const int lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes, half = lane / 32, n = lane % 32;
+  const int lane = threadIdx.x % kLanes, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+  const int half = lane / 32, n = lane % 32;
   if (threadIdx.x == 0) bad = 0;
   const int rows = u.q.count * kv.group, wrow = u.tile * M + 32 * wave, row = wrow + n;
   const int before = u.q.length - u.q.count;
@@ -935,8 +953,8 @@ __device__ __forceinline__ void many_body(const AttendArgs &a, ManyLds<D> &share
     };
     // 8 bits: into registers, from which a tile goes to LDS in 16 bits, laid out alike
     u32x4 kr[Held ? D / 64 : 1], vr[Held ? D / 64 : 1];
-    uint32_t kb;
-    uint2 vb[Held ? D / 64 : 1];
+    uint32_t kb, vb;
+    uint2 vb8[Held && !kFold ? D / 64 : 1];
     auto fetch = [&](int t0) {
       if constexpr (Held) {
         const int t = min(t0 + 16 * wave, (end - 1) & ~15);
@@ -946,27 +964,27 @@ __device__ __forceinline__ void many_body(const AttendArgs &a, ManyLds<D> &share
         for (int i = 0; i < D / 64; ++i) {
           kr[i] = *(const u32x4 *)(keys + at + i * 1024);
           vr[i] = *(const u32x4 *)(values + at + i * 1024);
-          vb[i] = *(const uint2 *)(vs + sc + 8 * ((i * 64 + lane) / (D / 2)));
+          if constexpr (!kFold) vb8[i] = *(const uint2 *)(vs + sc + 8 * ((i * 64 + lane) / (D / 2)));
         }
         kb = ks[sc + lane % 16];
+        if constexpr (kFold) vb = vs[sc + lane % 16];
       }
     };
     auto unpack = [&](int b) {
       if constexpr (Held) {
         uint8_t *dst = lds + b * 2 * kTileBytes + wave * 16 * D * 2;
         const float s = scale_of(kb);
+        if (kFold && lane < 16) shared.scales[b][wave * 16 + lane] = scale_of(vb);
 #pragma unroll
         for (int i = 0; i < D / 64; ++i) {
           const int unit = i * 64 + lane;  // keys: 16 elements of a token; values: eight tokens of two elements
           uint8_t *kd = dst + (unit / 16 * 32 + unit % 16) * 16, *vd = dst + kTileBytes + unit * 32;
-          float t[8];
-          scales_of(vb[i], t);
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             *(u32x4 *)(kd + j * 256) = operand<E>(kr[i][2 * j], kr[i][2 * j + 1], s);
-            const uint32_t lo = vr[i][2 * j], hi = vr[i][2 * j + 1];
-            *(u32x4 *)(vd + j * 16) = u32x4{decode2(lo, false, t[0], t[1], E()), decode2(lo, true, t[2], t[3], E()),
-                                            decode2(hi, false, t[4], t[5], E()), decode2(hi, true, t[6], t[7], E())};
+            u32x4 v = operand<E>(vr[i][2 * j], vr[i][2 * j + 1], 1.f);
+            if constexpr (!kFold) v = times_pairs(v, scales_of(vb8[i]));
+            *(u32x4 *)(vd + j * 16) = v;
           }
         }
       }
@@ -1001,9 +1019,15 @@ __device__ __forceinline__ void many_body(const AttendArgs &a, ManyLds<D> &share
         for (int j = 0; j < 2; ++j)
           s[j] = mma(*(const u32x4 *)(kt + j * 64 * D + c * 512 + koff), q[c], s[j], E());
       const bool edge = V != kPrefix && (t0 + KT - 1 > first || (window && t0 <= last - window));
+      auto softmax = [&](u32x4 (&p)[4]) {
+        if constexpr (kFold)
+          softmax_step<E, D, 2>(s, st, p, a.scale_log2, [&](int c) { return *(const Eight *)(shared.scales[b] + 16 * c + 8 * half); });
+        else
+          softmax_step<E, D, 2>(s, st, p, a.scale_log2);
+      };
       u32x4 p[4];
       if (!edge) {
-        softmax_step<E, D, 2>(s, st, p, a.scale_log2);
+        softmax(p);
 #pragma unroll
         for (int c = 0; c < 4; ++c)
 #pragma unroll
@@ -1011,7 +1035,7 @@ __device__ __forceinline__ void many_body(const AttendArgs &a, ManyLds<D> &share
             st.acc[i] = mma(*(const u32x4 *)(vt + c * 32 * D + i * 512 + voff), p[c], st.acc[i], E());
       } else {
         mask_scores<2>(s, t0, pos, floor);
-        softmax_step<E, D, 2>(s, st, p, a.scale_log2);
+        softmax(p);
         bool odd = false;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
