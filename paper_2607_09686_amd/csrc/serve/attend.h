@@ -1053,11 +1053,14 @@ __device__ __forceinline__ void many_body(const AttendArgs &a, ManyLds<D> &share
     }
   }
 
-  if (row >= rows) return;
+  // this lane's row again, from its number alone: the loop leaves no register for it
+  int own = threadIdx.x % kLanes;
+  asm volatile("" : "+v"(own));
+  const int trow = 32 * wave + own % 32, end_row = u.tile * M + trow, own_half = own / 32;
+  if (end_row >= rows) return;
   float l = st.l + __shfl_xor(st.l, 32);
   if (bad) l = __builtin_nanf("");
-  const int trow = 32 * wave + n;
-  if (u.slot >= 0 && half == 0) {
+  if (u.slot >= 0 && own_half == 0) {
     float *ml = unit_ml<D, M, V>(a, u.slot, u.kvh, trow);
     ml[0] = st.m, ml[1] = l;
   }
@@ -1067,11 +1070,11 @@ __device__ __forceinline__ void many_body(const AttendArgs &a, ManyLds<D> &share
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       const f32x4 o{st.acc[i][4 * g], st.acc[i][4 * g + 1], st.acc[i][4 * g + 2], st.acc[i][4 * g + 3]};
-      const int d = 32 * i + 8 * g + 4 * half;
+      const int d = 32 * i + 8 * g + 4 * own_half;
       if (u.slot >= 0)
         *(f32x4 *)(unit_o<D, M, V>(a, u.slot, u.kvh, trow) + d) = o;
       else
-        store_out<E, D>(a, u.q, u.kvh, row, d, o * inv);
+        store_out<E, D>(a, u.q, u.kvh, end_row, d, o * inv);
     }
 }
 
