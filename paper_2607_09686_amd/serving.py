@@ -26,12 +26,13 @@ def _bind():
 
 
 def _gpu(t, what, dtype, device):
+    if isinstance(t, _torch.Tensor) and t.device == device and t.dtype == dtype:
+        return
     if not isinstance(t, _torch.Tensor):
         raise TypeError(f"{what} must be a torch tensor")
     if t.device != device:
         raise ValueError(f"{what} must live on {device}, not on {t.device}")
-    if t.dtype != dtype:
-        raise TypeError(f"{what} must be {dtype}, got {t.dtype}")
+    raise TypeError(f"{what} must be {dtype}, got {t.dtype}")
 
 
 def _vector(t, what, dtype, n, device):
@@ -222,8 +223,10 @@ class KvCache:
         if q is not None:
             qp, qs = _rows(q, "q", kind, heads, dim, n, device)
             if q_out is None:
-                q_out = _torch.empty((n, heads, dim), dtype=self.dtype, device=device)
-            op, os = _rows(q_out, "q_out", self.dtype, heads, dim, n, device)
+                q_out = _torch.empty_strided((n, heads, dim), (heads * dim, dim, 1), dtype=self.dtype, device=device)
+                op, os = q_out.data_ptr(), heads * dim
+            else:
+                op, os = _rows(q_out, "q_out", self.dtype, heads, dim, n, device)
         elif q_out is not None:
             raise ValueError("q_out without q")
         b = self._batch(layer, pages, starts, lengths, n, status)
@@ -266,8 +269,10 @@ class KvCache:
         n, device, heads, dim = q.shape[0], self.device, self.n_heads, self.head_dim
         qp, qs = _rows(q, "q", self.dtype, heads, dim, n, device)
         if out is None:
-            out = _torch.empty((n, heads, dim), dtype=self.dtype, device=device)
-        op, os = _rows(out, "out", self.dtype, heads, dim, n, device)
+            out = _torch.empty_strided((n, heads, dim), (heads * dim, dim, 1), dtype=self.dtype, device=device)
+            op, os = out.data_ptr(), heads * dim
+        else:
+            op, os = _rows(out, "out", self.dtype, heads, dim, n, device)
         b = self._batch(layer, pages, starts, lengths, n, status)
         front = None
         if prefix is not None or shared is not None:
