@@ -403,14 +403,16 @@ int moe_kv_attend_workspace(const moe_kv_batch *b, uint64_t *bytes);
  * stands for c_d 2^e, which the batch's dtype holds exactly.  NaN and infinities are
  * held as NaN and do not count for e (a vector without a finite element has the least
  * e).  Rows are turned and normalised before, so each element is rounded once.  A
- * token takes 2 (head_dim + 1) bytes a KV head. */
+ * token takes 2 (head_dim + 1) bytes a KV head.  Other exponents than these are never written; what
+ * they stand for is not held exactly, but rows that do not see the token stay as they are. */
 typedef struct {
   uint8_t *keys, *values; /* device, 16-byte aligned, [n_pages][n_kv_heads][page_tokens] */
 } moe_kv_scales;
 
 /* The norm of each head's queries and keys before their turn:
  *   x_d / sqrt(mean of x^2 + eps) * weight_d
- * over all head_dim elements, the sum in fp32.  A NULL weight: no norm there. */
+ * over all head_dim elements, the sum in fp32 (which elements of 2^60 overflow).  A NULL
+ * weight: no norm there. */
 typedef struct {
   const void *q_weight, *k_weight; /* device [head_dim], 16-byte aligned */
   int32_t dtype;                   /* of the weights: MOE_F32 or the batch's dtype */

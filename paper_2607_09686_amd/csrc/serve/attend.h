@@ -628,11 +628,16 @@ __device__ __forceinline__ float finish(float l) { return l == 0.f ? 0.f : 1.f /
 // block's waves take 32 rows each: of a tile of 32 all four the same ones, in turns at the unit's
 // steps of 32 keys, of a tile of 64 two and two (the second pair finds the step's keys in the CU's
 // cache).  Keys go straight from memory into the operand registers (LDS would only add a copy); a
-// step's are requested while the step before is multiplied.  Two blocks to a CU (249 registers of
+// step's are requested while the step before is multiplied.  Two blocks to a CU (232 registers of
 // 256 with heads of 128), 64 KB of requests in flight.  Measured, 4 KV heads of 128: 64 sequences of 200
 // to 16000 keys, 1.10 GB, 203 us = 5.4 TB/s; 24 windows of 40 rows over 1000 to 9000 keys, 219 MB, 50 us where the
 // last-level cache holds them, the whole call 69 on keys that it does not (and 7 of the join).  Heads of 256, whole calls: 64
 // sequences of 8000 keys, 2.10 GB, 360 us = 5.8 TB/s; 24 windows of 40 rows, 494 MB, 132 us.
+//
+// Of a cache of 8 bits (held.h) a load of 16 bytes brings a lane two products' operands, keys' in the order that load_q
+// takes the queries in, values' as two neighbouring elements (d_of); a step's bytes are half, so two steps' are under way, and
+// the queries stay in LDS.  The conversions are 64 of about 260 vector instructions a step.  64 sequences of 200 to 16000
+// keys, 577 MB, 113 us = 5.1 TB/s.
 // ---------------------------------------------------------------------------------------------
 // An operand of eight numbers of 8 bits (two words) times a power of two.
 template <class E>
@@ -873,9 +878,12 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attend_few_kernel(A
 // LDS for 1024 cycles of products, the full rate of LDS; the products take 40 % of the time, the
 // softmax's exponentials, sums and conversions about as much again.  The loop holds no step with
 // masks (those take a path of their own, with half the speed).  Measured: 4096 tokens behind
-// 12288, 32 heads of 128 on 4, 0.96 TFLOP: the call 0.94 to 0.98 ms = 0.98 to 1.02 PFLOP/s from run to run (a library
-// product of 8192^3: 1.17), the kernel alone 0.98 to 1.03 where nothing else comes between its launches.  16 heads of 256
-// on 4, 4096 tokens behind 4096: 0.54 ms = 0.76 PFLOP/s.
+// 12288, 32 heads of 128 on 4, 0.96 TFLOP: the call 0.915 to 0.925 ms = 1.04 PFLOP/s (a library product of 8192^3: 1.17).
+// 16 heads of 256 on 4, 4096 tokens behind 4096: 0.54 ms = 0.76 PFLOP/s.
+//
+// Of a cache of 8 bits the next tile comes into registers and from there to LDS in 16 bits, laid out alike, a quarter
+// to a wave; values' powers of two go to the probabilities in bf16 (multiplying the values, as in fp16, 1020 us instead of
+// 990 for the 4096 tokens).  0.96 PFLOP/s.
 // ---------------------------------------------------------------------------------------------
 typedef __attribute__((address_space(3))) void lds_void;
 typedef const __attribute__((address_space(1))) void global_void;
