@@ -179,6 +179,84 @@ def test_weights_of_one_without_a_norm():
     assert torch.equal(got, q)
 
 
+@pytest.mark.parametrize("held", [False, True])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(7, 7, 64), (320, 64, 64), (1024, 1, 128), (130, 65, 256)])
+def test_any_number_of_heads(held, heads, kv_heads, dim):
+    """Each head of each token by itself: its norm, and what it is held as (no turn, no q for the second call)."""
+    torch = torch_cuda()
+    b = ExtBatch(torch, [(3, 30), (8, 8), (1, 77), (20, 3)], heads, kv_heads, dim, 16, torch.bfloat16, held=held, filled=False)
+    g = torch.Generator().manual_seed(heads)
+    q, k, v = (torch.randn(b.n, h, dim, generator=g) * 2 for h in (heads, kv_heads, kv_heads))
+    w = torch.rand(dim, generator=g) + 0.5
+    cache = b.cache(rope_dim=0)
+    got = cache.append(k.cuda(), v.cuda(), *b.index(), q=q.cuda(), q_norm=w.cuda(), k_norm=w.cuda(), norm_eps=0.5)
+    fp32 = (dim / 32 + 6) * 2.0 ** -24
+    want = ref.head_norm(q.double().numpy(), w.double().numpy(), 0.5)
+    assert (np.abs(got.double().cpu().numpy() - want) <= (2.0 ** -8 + fp32) * np.abs(want)).all()
+    kk, vv = (x.double().cpu().numpy() for x in cache.read(b.n, *b.index()))
+    want = ref.head_norm(k.double().numpy(), w.double().numpy(), 0.5)
+    if held:
+        most = np.abs(want).max(-1, keepdims=True)
+        assert (np.abs(kk - want) <= (2.0 ** -4 + 2 * fp32) * np.abs(want) + 2.0 ** -17 * most).all()
+        c, e = ref.hold(v.double().numpy(), -100, 119)
+        np.testing.assert_array_equal(vv, c * 2.0 ** e[..., None].astype(np.float64))
+    else:
+        assert (np.abs(kk - want) <= (2.0 ** -8 + fp32) * np.abs(want)).all()
+        np.testing.assert_array_equal(vv, v.bfloat16().double().numpy())
+    pools = [p.clone() for p in b.pools()]
+    assert cache.append(k.cuda(), v.cuda(), *b.index(), k_norm=w.cuda(), norm_eps=0.5) is None
+    assert all(torch.equal(p, x) for p, x in zip(b.pools(), pools))
+
+
+@pytest.mark.parametrize("held", [False, True])
+@pytest.mark.parametrize("counts", [[1] * 64, [1] * 65, [n % 12 for n in range(300)], [1] * 1100, [0] * 90 + [9] + [0] * 90])
+def test_many_sequences_written_and_read(held, counts):
+    torch = torch_cuda()
+    b = ExtBatch(torch, [(n, 7 * i % 50) for i, n in enumerate(counts)], 4, 2, 64, 16, torch.float16, held=held, filled=False,
+                 pad_rows=2)
+    x = torch.from_numpy(np.random.default_rng(1).standard_normal((2, b.n, 2, 64))).float()
+    w = torch.ones(64, device="cuda")
+    cache = b.cache(rope_dim=0)
+    cache.append(x[0].cuda(), x[1].cuda(), *b.index(), k_norm=w)
+    k = torch.full((b.n, 2, 64), 7.0, dtype=b.dtype, device="cuda")
+    k, v = cache.read(b.n, *b.index(), k=k)
+    new = b.n - 2
+    assert (k[new:] == 7).all()
+    if held:
+        c, e = ref.hold(x[1, :new].double().numpy(), -15, 7)
+        want = c * 2.0 ** e[..., None].astype(np.float64)
+    else:
+        want = x[1, :new].half().double().numpy()
+    np.testing.assert_array_equal(v[:new].double().cpu().numpy(), want)
+    want = ref.head_norm(x[0, :new].double().numpy(), np.ones(64), 1e-6)
+    step = 2.0 ** -4 if held else 2.0 ** -11
+    near = (step + 16 * 2.0 ** -24) * np.abs(want) + 2.0 ** -17 * np.abs(want).max(-1, keepdims=True)
+    assert (np.abs(k[:new].double().cpu().numpy() - want) <= near).all()
+
+
+@pytest.mark.parametrize("held", [False, True])
+def test_strided_rows(held):
+    """q, k and v as slices of one projection's output, with norms; rows read back into slices."""
+    torch = torch_cuda()
+    for seqs in ([(1, 77), (1, 5)], [(90, 20)]):
+        b = ExtBatch(torch, seqs, 4, 2, 128, 64, torch.bfloat16, held=held, filled=False)
+        flat = torch.randn(b.n, 8 * 128 + 64, device="cuda").to(b.dtype)
+        q, k, v = flat[:, :512].view(b.n, 4, 128), flat[:, 512:768].view(b.n, 2, 128), flat[:, 768:1024].view(b.n, 2, 128)
+        w = torch.rand(128, device="cuda") + 0.5
+        wide = torch.full((b.n, 6, 128), 7.0, dtype=b.dtype, device="cuda")
+        cache = b.cache()
+        cache.append(k, v, *b.index(), q=q, q_out=wide[:, 1:5], q_norm=w, k_norm=w)
+        pools = [p.clone() for p in b.pools()]
+        got = cache.append(k.contiguous(), v.contiguous(), *b.index(), q=q.contiguous(), q_norm=w, k_norm=w)
+        assert torch.equal(wide[:, 1:5], got) and (wide[:, 0] == 7).all() and (wide[:, 5] == 7).all()
+        assert all(torch.equal(p, x) for p, x in zip(b.pools(), pools))
+        o = torch.full((b.n, 6, 128), 7.0, dtype=b.dtype, device="cuda")
+        cache.read(b.n, *b.index(), k=o[:, 1:3], v=o[:, 3:5])
+        want = cache.read(b.n, *b.index())
+        assert torch.equal(o[:, 1:3], want[0]) and torch.equal(o[:, 3:5], want[1])
+        assert (o[:, 0] == 7).all() and (o[:, 5] == 7).all()
+
+
 # ------------------------------------------------------------------------------ reading back
 
 @pytest.mark.parametrize("held", [False, True])
@@ -294,6 +372,47 @@ def test_scales_of_every_size(dtype, new, dim):
             (b.k, b.v)[i][s] = c * 2.0 ** e[..., None].astype(np.float64)
         b.fill(s)
     b.check(b.cache().attend(b.q_gpu(), *b.index()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("gap", [14.0, 17.5])
+@pytest.mark.parametrize("dim,new,shared", [(64, 1, 0), (128, 5, 0), (256, 1, 0), (128, 70, 0), (128, 1, 3000), (64, 70, 3000)])
+def test_a_first_key_far_above_the_rest(dtype, gap, dim, new, shared):
+    """The first key's score is `gap` above the others', its value zero in most elements.  fp16 adds to Batch.check's
+    tolerance that of its smallest numbers: a probability is off by at most half of 2^-24 where the largest is at
+    least 2^10, so the output by 2^-35 of the sum of |v|."""
+    torch = torch_cuda()
+    before, group = 4000, 8
+    b = ExtBatch(torch, [(new, before)] * 2, 2 * group, 2, dim, 64, types()[dtype], shared=shared, seed=7, filled=False)
+    limits, rng = LIMITS[str(b.dtype)], np.random.default_rng(8)
+    for s in range(2):
+        if s and shared:  # both sequences are the same
+            b.k[1], b.v[1] = b.k[0].copy(), b.v[0].copy()
+        else:
+            b.k[s][:, :, 0], b.k[s][0] = 0.0, 0.0
+            b.k[s][0, :, 0] = gap * dim ** 0.5 / 8
+            b.v[s] = np.abs(b.v[s]) + 0.5
+            b.v[s][0, :, 2:] = 0.0
+        for i, x in enumerate((b.k, b.v)):
+            c, e = b.codes[i][s] = ref.hold(x[s], *limits)
+            x[s] = c * 2.0 ** e[..., None].astype(np.float64)
+        b.fill(s)
+    b.q = rng.standard_normal((2 * new, 2 * group, dim)) * 0.5
+    b.q[:, :, 0] = 8.0
+    b.q = b.rounded(b.q)
+    out = b.cache().attend(b.q_gpu(), *b.index(), **b.front()).double().cpu().numpy()
+    h, scale = half_step(b.dtype), dim ** -0.5
+    tiny = float(torch.finfo(b.dtype).smallest_normal) * h
+    for s in range(2):
+        rows, pos = b.q[b.rows(s)], b.positions(s)
+        want, weight = ref.attend(rows, b.k[s], b.v[s], pos, scale)
+        big = np.linalg.norm(rows, axis=2).max() * np.linalg.norm(b.k[s], axis=2).max() * scale
+        ds = (dim + 8) * 2.0 ** -24 * big
+        tol = h * np.abs(want) + (h + 2 * ds + 2.0 ** -18) * (1 + h) * weight + 4 * tiny
+        if dtype == "f16":
+            tol += 2.0 ** -35 * np.repeat(np.cumsum(np.abs(b.v[s]), axis=0)[pos], group, axis=1)
+        err = np.abs(out[b.rows(s)] - want)
+        assert np.all(err <= tol), (s, float((err / tol).max()))
 
 
 @pytest.mark.parametrize("seqs,row", [([(5, 60)], 2), ([(120, 40)], 50), ([(120, 700)], 119)])
