@@ -90,7 +90,9 @@ __global__ __launch_bounds__(kThreads) void append_ext_kernel(AppendArgs a) {
     float nx[8], ny[8];
     auto request = [&](int h) {
       const int hr = min(h, heads - 1);  // lanes without a head of theirs read another's
-      const I *src = hr < q_heads ? q_row + (int64_t)hr * D : hr < k_end ? k_row + (hr - q_heads) * D : v_row + (hr - k_end) * D;
+      const I *src = hr < q_heads ? q_row + (int64_t)hr * D
+                     : hr < k_end ? k_row + (int64_t)(hr - q_heads) * D
+                                  : v_row + (int64_t)(hr - k_end) * D;
       const bool as_is = Held && hr >= k_end;  // values: 16 elements together
       In<I>::load(src, as_is ? part * 16 : turned.ea, nx);
       In<I>::load(src, as_is ? part * 16 + 8 : turned.eb, ny);

@@ -1029,7 +1029,8 @@ __device__ __forceinline__ void many_body(const AttendArgs &a, ManyLds<D> &share
       const bool edge = V != kPrefix && (t0 + KT - 1 > first || (window && t0 <= last - window));
       auto softmax = [&](u32x4 (&p)[4]) {
         if constexpr (kFold)
-          softmax_step<E, D, 2>(s, st, p, a.scale_log2, [&](int c) { return *(const Eight *)(shared.scales[b] + 16 * c + 8 * half); });
+          softmax_step<E, D, 2>(s, st, p, a.scale_log2,
+                                [&](int c) { return *(const Eight *)(shared.scales[b] + 16 * c + 8 * half); });
         else
           softmax_step<E, D, 2>(s, st, p, a.scale_log2);
       };

@@ -132,7 +132,10 @@ void plan_prefix(AttendArgs *a) {
   a->prefix_tiles = (int)((rows + a->prefix_rows - 1) / a->prefix_rows);
   const int64_t tiles = (int64_t)a->prefix_tiles * kv.kv_heads;
   int64_t n = 1;
-  while (5 * (2 * n) * (2 * n) * tiles <= 2 * keys && keys / (2 * n) >= kPrefixMinKeys && 2 * n * tiles <= 2 * kResident) n *= 2;
+  const auto fits = [&](int64_t n) {
+    return 5 * n * n * tiles <= 2 * keys && keys / n >= kPrefixMinKeys && n * tiles <= 2 * kResident;
+  };
+  while (fits(2 * n)) n *= 2;
   a->prefix_splits = (int)n;
 }
 
