@@ -60,7 +60,7 @@ constexpr int kMaxSampleRows = 65535;  // rows are a grid's second dimension
 // 256: of one), or with few rows twice that where half as many tiles are there already, so that a
 // long and a short sequence's units even out.  Keys below which a tile isn't split.
 constexpr int kResident = 512;
-constexpr int kFewMinKeys = 256, kManyMinKeys = 512;
+constexpr int kFewMinKeys = 256, kManyMinKeys = 512, kShortMinKeys = 192;
 
 int check_kv(const moe_kv_batch *b, const char *who, KvView *kv) {
   if (!b) return fail(MOE_EINVAL, "%s: the batch is NULL", who);
@@ -150,9 +150,13 @@ int plan(AttendArgs *a, uint64_t *bytes, int dim) {
   a->target_log2 = 0;
   while (1 << a->target_log2 < target) ++a->target_log2;
   a->nearest = few && 4 * tiles * kv.kv_heads >= resident;
-  // where there are tiles enough, keys of 8 bits are as many again: 64 sequences of 50 to 1500, 24.8 us, with 256 keys 28.5
-  const bool wide = few && kv.key_scales && target > resident;
-  a->min_keys = few && !wide ? kFewMinKeys : kManyMinKeys;
+  // Keys of 8 bits, where there are tiles of few rows enough, are as many again: 64 sequences of 50 to 1500, 24.8 us, with
+  // 256 keys 28.5.  Few tiles of 128 rows over 8 bits or behind shared tokens are cut finer (kShortMinKeys, 512 keys): 60
+  // tokens over 460 with heads of 256 27 and 38 us, 3 chunks of 108 to 210 behind 800 shared and 580 to 819 own 36 and 55,
+  // 4 of 10 to 26 behind 1312 and 333 to 409 23 and 29; with more tiles it costs, 5 chunks of 65 to 438 60 and 47.
+  const bool ext = kv.key_scales || a->shared;
+  const bool wide = few && kv.key_scales && target > resident, fine = !few && ext && 4 * tiles * kv.kv_heads <= resident;
+  a->min_keys = fine ? kShortMinKeys : few && !wide ? kFewMinKeys : kManyMinKeys;
   // units: a tile's keys / C, to the nearest whole number; with C >= all tiles' keys / (target /
   // kv_heads) that is at most target / kv_heads in all, and one more per tile; nor can a tile
   // have more than its table's keys give.  A split tile's units, x + 1/2 at x >= 3/2, are fewer than 2 x.
