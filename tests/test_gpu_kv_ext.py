@@ -445,6 +445,28 @@ def test_what_a_row_does_not_see_has_no_effect(seqs, row, dtype):
     assert torch.equal(out[:row], clean[:row]) and torch.equal(out[:, 2:], clean[:, 2:])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim,new,page", [(64, 1, 16), (128, 3, 32), (256, 5, 16), (64, 40, 16), (128, 200, 64)])
+def test_what_a_window_has_passed_has_no_effect(dtype, dim, new, page):
+    """Old tokens with numbers and scales that are none, and page ids that are none before them."""
+    torch = torch_cuda()
+    window, before = 50, 420
+    b = ExtBatch(torch, [(new, before), (new, 30)], 8, 2, dim, page, types()[dtype], seed=new, first_page=1)
+    cache, q = b.cache(window=window), b.q_gpu()
+    clean = cache.attend(q, *b.index())
+    b.check(clean, window)
+    gone = before - window + 1  # tokens that no new one sees
+    keys, values, ks, vs = b.pools()
+    for t in (gone - 1, gone - 2, gone - 40):
+        pg, at = int(b.table[0, t // page]), t % page
+        keys[0, pg, :, at // 16, :, at % 16], values[0, pg, :, at // 16, at // 8 % 2, :, at % 8] = 0x7f, 0xff
+        ks[0, pg, :, at], vs[0, pg, :, at] = 255, 255
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    assert torch.equal(cache.attend(q, *b.index(), status=status), clean) and status.item() == 0
+    b.pages[0, :gone // page] = -1
+    assert torch.equal(cache.attend(q, *b.index(), status=status), clean) and status.item() == 0
+
+
 @pytest.mark.parametrize("new", [1, 90])
 def test_bad_lengths_and_pages(new):
     torch = torch_cuda()
