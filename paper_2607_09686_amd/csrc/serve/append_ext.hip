@@ -197,7 +197,8 @@ hipError_t launch(const AppendArgs &a, hipStream_t s) {
   const int runs = a.kv.n_tokens / kRun + 2 * a.kv.n_seqs;
   const bool held = a.kv.key_scales;
   const void *fn = held ? (const void *)append_ext_kernel<E, I, true> : (const void *)append_ext_kernel<E, I, false>;
-  const int items = ((a.q ? a.kv.heads : 0) + a.kv.kv_heads * (held ? 2 : 1)) * a.dim / 128;
+  // what a wave takes of a run at once: 128 elements of its eight tokens, one KV head of 64 being half of that
+  const int items = (((a.q ? a.kv.heads : 0) + a.kv.kv_heads * (held ? 2 : 1)) * a.dim + 127) / 128;
   const int shares = std::min((items + 3) / 4, std::max(1, (kBlocks + runs - 1) / runs));
   return hipLaunchKernel(fn, dim3(runs, shares), dim3(kThreads), args, 0, s);
 }

@@ -209,6 +209,38 @@ def test_any_number_of_heads(held, heads, kv_heads, dim):
 
 
 @pytest.mark.parametrize("held", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(1, 1, 64), (4, 1, 64), (3, 3, 64), (1, 1, 128), (8, 1, 256)])
+@pytest.mark.parametrize("seqs", [[(1, 0)], [(8, 8)], [(3, 30), (8, 8), (1, 77), (20, 3)], [(300, 5)]])
+def test_few_heads_without_q(held, dtype, heads, kv_heads, dim, seqs):
+    """Keys under a norm and values into pools that hold NaN, by a call that has no queries: both are there.
+    Tolerances as test_norms_and_turns'; values are bit for bit."""
+    torch = torch_cuda()
+    t = types()[dtype]
+    b = ExtBatch(torch, seqs, heads, kv_heads, dim, 16, t, held=held, filled=False)
+    g = torch.Generator().manual_seed(dim)
+    k, v = (2 * torch.randn(b.n, kv_heads, dim, generator=g) for _ in "kv")
+    w = torch.rand(dim, generator=g) + 0.5
+    assert b.cache(rope_dim=0).append(k.cuda(), v.cuda(), *b.index(), k_norm=w.cuda(), norm_eps=0.5) is None
+    norm = (dim / 32 + 6) * 2.0 ** -24
+    for s in range(len(seqs)):
+        r, pos = b.rows(s), b.positions(s)
+        want = ref.head_norm(k[r].double().numpy(), w.double().numpy(), 0.5)
+        if held:
+            c, e = pool_values(b, "k", s, pos)
+            scale = 2.0 ** e[..., None].astype(np.float64)
+            assert (np.abs(c * scale - want) <= (2.0 ** -4 + 2 * norm) * np.abs(want) + 2.0 ** -10 * scale).all()
+            c, e = pool_values(b, "v", s, pos)
+            number, exponent = ref.hold(v[r].double().numpy(), *LIMITS[str(t)])
+            np.testing.assert_array_equal(c, number)
+            np.testing.assert_array_equal(e, exponent)
+        else:
+            tiny = float(torch.finfo(t).smallest_normal) * half_step(t)
+            assert (np.abs(pool_values(b, "k", s, pos) - want) <= (half_step(t) + 2 * norm) * np.abs(want) + tiny).all()
+            np.testing.assert_array_equal(pool_values(b, "v", s, pos), v[r].to(t).double().numpy())
+
+
+@pytest.mark.parametrize("held", [False, True])
 @pytest.mark.parametrize("counts", [[1] * 64, [1] * 65, [n % 12 for n in range(300)], [1] * 1100, [0] * 90 + [9] + [0] * 90])
 def test_many_sequences_written_and_read(held, counts):
     torch = torch_cuda()
