@@ -62,12 +62,14 @@ __global__ __launch_bounds__(kPlanThreads) void plan_behind_kernel(AttendArgs a)
 // other ones): 64 sequences behind 8192 tokens, calls of 45.6 us; 46.5 with four at once, 50 to 52 with 512 threads.
 constexpr int kJoinThreads = 256, kAtOnce = 2;
 // Blocks that join, up to rows / 4 and at least 4 of them to a tile: about 2048 in all, what the card holds at once (the
-// 64 sequences' 320 tiles with 8 each 43.2 us, with 4 42.0; the 36 of 8 sequences 29.5 and 32.8).
+// 64 sequences' 320 tiles with 8 each 43.2 us, with 4 42.0; the 36 of 8 sequences 29.5 and 32.8); fewer than 4 where
+// all of them (up to 2^23 tiles) would be more threads than a grid holds.
 static inline dim3 join_behind_grid(const AttendArgs &a, int rows) {
-  const int tiles = a.max_tiles * a.kv.kv_heads;
+  const int64_t tiles = (int64_t)a.max_tiles * a.kv.kv_heads;
   int y = 4;
   while (2 * y <= rows / 4 && 2 * y * tiles <= 2048) y *= 2;
-  return dim3(tiles, y);
+  while (y > 1 && y * tiles * kJoinThreads >= (int64_t)1 << 32) y /= 2;
+  return dim3((unsigned)tiles, y);
 }
 template <class E, int D, int M>
 __global__ __launch_bounds__(kJoinThreads) void join_behind_kernel(AttendArgs a) {

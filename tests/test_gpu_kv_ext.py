@@ -607,6 +607,28 @@ def test_a_prefix_of_more_pages_than_one_list_of_ids():
             b.check(out[s * new:(s + 1) * new])
 
 
+def test_as_many_sequences_as_a_batch_may_have():
+    """65536 of one token with 64 KV heads, 2^22 tiles, behind the same tokens: no more threads than a grid holds,
+    and every row joined."""
+    torch = torch_cuda()
+    n = 65536
+    b = ExtBatch(torch, [(1, 70)], 64, 64, 64, 16, torch.bfloat16, held=False, shared=64)
+    q = torch.randn(n, 64, 64, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(b.dtype)
+    starts = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    lengths = b.lengths - (torch.arange(n, dtype=torch.int32, device="cuda") % 6)
+    out = torch.full_like(q, float("nan"))
+    index = b.pages.expand(n, -1).contiguous(), starts, lengths
+    b.cache().attend(q, *index, out=out, **b.front())
+    near = b.cache().attend(q, *index)
+    assert torch.isfinite(out).all()
+    assert (out.float() - near.float()).norm() <= 2 * half_step(b.dtype) * near.float().norm()
+    k, v = b.k[0], b.v[0]
+    for s in (0, 1, n // 2, n - 5, n - 1):
+        total = int(lengths[s])
+        b.q, b.k[0], b.v[0], b.total[0] = q[s:s + 1].double().cpu().numpy(), k[:total], v[:total], total
+        b.check(out[s:s + 1])
+
+
 def test_the_prefix_may_lie_in_pages_of_its_own():
     torch = torch_cuda()
     b = ExtBatch(torch, [(1, 300), (2, 320), (40, 260)], 8, 2, 128, 16, torch.float16, held=False, shared=256, own_front=True)

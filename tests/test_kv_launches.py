@@ -82,3 +82,20 @@ def test_every_call_launches_blocks(launches):
             assert found and any(KINDS[call] in name for name, _ in found), (case, call)
             for name, extents in found:
                 assert min(extents) >= 1, (case, call, name, extents)
+
+
+LARGEST = [dict(n_tokens=1 << 24, n_heads=8, n_kv_heads=8, n_seqs=65536), dict(n_tokens=1 << 17, n_heads=1024, n_kv_heads=1),
+           dict(n_tokens=1 << 17, n_heads=1024, n_kv_heads=64, n_seqs=65536),
+           dict(n_tokens=1 << 16, n_heads=1024, n_kv_heads=64, n_seqs=65536), dict(n_tokens=1 << 12, n_heads=1024, n_kv_heads=1024),
+           dict(n_tokens=1 << 12, n_heads=1024, n_kv_heads=1024, n_seqs=4096),
+           dict(n_tokens=1 << 16, n_heads=64, n_kv_heads=64, n_seqs=65536), dict(n_tokens=1 << 24, n_heads=1, n_kv_heads=1)]
+
+
+def test_a_grid_holds_fewer_than_2_to_the_32_threads(launches):
+    """Of the largest batches that the argument checks accept, over short and long tables and prefixes."""
+    cases = [dict(head_dim=dim, max_pages=pages, held=held, prefix=prefix, norm=1, q=1, **kw)
+             for kw in LARGEST for dim in (64, 256) for pages in (2, 1 << 26) for held in (0, 1) for prefix in (0, 2, 1 << 26)]
+    for case, calls in zip(cases, launches(cases)):
+        for found in calls.values():
+            for name, (x, y, z, *block) in found:
+                assert x * y * z * block[0] * block[1] * block[2] < 1 << 32, (case, name, (x, y, z))
