@@ -446,9 +446,11 @@ typedef struct {
 
 /* moe_kv_attend over pools of 8 bits (scales NULL: of the batch's dtype), with what
  * all sequences begin with read once for all of them (prefix NULL: nothing; window
- * must be 0 otherwise): the same result but for rounding.  A bad id among the
- * prefix's pages makes every row NaN (MOE_KV_BAD_PAGE).  What a number of 8 bits stands
- * for is multiplied as the batch's dtype holds it. */
+ * must be 0 otherwise): the same result but for rounding.  Read once are the first
+ * *tokens / 64 * 64 tokens: a bad id among the pages that hold them makes every row NaN
+ * (MOE_KV_BAD_PAGE).  Those after them, fewer than 64, are read from the sequences' own
+ * tables; the prefix's further pages are not read and may be anything.  What a number of
+ * 8 bits stands for is multiplied as the batch's dtype holds it. */
 int moe_kv_attend_ext(const moe_kv_batch *b, const moe_kv_scales *scales, const moe_kv_prefix *prefix, int32_t window,
                       float scale, const void *q, int64_t q_stride, void *out, int64_t out_stride, void *workspace,
                       uint64_t workspace_bytes);

@@ -265,7 +265,9 @@ class KvCache:
 
         Where all sequences begin with the same tokens, prefix (int32 [n], the pages that hold them)
         and shared (int32 [1], their number, none of them new) let these be read once for all: the
-        same result but for rounding (moe_kv_prefix).  Not with a window."""
+        same result but for rounding (moe_kv_prefix).  That is the first shared // 64 * 64 tokens; the
+        others are read by way of pages, and prefix's entries for them may be anything.  Not with a
+        window."""
         n, device, heads, dim = q.shape[0], self.device, self.n_heads, self.head_dim
         qp, qs = _rows(q, "q", self.dtype, heads, dim, n, device)
         if out is None:

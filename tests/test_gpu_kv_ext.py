@@ -660,6 +660,28 @@ def test_less_is_shared_than_the_prefix_holds():
         assert torch.equal(out, want)
 
 
+@pytest.mark.parametrize("held", [False, True])
+@pytest.mark.parametrize("page,shared", [(16, 100), (16, 63), (32, 160), (64, 127), (128, 130)])
+@pytest.mark.parametrize("new", [1, 40])
+def test_which_of_the_prefix_pages_are_read(held, page, shared, new):
+    """Those of its whole 64s of tokens: a bad id there makes every row NaN, one past them has no effect."""
+    torch = torch_cuda()
+    b = ExtBatch(torch, [(new, shared + 40), (new, shared), (2, 300)], 4, 2, 64, page, torch.bfloat16, held=held, shared=shared)
+    cache, q, status = b.cache(), b.q_gpu(), torch.zeros(1, dtype=torch.int32, device="cuda")
+    clean = cache.attend(q, *b.index(), status=status, **b.front())
+    b.check(clean)
+    read = -(-(shared // 64 * 64) // page)  # pages
+    prefix = b.prefix.clone()
+    for page_id in (-1, b.n_pages):
+        b.prefix[:] = prefix
+        b.prefix[read:] = page_id
+        assert torch.equal(cache.attend(q, *b.index(), status=status, **b.front()), clean) and status.item() == 0
+        if read:
+            b.prefix[read - 1] = page_id
+            assert torch.isnan(cache.attend(q, *b.index(), status=status, **b.front())).all() and status.item() == 1
+            status.zero_()
+
+
 @pytest.mark.parametrize("new", [1, 40])
 @pytest.mark.parametrize("many", [0, 80])
 def test_what_is_no_prefix(new, many):
