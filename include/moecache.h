@@ -383,7 +383,8 @@ int moe_kv_append(const moe_kv_batch *b, const moe_kv_rope *rope, int32_t in_dty
  * the batch's dtype, strides in elements, multiples of 16 bytes; out must not
  * overlap q.  Sums and softmax in fp32; probabilities are rounded to the dtype
  * for their product with the values (in MOE_F16 those below 2^-24 of the row's largest
- * to within 2^-35 of it).  Results do not depend on where a
+ * to within 2^-35 of it).  The sums are of up to 2^8 times the values: in MOE_BF16 values whose
+ * magnitudes add up to more than 2^119 over a row's tokens may overflow.  Results do not depend on where a
  * sequence's pages lie; they may differ in rounding with what else is in the
  * batch (the work is cut by the batch's lengths), never from run to run.
  * workspace: device scratch of the size that moe_kv_attend_workspace gives for
@@ -450,7 +451,9 @@ typedef struct {
  * *tokens / 64 * 64 tokens: a bad id among the pages that hold them makes every row NaN
  * (MOE_KV_BAD_PAGE).  Those after them, fewer than 64, are read from the sequences' own
  * tables; the prefix's further pages are not read and may be anything.  What a number of
- * 8 bits stands for is multiplied as the batch's dtype holds it. */
+ * 8 bits stands for is multiplied as the batch's dtype holds it; in MOE_BF16 a probability p (the
+ * largest of a row being 1) is off by up to 2^-134 / 2^e for a value of the power 2^e where p 2^e is below 2^-126,
+ * a row therefore by at most 2^-125 for each such token. */
 int moe_kv_attend_ext(const moe_kv_batch *b, const moe_kv_scales *scales, const moe_kv_prefix *prefix, int32_t window,
                       float scale, const void *q, int64_t q_stride, void *out, int64_t out_stride, void *workspace,
                       uint64_t workspace_bytes);

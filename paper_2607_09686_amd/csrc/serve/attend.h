@@ -329,7 +329,8 @@ __device__ __forceinline__ void mask_scores(f32x16 (&s)[N], int t0, int pos, int
 // row's maximum rose, and packs the B operands of the second product.
 // Probabilities are rounded to the cache's type, the type the matrix cores multiply; the sum
 // is taken in fp32 before that.  times(i), if given: powers of two that the probabilities of the i-th eight of this
-// lane's keys are multiplied by for the product, which rounds as without them.
+// lane's keys are multiplied by for the product.  That rounds as without them down to p 2^e = 2^-126; what is less is
+// off by up to 2^-134, so that a row is by up to 2^-134 |c| <= 2^-125 for each such key (the largest p is at least 1).
 struct alignas(16) Eight {
   float v[8];
 };

@@ -447,6 +447,72 @@ def test_a_first_key_far_above_the_rest(dtype, gap, dim, new, shared):
         assert np.all(err <= tol), (s, float((err / tol).max()))
 
 
+@pytest.mark.parametrize("dtype,gap", [("bf16", 17.0), ("bf16", 21.0), ("bf16", 30.0), ("f16", 5.0), ("f16", 17.0)])
+@pytest.mark.parametrize("dim,new,shared", [(64, 1, 0), (128, 5, 0), (256, 1, 0), (128, 70, 0), (128, 1, 3000), (64, 70, 3000)])
+def test_the_least_scale_under_a_first_key_far_above_the_rest(dtype, gap, dim, new, shared):
+    """All values are held with the least power of two, 2^e, and the first key, whose value is zero in most elements,
+    scores about `gap` above the others.  bf16 rounds p 2^e for the product: below 2^-126 to within 2^-134, so a row is off by
+    2^-134 |c| a token more than Batch.check's tolerance (the largest p being at least 1).  A gap of 17 (16 or 17 in e4m3, 24.6
+    of log2, and the others' scores within 0.5 of 0) keeps p 2^-100 above 2^-126.  fp16 as the test above."""
+    torch = torch_cuda()
+    before, group = 4000, 8
+    b = ExtBatch(torch, [(new, before)] * 2, 2 * group, 2, dim, 64, types()[dtype], shared=shared, seed=7, filled=False)
+    limits, rng = LIMITS[str(b.dtype)], np.random.default_rng(8)
+    for s in range(2):
+        if s and shared:  # both sequences are the same
+            b.k[1], b.v[1] = b.k[0].copy(), b.v[0].copy()
+        else:
+            b.k[s][:, :, 0], b.k[s][0] = 0.0, 0.0
+            b.k[s] *= 0.1
+            b.k[s][0, :, 0] = gap * dim ** 0.5 / 8
+            b.v[s] = (np.abs(b.v[s]) + 0.5) * 2.0 ** (limits[0] + 5)
+            b.v[s][0, :, 2:] = 0.0
+        for i, x in enumerate((b.k, b.v)):
+            c, e = b.codes[i][s] = ref.hold(x[s], *limits)
+            assert i == 0 or (e == limits[0]).all()
+            x[s] = c * 2.0 ** e[..., None].astype(np.float64)
+        b.fill(s)
+    b.q = rng.standard_normal((2 * new, 2 * group, dim)) * 0.5
+    b.q[:, :, 0] = 8.0
+    b.q = b.rounded(b.q)
+    out = b.cache().attend(b.q_gpu(), *b.index(), **b.front()).double().cpu().numpy()
+    h, scale = half_step(b.dtype), dim ** -0.5
+    tiny = float(torch.finfo(b.dtype).smallest_normal) * h
+    for s in range(2):
+        rows, pos = b.q[b.rows(s)], b.positions(s)
+        want, weight = ref.attend(rows, b.k[s], b.v[s], pos, scale)
+        big = np.linalg.norm(rows, axis=2).max() * np.linalg.norm(b.k[s], axis=2).max() * scale
+        ds = (dim + 8) * 2.0 ** -24 * big
+        tol = h * np.abs(want) + (h + 2 * ds + 2.0 ** -18) * (1 + h) * weight + 4 * tiny
+        if dtype == "f16":
+            tol += 2.0 ** -35 * np.repeat(np.cumsum(np.abs(b.v[s]), axis=0)[pos], group, axis=1)
+        elif gap > 17:
+            tol += 2.0 ** (-134 - limits[0]) * np.repeat(np.cumsum(np.abs(b.v[s]), axis=0)[pos], group, axis=1)
+        err = np.abs(out[b.rows(s)] - want)
+        log(f"least scale {dtype} gap {gap} dim {dim} new {new} shared {shared}: {float((err / tol).max()):.3f}")
+        assert np.all(err <= tol), (s, float((err / tol).max()))
+
+
+@pytest.mark.parametrize("new,before", [(1, 0), (1, 400), (5, 300), (90, 100)])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_the_largest_scales(new, before, dim):
+    """bf16 values up to the sums that the header allows: one of 2^127 alone, exactly, or hundreds of 2^107."""
+    torch = torch_cuda()
+    b = ExtBatch(torch, [(new, before)], 8, 2, dim, 16, torch.bfloat16, seed=new, filled=False)
+    most = 127.0 if new + before == 1 else 107.0
+    b.v[0] *= 2.0 ** most / np.abs(b.v[0]).max()
+    for i, x in enumerate((b.k, b.v)):
+        c, e = b.codes[i][0] = ref.hold(x[0], *LIMITS[str(b.dtype)])
+        x[0] = c * 2.0 ** e[..., None].astype(np.float64)
+    assert b.codes[1][0][1].max() == (119 if most == 127 else 99)
+    b.fill(0)
+    out = b.cache().attend(b.q_gpu(), *b.index())
+    if most == 127:
+        np.testing.assert_array_equal(out.double().cpu().numpy(), np.repeat(b.v[0], 4, axis=1))
+    else:
+        b.check(out)
+
+
 @pytest.mark.parametrize("seqs,row", [([(5, 60)], 2), ([(120, 40)], 50), ([(120, 700)], 119)])
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 def test_what_a_row_does_not_see_has_no_effect(seqs, row, dtype):
