@@ -412,7 +412,8 @@ typedef struct {
 
 /* The norm of each head's queries and keys before their turn:
  *   x_d / sqrt(mean of x^2 + eps) * weight_d
- * over all head_dim elements, the sum in fp32 (which elements of 2^60 overflow).  A NULL
+ * over all head_dim elements, the sum in fp32 (which elements of 2^60 overflow, and which
+ * loses a head whose elements are all below 2^-60, where eps does not outweigh them).  A NULL
  * weight: no norm there. */
 typedef struct {
   const void *q_weight, *k_weight; /* device [head_dim], 16-byte aligned */

@@ -179,6 +179,21 @@ def test_weights_of_one_without_a_norm():
     assert torch.equal(got, q)
 
 
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("size", [2.0 ** -60, 2.0 ** -20, 2.0 ** 20, 2.0 ** 55])
+def test_the_range_of_a_norm(dim, size):
+    """Elements of up to eight times `size`, eps 0: squares and their sum stay fp32's normal numbers, so that the
+    tolerance is as ever (what lies far below the largest counts for nothing in the sum)."""
+    torch = torch_cuda()
+    b = ExtBatch(torch, [(33, 3), (1, 9)], 4, 2, dim, 16, torch.bfloat16, held=False)
+    g = torch.Generator().manual_seed(dim)
+    q, k = (torch.randn(b.n, h, dim, generator=g).clamp(-4, 4) * 2 * size for h in (4, 2))
+    w = torch.rand(dim, generator=g) + 0.5
+    got = b.cache(rope_dim=0).append(k.cuda(), k.cuda(), *b.index(), q=q.cuda(), q_norm=w.cuda(), norm_eps=0.0)
+    want = ref.head_norm(q.double().numpy(), w.double().numpy(), 0.0)
+    assert (np.abs(got.double().cpu().numpy() - want) <= (2.0 ** -8 + (dim / 32 + 6) * 2.0 ** -24) * np.abs(want)).all()
+
+
 @pytest.mark.parametrize("held", [False, True])
 @pytest.mark.parametrize("heads,kv_heads,dim", [(7, 7, 64), (320, 64, 64), (1024, 1, 128), (130, 65, 256)])
 def test_any_number_of_heads(held, heads, kv_heads, dim):
