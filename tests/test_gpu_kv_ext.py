@@ -873,6 +873,37 @@ def test_streams_and_replayed_graphs(held):
             assert near <= 2 * half_step(b.dtype)
 
 
+@pytest.mark.parametrize("held", [False, True])
+def test_two_streams_at_once(held):
+    """All the operators on two batches, queued in turns on two streams without a wait between them, and a third
+    batch that both read: as one after the other."""
+    torch = torch_cuda()
+    w = torch.rand(128, device="cuda") + 0.5
+    sides = []
+    for seed, seqs, shared in ((1, [(1, 2000 + 40 * n) for n in range(40)], 1900), (2, [(90, 700), (5, 4000), (300, 600)], 600),
+                               (3, [(1, 500), (3, 3000)], 70)):
+        b = ExtBatch(torch, seqs, 8, 2, 128, 32, torch.bfloat16, held=held, shared=shared, seed=seed)
+        sides.append((b, b.cache(), b.q_gpu(), torch.randn(b.n, 2, 128, device="cuda").to(b.dtype)))
+    common, common_cache, common_q, _ = sides.pop()
+
+    def step(b, cache, q, k):
+        turned = cache.append(k, k, *b.index(), q=q, q_norm=w, k_norm=w)
+        return (turned, cache.attend(turned, *b.index(), **b.front()), cache.attend(turned, *b.index()),
+                *cache.read(b.n, *b.index()), common_cache.attend(common_q, *common.index(), **common.front()))
+
+    want = [step(*side) for side in sides]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sides]
+    got = []
+    for _ in range(20):
+        for i, (side, stream) in enumerate(zip(sides, streams)):
+            with torch.cuda.stream(stream):
+                got.append((i, step(*side)))
+    torch.cuda.synchronize()
+    for i, out in got:
+        assert all(torch.equal(x, y) for x, y in zip(out, want[i])), i
+
+
 def test_pages_past_32_bit_offsets():
     torch = torch_cuda()
     page_elems = 8 * 1024 * 128
