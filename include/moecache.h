@@ -454,7 +454,11 @@ typedef struct {
  * tables; the prefix's further pages are not read and may be anything.  What a number of
  * 8 bits stands for is multiplied as the batch's dtype holds it; in MOE_BF16 a probability p (the
  * largest of a row being 1) is off by up to 2^-134 / 2^e for a value of the power 2^e where p 2^e is below 2^-126,
- * a row therefore by at most 2^-125 for each such token. */
+ * a row therefore by at most 2^-125 for each such token.
+ * A prefix is for batches of many sequences with few new tokens each: every tile of rows leaves partial results
+ * in fp32, which takes a workspace of up to 8 times moe_kv_attend's, and where the new tokens are many,
+ * or the sequences or what they share few, more time than reading the shared tokens again does.  How finely they
+ * are cut goes by n_pages, which should therefore be no more than they fill. */
 int moe_kv_attend_ext(const moe_kv_batch *b, const moe_kv_scales *scales, const moe_kv_prefix *prefix, int32_t window,
                       float scale, const void *q, int64_t q_stride, void *out, int64_t out_stride, void *workspace,
                       uint64_t workspace_bytes);

@@ -7,8 +7,8 @@
 // head's sum and its largest magnitude are exchanged between lanes of one wave.  Values in 8 bits are
 // turned from tokens' rows to the cache's [D][8] through LDS where the run is whole.
 //
-// Bound by its launch in a decode step (64 tokens of 32 + 2 x 4 heads of 128: 5.2 us, in 8 bits 5.8; the
-// call's host side is 12), else by a wave's chain of loads, exchanges and stores over its heads, of which the next
+// Bound by its launch in a decode step (64 tokens of 32 + 2 x 4 heads of 128: 5.1 us, in 8 bits 6.3; the
+// call's host side is 10.7), else by a wave's chain of loads, exchanges and stores over its heads, of which the next
 // one's elements are requested ahead: 4096 tokens of them from fp32 in 8 bits, 122 MB, 28.3 us = 4.3 TB/s (31.1
 // without the request ahead, 31.7 with sines, cosines and weights kept in registers, which leaves two waves a SIMD);
 // 16384 from bf16, 319 MB, 70.5 us = 4.5 TB/s.

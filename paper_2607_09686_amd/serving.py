@@ -267,7 +267,9 @@ class KvCache:
         and shared (int32 [1], their number, none of them new) let these be read once for all: the
         same result but for rounding (moe_kv_prefix).  That is the first shared // 64 * 64 tokens; the
         others are read by way of pages, and prefix's entries for them may be anything.  Not with a
-        window."""
+        window.  It pays where many sequences have few new tokens (64 of one token behind 8192: 0.6 of
+        the time) and costs in chunks of prompts (up to 1.5 of it, and up to 8 times the workspace):
+        there leave it out, the pages hold these tokens too."""
         n, device, heads, dim = q.shape[0], self.device, self.n_heads, self.head_dim
         qp, qs = _rows(q, "q", self.dtype, heads, dim, n, device)
         if out is None:
